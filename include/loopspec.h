@@ -48,6 +48,7 @@ extern "C" {
 
 #define LOOPSPEC_F32 0
 #define LOOPSPEC_BF16 1
+#define LOOPSPEC_F16 2          /* paged caches and sampled logits only */
 
 typedef struct loopspec_handle* loopspec_t;
 
@@ -455,6 +456,112 @@ int loopspec_cascade(const loopspec_cascade_cfg* cfg, int32_t rows, const float*
 int loopspec_cascade_noalloc(const loopspec_cascade_cfg* cfg, int32_t rows, const float* z1_dev,
                              const float* z2_dev, const float* zR_dev, int64_t z_stride, const int32_t* keys_dev,
                              int32_t* out_dev, float* q1_dev, float* q2_dev, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A batch of sequences over a paged key/value cache, for serving loops that
+ * run their own layers: the append of a step's keys and values with the
+ * rotation on the way, attention of all sequences over one long prefix that
+ * they share and each over its own positions, and the draw of the next tokens.
+ * These calls need no handle, allocate nothing, use no memory but what they
+ * are given, wait for nothing and hold no state: they may be captured into a
+ * HIP graph.  The current device must be the stream's.  Calls that overlap
+ * must not share a workspace.
+ * ------------------------------------------------------------------------- */
+
+/* The cache: pages of page_size positions.  Key element d of head g of
+ * position s of page p lies at k_dev + p * k_page + g * k_head + s * k_pos + d
+ * (elements; values alike), so pages may hold heads or positions outermost.
+ * Strides are multiples of 8 and addresses of 16 bytes; k_pos >= head_dim. */
+typedef struct {
+    int32_t dtype;        /* LOOPSPEC_F16 or LOOPSPEC_BF16; queries and outputs have the same */
+    int32_t n_pages;
+    int32_t page_size;    /* a multiple of 16, up to 1024 */
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* 16, 32, 64, 96 or 128 */
+    void* k_dev;
+    void* v_dev;
+    int64_t k_page, k_head, k_pos;
+    int64_t v_page, v_head, v_pos;
+} loopspec_paged_cache;
+
+/* The sequences and this step's tokens.  Sequence b has seq_len[b] positions
+ * of its own, behind the prefix; its tokens in this step, q_start[b] ..
+ * q_start[b+1] - 1, stand at its last own positions (token q_start[b+1] - 1 at
+ * seq_len[b] - 1).  Own position s lies in page table[b][s / page_size], prefix
+ * position p in page prefix_table[p / page_size].  All arrays are device
+ * memory, read when the kernels run: a captured call follows their contents.
+ * Padding: a token of no sequence (below q_start[0], from q_start[n_seqs] on,
+ * or, without q_start, from n_seqs on) and the tokens of a sequence with
+ * seq_len < 0 are left out, and what a call would write for them stays as it
+ * is. */
+typedef struct {
+    int32_t n_seqs;
+    int32_t n_tokens;               /* rows of the queries */
+    const int32_t* q_start_dev;     /* [n_seqs + 1] ascending; NULL: token b is sequence b's only one */
+    const int32_t* seq_len_dev;     /* [n_seqs] own positions, with this step's tokens */
+    const int32_t* table_dev;       /* [n_seqs][table_stride], table_width of each row in use */
+    int64_t table_stride;
+    int32_t table_width;            /* table_width * page_size <= 2^28 */
+    int32_t prefix_len;             /* positions of the prefix, 0 .. 2^28 */
+    const int32_t* prefix_table_dev; /* ceil(prefix_len / page_size) pages (not read by loopspec_rope_append) */
+} loopspec_paged_batch;
+
+typedef struct {
+    int32_t n_heads;                /* query heads, a multiple of n_kv_heads */
+    int32_t rot_dim;                /* rotated elements of a head, a multiple of 16 up to head_dim; 0: no rotation */
+    float eps;                      /* of the norms */
+    const void *q_dev, *k_dev, *v_dev;  /* [n_tokens][heads][head_dim] by the strides below */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+    void* q_out_dev;                /* may be q_dev with its strides: in place */
+    int64_t out_token, out_head;
+    const double* freq_dev;         /* [rot_dim / 2] radians per position */
+    const float* q_norm_dev;        /* [head_dim] gains of the per-head RMSNorm, or NULL: no norm */
+    const float* k_norm_dev;
+} loopspec_rope_args;
+
+/* Queries, keys and values of a step's tokens.  Queries and keys: RMSNorm over
+ * each head (when gains are given), then the rotate-half rotation of the first
+ * rot_dim elements by position * freq (position = prefix_len + own position),
+ * in fp32 from angles reduced in 64 bits, rounded once.  Queries go to q_out,
+ * keys and values to their sequence's page.  A token before its sequence's
+ * first position is padding; one whose page the table does not name, or names
+ * outside the cache, gets its query but no key or value.  Two tokens that the
+ * tables send to one place leave one of the two there, or parts of both.
+ * Errors: EINVAL (arguments, checked before any launch), EHIP. */
+int loopspec_rope_append(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch,
+                         const loopspec_rope_args* args, void* stream);
+
+typedef struct {
+    int32_t n_heads;                /* query heads, a multiple of n_kv_heads: head h reads key/value head h / (n_heads / n_kv_heads) */
+    float scale;                    /* > 0; scores are scale * q . k */
+    const void* q_dev;              /* [n_tokens][n_heads][head_dim] by the strides below */
+    int64_t q_token, q_head;
+    void* out_dev;
+    int64_t out_token, out_head;
+    float* lse_dev;                 /* [n_tokens][n_heads] log of the sum of exp(score), or NULL */
+} loopspec_attention_args;
+
+/* Bytes of device workspace loopspec_prefix_attention needs (0 for arguments
+ * it refuses): a row's partial result per chunk of positions. */
+uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch,
+                                                   int32_t n_heads);
+
+/* Attention of the step's queries: each sees the whole prefix and its own
+ * sequence's positions up to its own place.  The prefix's keys and values are
+ * read once for all sequences (once per 64 rows, rows = tokens x query heads
+ * of a key/value head).  A row that sees nothing gives zeros and an lse of
+ * -infinity.  What lies behind a sequence's positions in its pages, and the
+ * positions that a row does not see, have no influence on it, whatever they
+ * hold.  A visible position whose page lies outside the table or the cache
+ * makes the rows that see it NaN; no memory outside the cache is read.
+ * Products are of the cache's type with fp32 sums; the weights exp(s - m) are
+ * rounded to that type.  A row's result does not depend on the other
+ * sequences' contents.  workspace: 16-byte aligned, its contents on entry do
+ * not matter.  Errors: EINVAL (arguments, workspace too small; checked before
+ * any launch), EHIP. */
+int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch,
+                              const loopspec_attention_args* args, void* workspace_dev, uint64_t workspace_bytes,
+                              void* stream);
 
 /* Library version string. */
 const char* loopspec_version(void);

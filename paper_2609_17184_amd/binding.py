@@ -16,7 +16,7 @@ import numpy as np
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "libloopspec.so")
 
 OK, EINVAL, ENOMEM, EHIP, ECAPACITY, ESTATE, ENUMERIC = 0, -1, -2, -3, -4, -5, -6
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 
 
 class Dims(ctypes.Structure):
@@ -62,6 +62,32 @@ class CascadeCfg(ctypes.Structure):
 class Branch(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "active", "seq", "pos", "depth", "token", "parent", "tdone", "x1", "x2", "gate")]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads", "head_dim")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v")] + [
+        (n, ctypes.c_int64) for n in ("k_page", "k_head", "k_pos", "v_page", "v_head", "v_pos")]
+
+
+class PagedBatchC(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("q_start", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("table_width", ctypes.c_int32), ("prefix_len", ctypes.c_int32), ("prefix_table", ctypes.c_void_p)]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("eps", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("q", "k", "v")] + [
+        (n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head")] + [
+        ("q_out", ctypes.c_void_p), ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64),
+        ("freq", ctypes.c_void_p), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p)]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("scale", ctypes.c_float), ("q", ctypes.c_void_p),
+                ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64), ("lse", ctypes.c_void_p)]
 
 
 class LoopSpecError(RuntimeError):
@@ -130,6 +156,11 @@ def load_library() -> ctypes.CDLL:
                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64,
                                             ctypes.c_void_p]),
+        "loopspec_rope_append": (ctypes.c_int, [P(PagedCacheC), P(PagedBatchC), P(RopeArgs), ctypes.c_void_p]),
+        "loopspec_prefix_attention_workspace_bytes": (ctypes.c_uint64, [P(PagedCacheC), P(PagedBatchC),
+                                                                        ctypes.c_int32]),
+        "loopspec_prefix_attention": (ctypes.c_int, [P(PagedCacheC), P(PagedBatchC), P(AttentionArgs),
+                                                     ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
