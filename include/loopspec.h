@@ -563,6 +563,38 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
                               const loopspec_attention_args* args, void* workspace_dev, uint64_t workspace_bytes,
                               void* stream);
 
+typedef struct {
+    int32_t vocab;                  /* V, 1 .. 262144 */
+    int32_t dtype;                  /* of the logits: LOOPSPEC_F32, LOOPSPEC_BF16 or LOOPSPEC_F16 */
+    /* settings of every row, or (device pointers, [rows]) of each: */
+    float temperature;              /* >= 0; 0: the largest logit, ties to the lowest id */
+    int32_t top_k;                  /* the first k ranks; <= 0: all */
+    float top_p;                    /* (0, 1]; 1: all */
+    float min_p;                    /* [0, 1] */
+    const float* temperature_dev;   /* NULL: the value above */
+    const int32_t* top_k_dev;
+    const float* top_p_dev;
+    const float* min_p_dev;
+} loopspec_sample_cfg;
+
+/* Draw one token per row of logits (row i at logits_dev + i * stride elements;
+ * stride 0: the same logits for every row) with the row's uniform number u_dev[i]
+ * in [0, 1).  With w_v = exp((z_v - max z) / temperature) and ids ranked by
+ * (logit descending, id ascending): top-k keeps the first top_k ranks; top-p
+ * keeps, of those, the ranks whose preceding weight is below top_p of the top-k
+ * weight; min-p keeps, of those, w_v >= min_p (the largest has w = 1).  The token
+ * is the smallest id whose kept weight through it exceeds u * kept weight.
+ * Logits of -infinity are never kept.  token_dev[i]: the token; prob_dev[i] (may
+ * be NULL): its share of the kept weight; kept_dev[i] (may be NULL): how many
+ * ids were kept.  Weights are 64-bit, sums exact in units of 2^-44 of the
+ * largest weight, so the draw does not depend on the order of adding; a weight
+ * below half a unit is kept and counted but not drawn.
+ * A row with a NaN or +infinity among its logits, without a finite one, or whose
+ * settings or number are outside their ranges gives token -1, prob 0, kept 0.
+ * Asynchronous, no workspace.  Errors: EINVAL (arguments), EHIP. */
+int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* logits_dev, int64_t stride,
+                    const double* u_dev, int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* stream);
+
 /* Library version string. */
 const char* loopspec_version(void);
 

@@ -90,6 +90,12 @@ class AttentionArgs(ctypes.Structure):
                 ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64), ("lse", ctypes.c_void_p)]
 
 
+class SampleCfg(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
+                ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("temperature_dev", "top_k_dev", "top_p_dev", "min_p_dev")]
+
+
 class LoopSpecError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"loopspec error {code}: {msg}")
@@ -161,6 +167,9 @@ def load_library() -> ctypes.CDLL:
                                                                         ctypes.c_int32]),
         "loopspec_prefix_attention": (ctypes.c_int, [P(PagedCacheC), P(PagedBatchC), P(AttentionArgs),
                                                      ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
+        "loopspec_sample": (ctypes.c_int, [P(SampleCfg), ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)

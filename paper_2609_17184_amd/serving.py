@@ -168,3 +168,37 @@ def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] 
     _check(_launch(cache.device, L.loopspec_prefix_attention, cache._ref, ref, ctypes.byref(a), ws.data_ptr(), nbytes),
            "loopspec_prefix_attention")
     return (out, lse) if return_lse else out
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One token per row of logits [rows, vocab] (float32, bfloat16 or float16; rows may be strided or expanded) with
+    the row's uniform number u [rows] (float64, in [0, 1)): temperature (0: the largest logit), then top_k (<= 0:
+    all), top_p and min_p (relative to the likeliest token), each a number or a tensor [rows] (float32; top_k int32).
+    Returns (tokens int32, their probabilities among the kept ids float32, number of kept ids int32), [rows] each;
+    a row that cannot be drawn from (NaN or +infinity, no finite logit, settings out of range) gives (-1, 0, 0)."""
+    import torch
+    _need(logits.dim() == 2 and logits.is_cuda and _dtype(logits) >= 0, "logits: [rows, vocab] float32, bfloat16 or "
+          "float16 on a GPU")
+    rows, vocab = logits.shape
+    dev = logits.device
+    _need(vocab == 1 or logits.stride(1) == 1, "logits: a row's elements next to each other")
+    _need(u.dtype == torch.float64 and u.shape == (rows,) and u.is_contiguous() and u.device == dev,
+          "u: float64 [rows] on the logits' device")
+    values, arrays = [], []
+    for name, x, kind in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                          ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if torch.is_tensor(x):
+            _need(x.dtype == kind and x.shape == (rows,) and x.is_contiguous() and x.device == dev,
+                  f"{name}: a number or {kind} [rows] on the logits' device")
+            values.append(0)
+            arrays.append(x.data_ptr())
+        else:
+            values.append(x)
+            arrays.append(None)
+    cfg = B.SampleCfg(vocab, _dtype(logits), *values, *arrays)
+    token, kept = torch.empty((2, rows), dtype=torch.int32, device=dev)
+    prob = torch.empty(rows, dtype=torch.float32, device=dev)
+    _check(_launch(dev, B.load_library().loopspec_sample, ctypes.byref(cfg), rows, logits.data_ptr(),
+                   logits.stride(0), u.data_ptr(), token.data_ptr(), prob.data_ptr(), kept.data_ptr()),
+           "loopspec_sample")
+    return token, prob, kept

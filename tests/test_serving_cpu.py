@@ -112,3 +112,24 @@ def test_binding_checks_tensors():
             serving.PagedCache(kk, vv)                      # host memory, shape, types
     with pytest.raises(ValueError):
         serving.Batch(torch.zeros(3, dtype=torch.int32), torch.zeros((3, 4), dtype=torch.int32))
+
+
+def _sample_rc(rows=4, logits=FAKE, stride=1000, u=FAKE, token=FAKE, **kw):
+    c = dict(vocab=1000, dtype=B.F32, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    c.update(kw)
+    cfg = B.SampleCfg(**c)
+    return B.load_library().loopspec_sample(ctypes.byref(cfg), rows, logits, stride, u, token, None, None, None)
+
+
+@pytest.mark.parametrize("bad", [dict(vocab=0), dict(vocab=262145), dict(dtype=3), dict(temperature=-0.5),
+                                 dict(temperature=float("nan")), dict(temperature=float("inf")), dict(top_p=0.0),
+                                 dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1),
+                                 dict(rows=-1), dict(logits=None), dict(logits=FAKE + 2), dict(stride=-1), dict(u=None),
+                                 dict(token=None)], ids=str)
+def test_bad_samples(bad):
+    assert _sample_rc(**bad) == B.EINVAL
+
+
+def test_sample_of_no_rows():
+    assert _sample_rc(rows=0) == B.OK
+    assert B.load_library().loopspec_sample(None, 1, FAKE, 10, FAKE, FAKE, None, None, None) == B.EINVAL
