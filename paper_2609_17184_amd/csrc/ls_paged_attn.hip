@@ -40,6 +40,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kAThreads = 256;
 constexpr int kATile = 32;                    // positions per wave and step
 constexpr int kAStep = 4 * kATile;            // positions per workgroup and step
+constexpr float kNone = -3e38f;               // the reference before the first score
 constexpr float kRaise = 8.0f, kLift = 7.0f;  // log2 of what a weight may exceed the reference's by; of the reference's weight
 
 struct AttnArgs {
@@ -50,11 +51,11 @@ struct AttnArgs {
     float* lse;
     float* part;                              // [rows][splits][D], rows = tokens x heads
     float* ml;                                // [rows][splits][2]: reference (base 2), sum
-    float c;                                  // scale * log2(e)
+    float c, rc;                              // scale * log2(e), and its reciprocal
     int H, per;                               // query heads; per key/value head
     int NP, pchunk;                           // prefix: chunks, positions per chunk
     int NO, ochunk;                           // own positions: chunks at most, positions per chunk
-    int rb;                                   // row blocks of the prefix
+    int rb, rows;                             // prefix: row blocks, rows of a block
     int ptasks;                               // workgroups of the prefix
 };
 
@@ -70,31 +71,38 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     if (BF) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
     return pack_h2(a, b);
 }
-// both halves of a word finite
 template <bool BF>
-__device__ __forceinline__ bool finite2(uint32_t w) {
+__device__ __forceinline__ bool finite16(uint32_t w) {
     constexpr uint32_t e = BF ? 0x7F80u : 0x7C00u;
-    return (w & e) != e && ((w >> 16) & e) != e;
+    return (w & e) != e;
+}
+// the halves of a word that are finite; *all becomes false when one is not
+template <bool BF>
+__device__ __forceinline__ uint32_t sane(uint32_t w, bool* all) {
+    const uint32_t k = (finite16<BF>(w) ? 0xFFFFu : 0u) | (finite16<BF>(w >> 16) ? 0xFFFF0000u : 0u);
+    *all = *all && k == ~0u;
+    return w & k;
 }
 
-// D/16 consecutive 16-bit columns of one position
+// D/16 consecutive 16-bit columns of one position: `off` bytes behind a
+// wave-uniform address
 template <int E>
 struct VRow {
     uint32_t w[(E + 1) / 2];
-    __device__ __forceinline__ void load(const uint16_t* p) {
+    __device__ __forceinline__ void load(const char* p, uint32_t off) {
         if constexpr (E == 8) {
-            const u32x4 u = *(const u32x4*)p;
+            const u32x4 u = *(const u32x4*)(p + off);
             w[0] = u[0], w[1] = u[1], w[2] = u[2], w[3] = u[3];
         } else if constexpr (E == 6) {
-            const uint32_t* q = (const uint32_t*)p;         // 12 bytes, 4-byte aligned
+            const uint32_t* q = (const uint32_t*)(p + off);         // 12 bytes, 4-byte aligned
             w[0] = q[0], w[1] = q[1], w[2] = q[2];
         } else if constexpr (E == 4) {
-            const u32x2 u = *(const u32x2*)p;
+            const u32x2 u = *(const u32x2*)(p + off);
             w[0] = u[0], w[1] = u[1];
         } else if constexpr (E == 2) {
-            w[0] = *(const uint32_t*)p;
+            w[0] = *(const uint32_t*)(p + off);
         } else {
-            w[0] = *p;
+            w[0] = *(const uint16_t*)(p + off);
         }
     }
     __device__ __forceinline__ void zero() {
@@ -112,20 +120,18 @@ struct AttnTask {
     int lim0;                                 // visible positions of token tok0; token tok0 + i sees i more (own positions)
     bool causal;
     int split;                                // where the partials go
+
+    __device__ __forceinline__ int token(int r, int per) const { return tok0 + (r0 + r) / per; }
+    // visible positions of row r, within the task's
+    __device__ __forceinline__ int limit(int r, int per) const { return causal ? min(p1, lim0 + (r0 + r) / per) : p1; }
 };
 
-template <bool BF, int D, int NR>
-struct Attend {
-    static constexpr int E = D / 16, NS = (D + 31) / 32, LDO = D + 4;
-    struct Lds {
-        u32x4 q[NR][NS][64];
-        float o[4][16][LDO];
-        float ml[4][NR * 16][2];
-    };
-    struct Tile {
-        u32x4 k[2][NS];
-        VRow<E> v[8];
-    };
+// Keys and values of 32 positions in a wave's registers.
+template <bool BF, int D>
+struct Tile {
+    static constexpr int E = D / 16, NS = (D + 31) / 32;
+    u32x4 k[2][NS];
+    VRow<E> v[8];
 
     // page of the 16 positions from p; -1 when the table names none of the cache's
     static __device__ __forceinline__ int look(const PagedCache& c, const AttnTask& t, int p) {
@@ -135,254 +141,476 @@ struct Attend {
         const int id = ld_uniform(t.table + i);
         return (unsigned)id < (unsigned)c.n_pages ? id : -1;
     }
-
-    static __device__ __forceinline__ void load(const PagedCache& c, const AttnTask& t, int p, const int (&id)[2], Tile& x) {
+    // address of the 16 positions from p in page id (any page for a masked or missing one)
+    static __device__ __forceinline__ const char* spot(const PagedCache& c, const uint16_t* b, int64_t page, int64_t head, int64_t pos,
+                                                       int g, int p, int id) {
+        const unsigned blk = (unsigned)p >> 4, off = (blk - unit_div(blk, c.magic) * c.unit) * kPageUnit;
+        return (const char*)(b + (id < 0 ? 0 : id) * page + g * head + off * pos);
+    }
+    __device__ __forceinline__ void load_k(const PagedCache& c, const AttnTask& t, int p, const int (&id)[2]) {
         const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+        const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            const unsigned blk = ((unsigned)p >> 4) + a;
-            const int64_t off = (int64_t)(blk - unit_div(blk, c.magic) * c.unit) * kPageUnit;
-            const int64_t pg = id[a] < 0 ? 0 : id[a];
-            const uint16_t* kb = c.k + pg * c.kp + t.g * c.kh + off * c.ks;
-            const uint16_t* vb = c.v + pg * c.vp + t.g * c.vh + off * c.vs;
-            const int ko = n * (int)c.ks + 8 * gq, vo = 4 * gq * (int)c.vs + E * n;
+            const char* b = spot(c, c.k, c.kp, c.kh, c.ks, t.g, p + 16 * a, id[a]);
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 if (D % 32 == 0 || gq < 2)
-                    x.k[a][s] = *(const u32x4*)(kb + ko + 32 * s);
+                    k[a][s] = *(const u32x4*)(b + 64 * s + lo);
                 else
-                    x.k[a][s] = u32x4{0, 0, 0, 0};
+                    k[a][s] = u32x4{0, 0, 0, 0};
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.v[a * 4 + i].load(vb + vo + i * (int)c.vs);
         }
     }
+    __device__ __forceinline__ void load_v(const PagedCache& c, const AttnTask& t, int p, const int (&id)[2]) {
+        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+        const uint32_t lo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const char* b = spot(c, c.v, c.vp, c.vh, c.vs, t.g, p + 16 * a, id[a]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[a * 4 + i].load(b + i * (2 * c.vs), lo);
+        }
+    }
+    // the lane's position of row i of v, from the tile's first
+    static __device__ __forceinline__ int place(int i) { return 16 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (i & 3); }
+    // operand of 32 positions for the columns E * (lane % 16) + e
+    __device__ __forceinline__ u32x4 column(int e) const {
+        u32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            r[j] = __builtin_amdgcn_perm(v[2 * j + 1].w[e / 2], v[2 * j].w[e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+        return r;
+    }
+    // Values that no row sees do not reach the second product, whatever they hold: zero from `end` on.
+    __device__ __forceinline__ void cut(int p, int end) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (p + place(i) >= end) v[i].zero();
+    }
+    // Zero where not finite; true when the wave has met any.
+    __device__ __forceinline__ bool sane() {
+        bool f = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < (E + 1) / 2; ++j) v[i].w[j] = ls::sane<BF>(v[i].w[j], &f);
+        return __any(!f);
+    }
+};
 
-    static __device__ void run(const PagedCache& c, const AttnArgs& a, const AttnTask& t, Lds& l) {
-        const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, gq = lane >> 4;
-        __syncthreads();                                            // an earlier task's LDS is read out
-        for (int i = tid; i < NR * NS * 64; i += kAThreads) {
-            const int la = i & 63, s = (i >> 6) % NS, rt = (i >> 6) / NS, r = rt * 16 + (la & 15), d = 32 * s + 8 * (la >> 4);
-            u32x4 u = {0, 0, 0, 0};
-            if (r < t.rows && d < D) {
-                const int rr = t.r0 + r, tok = t.tok0 + rr / a.per, h = t.g * a.per + rr % a.per;
-                u = *(const u32x4*)(a.q + tok * a.qt + h * a.qh + d);
-            }
-            l.q[rt][s][la] = u;
-        }
-        // visible positions of the lane's row in each row tile, and of the block's first and last row
-        int lim[NR], minlim = t.p1, maxlim = t.p1;
+__device__ __forceinline__ size_t part_slot(const AttnArgs& a, const AttnTask& t, int r) {
+    return ((size_t)t.token(r, a.per) * a.H + t.g * a.per + (t.r0 + r) % a.per) * (a.NP + a.NO) + t.split;
+}
+
+// NR tiles of 16 rows in a wave: output (transposed, lane = row), reference of
+// the exponent and the lane's share of the sum.
+template <bool BF, int D, int NR>
+struct Rows {
+    static constexpr int E = D / 16, NS = (D + 31) / 32;
+    f32x4 o[NR][E];
+    float ref[NR], sum[NR];                   // weights are 2^(c * score - ref)
+
+    __device__ __forceinline__ void start() {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
-            const int r = rt * 16 + n;
-            lim[rt] = r < t.rows ? t.p1 : 0;
-            if (t.causal && r < t.rows) lim[rt] = min(t.p1, t.lim0 + (t.r0 + r) / a.per);
-        }
-        if (t.causal) {
-            minlim = min(t.p1, t.lim0 + t.r0 / a.per);
-            maxlim = min(t.p1, t.lim0 + (t.r0 + t.rows - 1) / a.per);
-        }
-        f32x4 o[NR][E];
-        float m[NR], mc[NR], sum[NR];
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            m[rt] = -INFINITY, mc[rt] = 0.f, sum[rt] = 0.f;
+            ref[rt] = kNone, sum[rt] = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        __syncthreads();
-
-        const float raise = kRaise / a.c;
-        Tile cur, nxt;
-        int id[2], id_n[2];
-        int p = t.p0 + kATile * w;
-        if (p < t.p1) {
-            id[0] = look(c, t, p), id[1] = look(c, t, p + 16);
-            load(c, t, p, id, cur);
-            id_n[0] = look(c, t, p + kAStep), id_n[1] = look(c, t, p + kAStep + 16);
+    }
+    // positions from `lim` on do not count for the lane's row
+    static __device__ __forceinline__ void hide(int lim, int p, f32x4 (&s)[2]) {
+        const int gq = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (p + 4 * gq + i >= lim) s[0][i] = -INFINITY;
+            if (p + 16 + 4 * gq + i >= lim) s[1][i] = -INFINITY;
         }
-        for (; p < t.p1; p += kAStep) {
-            int id_2[2] = {0, 0};
-            if (p + kAStep < t.p1) {
-                load(c, t, p + kAStep, id_n, nxt);
-                id_2[0] = look(c, t, p + 2 * kAStep), id_2[1] = look(c, t, p + 2 * kAStep + 16);
-            }
-            // positions no row sees do not reach the second product, whatever they hold
-            if (p + kATile > t.p1) {
+    }
+    static __device__ __forceinline__ float top(const f32x4 (&s)[2]) {
+        return fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    }
+    __device__ __forceinline__ bool high(int rt, float mx, const AttnArgs& a) const { return fmaf(mx, a.c, -ref[rt]) > kLift + kRaise; }
+    // a new reference: the largest score so far gets the weight 2^kLift
+    __device__ __forceinline__ void raise(int rt, float mx, const AttnArgs& a) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float now = fmaxf(ref[rt], fmaf(mx, a.c, -kLift)), al = __builtin_amdgcn_exp2f(ref[rt] - now);
+        ref[rt] = now;
+        sum[rt] *= al;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (p + 16 * (i >> 2) + 4 * gq + (i & 3) >= t.p1) cur.v[i].zero();
-            }
-            u32x4 vt[E];
+        for (int e = 0; e < E; ++e) o[rt][e] *= al;
+    }
+    __device__ __forceinline__ u32x4 weights(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
+        float x[2][4];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    vt[e][j] = __builtin_amdgcn_perm(cur.v[2 * j + 1].w[e / 2], cur.v[2 * j].w[e / 2],
-                                                     (e & 1) ? 0x07060302u : 0x05040100u);
-            const bool masked = p + kATile > minlim, bad = (id[0] | id[1]) < 0;
-            // some positions hidden from some rows only: a value there that is not finite would reach
-            // them as 0 * value
-            bool apart = false;
-            if (masked && minlim != maxlim) {
-                bool f = true;
+            for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.c, -ref[rt]));
+        sum[rt] += ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
+        return u32x4{pack2<BF>(x[0][0], x[0][1]), pack2<BF>(x[0][2], x[0][3]), pack2<BF>(x[1][0], x[1][1]), pack2<BF>(x[1][2], x[1][3])};
+    }
+    // O += V^T P
+    __device__ __forceinline__ void add(const Tile<BF, D>& x, const u32x4 (&p)[NR]) {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
+        for (int e = 0; e < E; ++e) {
+            const u32x4 vt = x.column(e);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f = f && finite2<BF>(vt[e][j]);
-                apart = __any(!f);
-            }
-#pragma unroll
-            for (int rt = 0; rt < NR; ++rt) {
-                if (rt && rt * 16 >= t.rows) break;
-                f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const u32x4 qf = l.q[rt][s][lane];
-                    s0 = mfma16<BF>(cur.k[0][s], qf, s0);
-                    s1 = mfma16<BF>(cur.k[1][s], qf, s1);
-                }
-                if (masked || bad) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (id[0] < 0) s0[i] = NAN;
-                        if (id[1] < 0) s1[i] = NAN;
-                        if (p + 4 * gq + i >= lim[rt]) s0[i] = -INFINITY;
-                        if (p + 16 + 4 * gq + i >= lim[rt]) s1[i] = -INFINITY;
-                    }
-                }
-                float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-                if (__any(mx > m[rt] + raise)) {
-                    mx = fmaxf(mx, __shfl_xor(mx, 16));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32));
-                    const float mn = fmaxf(m[rt], mx);
-                    const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[rt] - mn) * a.c);
-                    m[rt] = mn;
-                    mc[rt] = mn == -INFINITY ? 0.f : mn * a.c - kLift;
-                    sum[rt] *= al;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[rt][e] *= al;
-                }
-                float e0[4], e1[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e0[i] = __builtin_amdgcn_exp2f(fmaf(s0[i], a.c, -mc[rt]));
-                    e1[i] = __builtin_amdgcn_exp2f(fmaf(s1[i], a.c, -mc[rt]));
-                }
-                sum[rt] += ((e0[0] + e0[1]) + (e0[2] + e0[3])) + ((e1[0] + e1[1]) + (e1[2] + e1[3]));
-                const u32x4 pf = {pack2<BF>(e0[0], e0[1]), pack2<BF>(e0[2], e0[3]), pack2<BF>(e1[0], e1[1]), pack2<BF>(e1[2], e1[3])};
-                if (!apart) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[rt][e] = mfma16<BF>(vt[e], pf, o[rt][e]);
-                } else {
-                    // one product per limit, over the positions below it, for the rows that have it
-                    const int mine = min(lim[rt], p + kATile);
-                    for (int lm = max(minlim, p); lm <= min(maxlim, p + kATile); ++lm) {
-                        uint32_t keep[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int pos = p + 16 * (j >> 1) + 4 * gq + 2 * (j & 1);
-                            keep[j] = (pos < lm ? 0xFFFFu : 0u) | (pos + 1 < lm ? 0xFFFF0000u : 0u);
-                        }
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            u32x4 vm;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) vm[j] = vt[e][j] & keep[j];
-                            const f32x4 part = mfma16<BF>(vm, pf, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[rt][e][i] = mine == lm ? o[rt][e][i] + part[i] : o[rt][e][i];
-                        }
-                    }
-                }
-            }
-            cur = nxt;
-            id[0] = id_n[0], id[1] = id_n[1];
-            id_n[0] = id_2[0], id_n[1] = id_2[1];
+            for (int rt = 0; rt < NR; ++rt) o[rt][e] = mfma16<BF>(vt, p[rt], o[rt][e]);
         }
-
-        // the four waves meet
+    }
+    // What values that are not finite contribute: the products' operand has zeros in their places, since a
+    // zero weight would not keep them out of the rows that do not see them.
+    __device__ __forceinline__ void add_odd(const PagedCache& c, const AttnTask& t, int p, const int (&lim)[NR]) {
+        const int gq = (threadIdx.x & 63) >> 4;
+        for (int i = 0; i < kATile && p + i < t.p1; ++i) {
+            const int id = Tile<BF, D>::look(c, t, p + i);
+            const uint16_t* row = (const uint16_t*)Tile<BF, D>::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p + i, id) +
+                                  ((p + i) & 15) * c.vs + 4 * E * gq;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const uint16_t b = row[E * k + e];
+                    if (finite16<BF>(b)) continue;
+                    const float v = BF ? __uint_as_float((uint32_t)b << 16) : h2f(b);
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt)
+                        if (p + i < lim[rt]) o[rt][e][k] += v;
+                }
+        }
+    }
+    __device__ __forceinline__ void finish() {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
             sum[rt] += __shfl_xor(sum[rt], 16);
             sum[rt] += __shfl_xor(sum[rt], 32);
-            if (gq == 0) {
-                l.ml[w][rt * 16 + n][0] = m[rt] == -INFINITY ? -INFINITY : mc[rt];
-                l.ml[w][rt * 16 + n][1] = sum[rt];
-            }
         }
-        __syncthreads();
-        const int S = a.NP + a.NO;
+    }
+    // row rt * 16 + lane % 16 of the block, without a workgroup's other waves
+    __device__ __forceinline__ void store(const AttnArgs& a, const AttnTask& t, int row0) {
+        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+        finish();
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
-            if (rt * 16 >= t.rows) break;
-            const int r = rt * 16 + n;
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, l.ml[i][r][0]);
-            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l.ml[w][r][0] - top);
+            const int r = row0 + rt * 16 + n;
+            if (r >= t.rows) continue;
+            const size_t slot = part_slot(a, t, r);
+            float* p = a.part + slot * D + 4 * E * gq;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) l.o[w][n][4 * E * gq + E * i + e] = o[rt][e][i] * f;
-            __syncthreads();
-            for (int i = tid; i < 16 * (D / 4); i += kAThreads) {
-                const int rr = i / (D / 4), d = i % (D / 4) * 4, row = rt * 16 + rr;
-                if (row >= t.rows) continue;
-                f32x4 v = *(const f32x4*)&l.o[0][rr][d];
-#pragma unroll
-                for (int k = 1; k < 4; ++k) v += *(const f32x4*)&l.o[k][rr][d];
-                const int gr = t.r0 + row;
-                const size_t slot = ((size_t)(t.tok0 + gr / a.per) * a.H + t.g * a.per + gr % a.per) * S + t.split;
-                *(f32x4*)(a.part + slot * D + d) = v;
-                if (d == 0) {
-                    float tp = -INFINITY, sm = 0.f;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        sm += l.ml[k][row][1] * (tp == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp));
-                    a.ml[slot * 2] = tp;
-                    a.ml[slot * 2 + 1] = sm;
-                }
-            }
-            __syncthreads();
+                for (int e = 0; e < E; ++e) p[E * i + e] = o[rt][e][i];
+            if (gq == 0) a.ml[slot * 2] = ref[rt], a.ml[slot * 2 + 1] = sum[rt];
         }
     }
 };
 
-// One launch: workgroups below ptasks take the prefix (key/value head, chunk,
-// row block), the others walk the own positions' tasks (sequence, chunk, row
-// block, key/value head), whose number only the device knows.
+// Few rows (16 or 32): Q in registers, the next tile's loads in flight under
+// the current one's products.  The wave takes the tiles p, p + step, ...
 template <bool BF, int D, int NR>
-__global__ void __launch_bounds__(kAThreads, NR > 2 ? 1 : 2) k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
-    using A = Attend<BF, D, NR>;
-    __shared__ typename A::Lds l;
-    constexpr int RT = 16 * NR;
-    if ((int)blockIdx.x < a.ptasks) {
-        // the row blocks of one chunk follow each other on one XCD (workgroups go round the 8 XCDs)
-        const int j = blockIdx.x / 8, pair = j / a.rb * 8 + blockIdx.x % 8, rb = j % a.rb;
-        if (pair >= c.G * a.NP) return;
-        AttnTask t;
-        t.table = b.prefix_table;
-        t.width = (b.prefix + c.unit * kPageUnit - 1) / (c.unit * kPageUnit);
-        t.g = pair % c.G;
-        t.split = pair / c.G;
-        t.p0 = t.split * a.pchunk;
-        t.p1 = min(t.p0 + a.pchunk, b.prefix);
-        t.tok0 = 0;
-        t.r0 = rb * RT;
-        t.rows = min(RT, b.T * a.per - t.r0);
-        t.lim0 = 0;
-        t.causal = false;
-        A::run(c, a, t, l);
-        return;
+__device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, const AttnTask& t, int p, int step, Rows<BF, D, NR>& r) {
+    constexpr int NS = (D + 31) / 32;
+    using T = Tile<BF, D>;
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+    T x, y;
+    int id[2] = {T::look(c, t, p), T::look(c, t, p + 16)}, nx[2] = {0, 0};
+    r.start();
+    if (p >= t.p1) return;
+    x.load_k(c, t, p, id);
+    x.load_v(c, t, p, id);
+    nx[0] = T::look(c, t, p + step), nx[1] = T::look(c, t, p + step + 16);
+    u32x4 q[NR][NS];
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        const int i = rt * 16 + n, tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            q[rt][s] = u32x4{0, 0, 0, 0};
+            if (i < t.rows && 32 * s + 8 * gq < D) q[rt][s] = *(const u32x4*)(a.q + tok * a.qt + h * a.qh + 32 * s + 8 * gq);
+        }
     }
-    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
-    const int lane = threadIdx.x & 63;
+    const int lo = t.limit(0, a.per), hi = t.limit(t.rows - 1, a.per);
+    f32x4 s[NR][2];
+    u32x4 w[NR];
+    auto scores = [&]() {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                s[rt][0] = mfma16<BF>(x.k[0][k], q[rt][k], s[rt][0]);
+                s[rt][1] = mfma16<BF>(x.k[1][k], q[rt][k], s[rt][1]);
+            }
+        }
+    };
+    auto soften = [&]() {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            const float mx = r.top(s[rt]);
+            if (__any(r.high(rt, mx, a))) r.raise(rt, mx, a);
+            w[rt] = r.weights(rt, s[rt], a);
+        }
+    };
+    int bad = 0;
+    for (; p + kATile <= lo; p += step) {
+        const int nn[2] = {T::look(c, t, p + 2 * step), T::look(c, t, p + 2 * step + 16)};
+        if (p + step < t.p1) {
+            y.load_k(c, t, p + step, nx);
+            y.load_v(c, t, p + step, nx);
+        }
+        bad |= id[0] | id[1];
+        scores();
+        soften();
+        r.add(x, w);
+        x = y;
+        id[0] = nx[0], id[1] = nx[1], nx[0] = nn[0], nx[1] = nn[1];
+    }
+    if (bad < 0)
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) r.sum[rt] = NAN;
+    int lim[NR];                              // visible positions of the lane's row
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) lim[rt] = rt * 16 + n < t.rows ? t.limit(rt * 16 + n, a.per) : 0;
+    while (p < t.p1) {
+        scores();
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) r.hide(lim[rt], p, s[rt]);
+        soften();
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (id[h] < 0 && p + 16 * h < lim[rt]) r.sum[rt] = NAN;
+        x.cut(p, t.p1);
+        const bool odd = lo != hi && x.sane();
+        r.add(x, w);
+        if (odd) r.add_odd(c, t, p, lim);
+        p += step;
+        if (p >= t.p1) break;
+        id[0] = T::look(c, t, p), id[1] = T::look(c, t, p + 16);
+        x.load_k(c, t, p, id);
+        x.load_v(c, t, p, id);
+    }
+}
+
+// Many rows: the four waves share the positions and each has its own 16 * NR
+// rows, Q in registers.  A stage of 64 positions comes to LDS in operand order
+// (a wave brings 16 positions, in registers while the stage before is worked
+// on) and every wave reads all of it.
+constexpr int kStage = 64;
+
+template <int D>
+struct StageLds {
+    static constexpr int E = D / 16, NS = (D + 31) / 32;
+    u32x4 k[4][NS][64];                       // 16 positions each
+    u32x4 v[E][2][64];                        // a column of each lane's, 32 positions each
+};
+
+template <bool BF, int D, int NR>
+__device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a, const AttnTask& t, StageLds<D> (&l)[2], Rows<BF, D, NR>& r) {
+    constexpr int E = D / 16, NS = (D + 31) / 32;
+    using T = Tile<BF, D>;
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row0 = w * NR * 16;             // the wave's rows of the block
+    // this wave's 16 positions of a stage
+    u32x4 pk[NS];
+    VRow<E> pv[4];
+    auto bring = [&](int p, int id) {
+        p += 16 * w;
+        const char* b = T::spot(c, c.k, c.kp, c.kh, c.ks, t.g, p, id);
+        const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            pk[s] = u32x4{0, 0, 0, 0};
+            if (D % 32 == 0 || gq < 2) pk[s] = *(const u32x4*)(b + 64 * s + lo);
+        }
+        b = T::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p, id);
+        const uint32_t vo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pv[i].load(b + i * (2 * c.vs), vo);
+    };
+    auto put = [&](int p, int id, StageLds<D>& s) {
+        p += 16 * w;
+        if (id < 0)                           // scores of a page outside the cache are NaN
+#pragma unroll
+            for (int k = 0; k < NS; ++k) pk[k] = u32x4{~0u, ~0u, ~0u, ~0u};
+        if (p + 16 > t.p1)                    // values that no row sees
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (p + 4 * gq + i >= t.p1) pv[i].zero();
+#pragma unroll
+        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = pk[k];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(pv[1].w[e / 2], pv[0].w[e / 2], sel),
+                                                          __builtin_amdgcn_perm(pv[3].w[e / 2], pv[2].w[e / 2], sel)};
+        }
+    };
+    int p = t.p0, id = T::look(c, t, p + 16 * w);
+    bring(p, id);
+    int nx = T::look(c, t, p + kStage + 16 * w);
+    u32x4 q[NR][NS];
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        const int i = row0 + rt * 16 + n, tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            q[rt][s] = u32x4{0, 0, 0, 0};
+            if (i < t.rows && 32 * s + 8 * gq < D) q[rt][s] = *(const u32x4*)(a.q + tok * a.qt + h * a.qh + 32 * s + 8 * gq);
+        }
+    }
+    r.start();
+    const bool idle = row0 >= t.rows;
+    const int lo = idle ? 0 : t.limit(row0, a.per), hi = idle ? 0 : t.limit(min(row0 + NR * 16, t.rows) - 1, a.per);
+    put(p, id, l[0]);
+    id = nx;
+    if (p + kStage < t.p1) bring(p + kStage, id);
+    nx = T::look(c, t, p + 2 * kStage + 16 * w);
+    __syncthreads();
+
+    f32x4 s[NR][2];
+    u32x4 wt[NR];
+    auto scores = [&](int h, const StageLds<D>& st) {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const u32x4 f = st.k[2 * h + b][k][lane];
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) s[rt][b] = mfma16<BF>(f, q[rt][k], s[rt][b]);
+            }
+    };
+    for (int turn = 0;; ++turn, p += kStage) {
+        const StageLds<D>& st = l[turn & 1];
+        if (p + kStage <= lo) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                scores(h, st);
+                float mx[NR];
+                bool any = false;
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) {
+                    mx[rt] = r.top(s[rt]);
+                    any |= r.high(rt, mx[rt], a);
+                }
+                if (__any(any))
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt) r.raise(rt, mx[rt], a);
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) wt[rt] = r.weights(rt, s[rt], a);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const u32x4 v = st.v[e][h][lane];
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
+                }
+            }
+        } else {
+            int lim[NR];
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) lim[rt] = row0 + rt * 16 + n < t.rows ? t.limit(row0 + rt * 16 + n, a.per) : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int ph = p + kATile * h;
+                if (ph >= hi) break;
+                scores(h, st);
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) {
+                    r.hide(lim[rt], ph, s[rt]);
+                    const float mx = r.top(s[rt]);
+                    if (__any(r.high(rt, mx, a))) r.raise(rt, mx, a);
+                    wt[rt] = r.weights(rt, s[rt], a);
+                }
+                bool f = true;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    u32x4 v = st.v[e][h][lane];
+                    if (lo != hi) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &f);
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
+                }
+                if (__any(!f)) r.add_odd(c, t, ph, lim);
+            }
+        }
+        if (p + kStage >= t.p1) break;
+        put(p + kStage, id, l[(turn + 1) & 1]);
+        id = nx;
+        if (p + 2 * kStage < t.p1) bring(p + 2 * kStage, id);
+        nx = T::look(c, t, p + 3 * kStage + 16 * w);
+        __syncthreads();
+    }
+}
+
+template <int D, int NR>
+struct MeetLds {
+    float o[4][16][D + 4];
+    float ml[4][NR * 16][2];
+};
+
+// the four waves' results of a workgroup's task, summed and stored
+template <bool BF, int D, int NR>
+__device__ __forceinline__ void meet(const AttnArgs& a, const AttnTask& t, Rows<BF, D, NR>& r, MeetLds<D, NR>& l) {
+    constexpr int E = D / 16;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, n = lane & 15, gq = lane >> 4;
+    r.finish();
+    __syncthreads();                          // an earlier task's LDS is read out
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt)
+        if (gq == 0) l.ml[w][rt * 16 + n][0] = r.ref[rt], l.ml[w][rt * 16 + n][1] = r.sum[rt];
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        if (rt * 16 >= t.rows) break;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, l.ml[i][rt * 16 + n][0]);
+        const float f = __builtin_amdgcn_exp2f(r.ref[rt] - top);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) l.o[w][n][4 * E * gq + E * i + e] = r.o[rt][e][i] * f;
+        __syncthreads();
+        for (int i = tid; i < 16 * (D / 4); i += kAThreads) {
+            const int rr = i / (D / 4), d = i % (D / 4) * 4, row = rt * 16 + rr;
+            if (row >= t.rows) continue;
+            f32x4 v = *(const f32x4*)&l.o[0][rr][d];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) v += *(const f32x4*)&l.o[k][rr][d];
+            const size_t slot = part_slot(a, t, row);
+            *(f32x4*)(a.part + slot * D + d) = v;
+            if (d == 0) {
+                float tp = -INFINITY, sm = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    sm += l.ml[k][row][1] * __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp);
+                a.ml[slot * 2] = tp;
+                a.ml[slot * 2 + 1] = sm;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The own positions' tasks, numbered sequence by sequence: (chunk, row block,
+// key/value head).  How many there are only the device knows; whoever asks for
+// rising numbers walks the sequences once.
+struct OwnTasks {
     int base = 0;                             // sequences [base, base + 64) are in the lanes; those before hold `done` tasks
     int64_t done = 0;
-    for (int64_t task = blockIdx.x - a.ptasks;; task += gridDim.x - a.ptasks) {
+
+    __device__ bool find(const PagedCache& c, const PagedBatch& b, const AttnArgs& a, int64_t task, int RT, AttnTask& t) {
+        const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
+        const int lane = threadIdx.x & 63;
         int len = 0, start = 0, n = 0, end = 0, blocks = 0, chunks = 0;
         int64_t upto = 0;
         int hit = -1;
@@ -410,19 +638,19 @@ __global__ void __launch_bounds__(kAThreads, NR > 2 ? 1 : 2) k_paged_attn(PagedC
             }
             done += __shfl(upto, 63);
         }
-        if (hit < 0) return;
+        if (hit < 0) return false;
         blocks = __shfl(blocks, hit);
         chunks = __shfl(chunks, hit);
         n = __shfl(n, hit), start = __shfl(start, hit), end = __shfl(end, hit), len = __shfl(len, hit);
         const int64_t all = (int64_t)blocks * chunks * c.G;
-        const int64_t rest = task - (done + __shfl(upto, hit) - all);
+        const unsigned rest = __builtin_amdgcn_readfirstlane((int)(task - (done + __shfl(upto, hit) - all)));
         const int seq = __builtin_amdgcn_readfirstlane(base + hit);
-        const int rest_b = (int)(rest / c.G);
-        AttnTask t;
+        blocks = __builtin_amdgcn_readfirstlane(blocks);
+        const unsigned rest_b = rest / c.G;
         t.table = b.table + seq * b.table_stride;
         t.width = b.width;
-        t.g = __builtin_amdgcn_readfirstlane((int)(rest % c.G));
-        const int rb = __builtin_amdgcn_readfirstlane(rest_b % blocks), ch = __builtin_amdgcn_readfirstlane(rest_b / blocks);
+        t.g = rest % c.G;
+        const int rb = rest_b % blocks, ch = rest_b / blocks;
         t.split = a.NP + ch;
         t.tok0 = __builtin_amdgcn_readfirstlane(start);
         t.r0 = rb * RT;
@@ -433,11 +661,76 @@ __global__ void __launch_bounds__(kAThreads, NR > 2 ? 1 : 2) k_paged_attn(PagedC
         t.causal = true;
         t.p0 = ch * a.ochunk;
         t.p1 = __builtin_amdgcn_readfirstlane(min(min(t.p0 + a.ochunk, len), t.lim0 + (t.r0 + t.rows - 1) / a.per));
-        if (t.p1 > t.p0) A::run(c, a, t, l);  // else no row of the block sees the chunk
+        return true;
+    }
+};
+
+// One launch.  Workgroups below ptasks take the prefix (key/value head, chunk,
+// row block): up to 32 rows with the four waves on different positions, or
+// (WIDE) up to 64 * NR rows with the four waves on different rows.  The others
+// walk the own positions' tasks: a wave each with 16 rows, or (WIDE_OWN) a
+// workgroup each like the prefix.
+template <bool BF, int D, int NR, bool WIDE, bool WIDE_OWN>
+__global__ void __launch_bounds__(kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
+k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
+    constexpr int ROWS = WIDE ? 64 * NR : 16 * NR;
+    union Lds {
+        StageLds<(WIDE ? D : 16)> st[2];
+        MeetLds<(WIDE ? 16 : D), (WIDE ? 1 : NR)> m;
+    };
+    __shared__ Lds l;
+    const bool prefix = (int)blockIdx.x < a.ptasks;
+    if (prefix || WIDE_OWN) {
+        OwnTasks own;
+        for (int64_t task = (int)blockIdx.x - a.ptasks;; task += gridDim.x - a.ptasks) {
+            AttnTask t;
+            if (prefix) {
+                // the row blocks of one chunk follow each other on one XCD (workgroups go round the 8 XCDs)
+                const int j = blockIdx.x / 8, pair = j / a.rb * 8 + blockIdx.x % 8, rb = j % a.rb;
+                if (pair >= c.G * a.NP) return;
+                t.table = b.prefix_table;
+                t.width = (b.prefix + c.unit * kPageUnit - 1) / (c.unit * kPageUnit);
+                t.g = pair % c.G;
+                t.split = pair / c.G;
+                t.p0 = t.split * a.pchunk;
+                t.p1 = min(t.p0 + a.pchunk, b.prefix);
+                t.tok0 = 0;
+                t.r0 = rb * a.rows;
+                t.rows = min(a.rows, b.T * a.per - t.r0);
+                t.lim0 = 0;
+                t.causal = false;
+            } else {
+                if (!own.find(c, b, a, task, ROWS, t)) return;
+                if (t.p1 <= t.p0) continue;   // no row of the block sees the chunk
+            }
+            Rows<BF, D, NR> r;
+            if constexpr (WIDE) {
+                __syncthreads();              // an earlier task's LDS is read out
+                walk_wide<BF, D, NR>(c, a, t, l.st, r);
+                r.store(a, t, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
+            } else {
+                walk<BF, D, NR>(c, a, t, t.p0 + kATile * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kAStep, r);
+                meet<BF, D, NR>(a, t, r, l.m);
+            }
+            if (prefix) return;
+        }
+    }
+    if constexpr (!WIDE_OWN) {
+        OwnTasks own;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        for (int64_t task = ((int)blockIdx.x - a.ptasks) * 4 + w;; task += ((int)gridDim.x - a.ptasks) * 4) {
+            AttnTask t;
+            if (!own.find(c, b, a, task, 16, t)) return;
+            if (t.p1 <= t.p0) continue;
+            Rows<BF, D, 1> r;
+            walk<BF, D, 1>(c, a, t, t.p0, kATile, r);
+            r.store(a, t, 0);
+        }
     }
 }
 
-// One wave per row (token, head): its chunks joined in order.
+// One wave per row (token, head): its chunks joined, each group of lanes (four
+// columns a lane) taking every so manieth chunk in order.
 template <bool BF>
 __global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBatch b, AttnArgs a) {
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), D = c.D;
@@ -450,26 +743,48 @@ __global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBat
     const int own = (int)((min(see, cap) + a.ochunk - 1) / a.ochunk), S = a.NP + a.NO, n = a.NP + own;
     const float* ml = a.ml + (size_t)row * S * 2;
     const float* part = a.part + (size_t)row * S * D;
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 64) top = fmaxf(top, ml[2 * i]);
+    const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float top = kNone, sum = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = i0 + lane;
+        float2 v = {kNone, 0.f};
+        if (i < n) v = *(const float2*)(ml + 2 * i);
+        float tp = fmaxf(top, v.x);
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
-    float x0 = 0.f, x1 = 0.f, sum = 0.f;
-    const int d = lane * 2;
-    for (int i = 0; i < n; ++i) {
-        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2 * i] - top);
-        sum = fmaf(ml[2 * i + 1], f, sum);
-        if (d < D) {
-            const float2 v = *(const float2*)(part + (size_t)i * D + d);
-            x0 = fmaf(v.x, f, x0);
-            x1 = fmaf(v.y, f, x1);
+        for (int o = 1; o < 64; o *= 2) tp = fmaxf(tp, __shfl_xor(tp, o));
+        const float old = __builtin_amdgcn_exp2f(top - tp), f = __builtin_amdgcn_exp2f(v.x - tp);
+        float s = v.y * f;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) s += __shfl_xor(s, o);
+        sum = fmaf(sum, old, s);
+        acc *= old;
+        top = tp;
+        const int m = min(64, n - i0);
+        for (int k0 = g; k0 - g < m; k0 += 4 * groups) {
+            f32x4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + j * groups;
+                x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (k < m && d < D) x[j] = *(const f32x4*)(part + (size_t)(i0 + k) * D + d);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float fk = __shfl(f, min(k0 + j * groups, 63));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[j][e], fk, acc[e]);
+            }
         }
     }
+    for (int o = gl; o < 64; o *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
     if (see > cap) sum = NAN;                                       // positions that the table does not hold
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    if (d < D) {
-        uint32_t* o = (uint32_t*)(a.out + t * a.ot + h * a.oh + d);
-        *o = pack2<BF>(x0 * inv, x1 * inv);
+    if (g == 0 && d < D) {
+        const u32x2 r = {pack2<BF>(acc[0] * inv, acc[1] * inv), pack2<BF>(acc[2] * inv, acc[3] * inv)};
+        *(u32x2*)(a.out + t * a.ot + h * a.oh + d) = r;
     }
     if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
 }
@@ -477,41 +792,51 @@ __global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBat
 namespace {
 
 struct AttnPlan {
-    int nr, rb, NP, pchunk, NO, ochunk, ptasks, otasks;
+    int nr;                                   // tiles of 16 rows a wave has
+    bool wide, wide_own;
+    int rb, rows, NP, pchunk, NO, ochunk, ptasks, otasks;
 };
 
 // Rows per block, chunks and workgroups from the sizes that the host knows.
 int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int per = H / c.G;
-    const int64_t rows = (int64_t)b.T * per;
+    const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > (1 << 30)) return LOOPSPEC_EINVAL;
-    const int64_t most = b.prefix > 0 ? rows : (rows + b.B - 1) / b.B;
-    pl->nr = most <= 16 ? 1 : most <= 32 ? 2 : 4;
-    const int RT = 16 * pl->nr, slots = pl->nr > 2 ? 256 : 512;
-    pl->rb = (int)((rows + RT - 1) / RT);
+    pl->wide_own = each > 32;
+    pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32);
+    if (pl->wide)
+        pl->nr = pl->wide_own || rows > 64 ? 2 : 1;
+    else
+        pl->nr = b.prefix > 0 && rows > 16 ? 2 : 1;
+    const int block = pl->nr * (pl->wide ? 64 : 16), slots = 512;
+    pl->rb = (int)((rows + block - 1) / block);
+    pl->rows = (int)((rows + pl->rb * 16 - 1) / (pl->rb * 16) * 16);
     // prefix: the number of chunks whose rounds of resident workgroups take the least time, a
-    // workgroup's start and end counted as one step
+    // workgroup's start and end counted as two steps
     pl->NP = pl->pchunk = 0;
     if (b.prefix > 0) {
         const int64_t steps = (b.prefix + kAStep - 1) / kAStep, heads = (int64_t)c.G * pl->rb;
         int64_t best = -1;
         for (int64_t np = 1; np <= std::min<int64_t>(steps, 128); ++np) {
             const int64_t len = (steps + np - 1) / np, n = (steps + len - 1) / len;
-            const int64_t cost = (heads * n + slots - 1) / slots * (len + 1);
+            const int64_t cost = (heads * n + slots - 1) / slots * (len + 2);
             if (best < 0 || cost < best) best = cost, pl->NP = (int)n, pl->pchunk = (int)(len * kAStep);
         }
     }
     const int64_t pairs = ((int64_t)c.G * pl->NP + 7) / 8 * 8;
     if (pairs * pl->rb > (1 << 30)) return LOOPSPEC_EINVAL;
     pl->ptasks = (int)(pairs * pl->rb);
-    // own positions: chunks that give about a thousand tasks when every table is full
-    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
-    int64_t chunk = (cap * b.B * c.G / 1024 + kAStep - 1) / kAStep * kAStep;
-    chunk = std::min<int64_t>(std::max<int64_t>(chunk, 2 * kAStep), 32 * kAStep);
+    // own positions: chunks that give a few thousand waves (or several hundred workgroups) work when every
+    // table is full, of at least 8 tiles a wave
+    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, want = pl->wide_own ? 1024 : 4096;
+    const int64_t unit = pl->wide_own ? 8 * kAStep : 8 * kATile;
+    int64_t chunk = (cap * b.B * c.G / want + unit - 1) / unit * unit;
+    chunk = std::min<int64_t>(std::max<int64_t>(chunk, unit), 4096);
     pl->ochunk = (int)chunk;
     pl->NO = (int)((cap + chunk - 1) / chunk);
+    const int RT = pl->wide_own ? block : 16;
     const int64_t own = ((rows + RT - 1) / RT + b.B) * pl->NO * c.G;
-    pl->otasks = (int)std::min<int64_t>(own, slots);
+    pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + 3) / 4, slots);
     return LOOPSPEC_OK;
 }
 
@@ -520,21 +845,19 @@ uint64_t attn_bytes(const PagedCache& c, const PagedBatch& b, int H, const AttnP
 }
 
 template <bool BF, int D>
-const void* attn_kernel(int nr) {
-    switch (nr) {
-        case 1: return (const void*)k_paged_attn<BF, D, 1>;
-        case 2: return (const void*)k_paged_attn<BF, D, 2>;
-        default: return (const void*)k_paged_attn<BF, D, 4>;
-    }
+const void* attn_kernel(const AttnPlan& p) {
+    if (p.wide_own) return (const void*)k_paged_attn<BF, D, 2, true, true>;
+    if (!p.wide) return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, false, false> : (const void*)k_paged_attn<BF, D, 2, false, false>;
+    return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, true, false> : (const void*)k_paged_attn<BF, D, 2, true, false>;
 }
 template <bool BF>
-const void* attn_kernel(int D, int nr) {
+const void* attn_kernel(int D, const AttnPlan& p) {
     switch (D) {
-        case 16: return attn_kernel<BF, 16>(nr);
-        case 32: return attn_kernel<BF, 32>(nr);
-        case 64: return attn_kernel<BF, 64>(nr);
-        case 96: return attn_kernel<BF, 96>(nr);
-        default: return attn_kernel<BF, 128>(nr);
+        case 16: return attn_kernel<BF, 16>(p);
+        case 32: return attn_kernel<BF, 32>(p);
+        case 64: return attn_kernel<BF, 64>(p);
+        case 96: return attn_kernel<BF, 96>(p);
+        default: return attn_kernel<BF, 128>(p);
     }
 }
 
@@ -585,13 +908,13 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     AttnArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
-               args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (pl.NP + pl.NO) * c.D, cs,
-               args->n_heads, args->n_heads / c.G, pl.NP, pl.pchunk, pl.NO, pl.ochunk, pl.rb, pl.ptasks};
+               args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (pl.NP + pl.NO) * c.D, cs, 1.0f / cs,
+               args->n_heads, args->n_heads / c.G, pl.NP, pl.pchunk, pl.NO, pl.ochunk, pl.rb, pl.rows, pl.ptasks};
     hipStream_t st = (hipStream_t)stream;
     void* kargs[] = {&c, &b, &a};
     const bool bf = cache->dtype == LOOPSPEC_BF16;
     if (pl.ptasks + pl.otasks > 0) {
-        const void* f = bf ? attn_kernel<true>(c.D, pl.nr) : attn_kernel<false>(c.D, pl.nr);
+        const void* f = bf ? attn_kernel<true>(c.D, pl) : attn_kernel<false>(c.D, pl);
         if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
     }
     const void* j = bf ? (const void*)k_paged_join<true> : (const void*)k_paged_join<false>;
