@@ -27,6 +27,7 @@
 // vanish.  Sums are fp32; weights are rounded to the cache's type for the
 // second product.
 #include <algorithm>
+#include <type_traits>
 
 #include "ls_paged.h"
 
@@ -307,15 +308,16 @@ struct Rows {
     }
 };
 
-// Few rows (16 or 32): Q in registers, the next tile's loads in flight under
-// the current one's products.  The wave takes the tiles p, p + step, ...
+// Few rows (16 or 32): Q in registers; the next tile's keys and values come
+// into the registers of this one's as soon as a product has read them.  The
+// wave takes the tiles p, p + step, ...
 template <bool BF, int D, int NR>
 __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, const AttnTask& t, int p, int step, Rows<BF, D, NR>& r) {
     constexpr int NS = (D + 31) / 32;
     using T = Tile<BF, D>;
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-    T x, y;
-    int id[2] = {T::look(c, t, p), T::look(c, t, p + 16)}, nx[2] = {0, 0};
+    T x;
+    int id[2] = {T::look(c, t, p), T::look(c, t, p + 16)}, nx[2];
     r.start();
     if (p >= t.p1) return;
     x.load_k(c, t, p, id);
@@ -354,17 +356,15 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
         }
     };
     int bad = 0;
-    for (; p + kATile <= lo; p += step) {
+    // a tile that all rows see, with another one behind it
+    for (; p + kATile <= lo && p + step < t.p1; p += step) {
         const int nn[2] = {T::look(c, t, p + 2 * step), T::look(c, t, p + 2 * step + 16)};
-        if (p + step < t.p1) {
-            y.load_k(c, t, p + step, nx);
-            y.load_v(c, t, p + step, nx);
-        }
         bad |= id[0] | id[1];
         scores();
+        x.load_k(c, t, p + step, nx);
         soften();
         r.add(x, w);
-        x = y;
+        x.load_v(c, t, p + step, nx);
         id[0] = nx[0], id[1] = nx[1], nx[0] = nn[0], nx[1] = nn[1];
     }
     if (bad < 0)
@@ -395,10 +395,11 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
     }
 }
 
-// Many rows: the four waves share the positions and each has its own 16 * NR
-// rows, Q in registers.  A stage of 64 positions comes to LDS in operand order
-// (a wave brings 16 positions, in registers while the stage before is worked
-// on) and every wave reads all of it.
+// Many rows: a workgroup's NW waves share the positions and each has its own
+// 16 * NR rows, Q in registers.  A stage of 64 positions comes to LDS in operand
+// order and every wave reads all of it.  Two waves (NW = 8) or one (NW = 4) bring
+// 16 positions each, in registers while the one or two stages before are worked
+// on.
 constexpr int kStage = 64;
 
 template <int D>
@@ -408,50 +409,71 @@ struct StageLds {
     u32x4 v[E][2][64];                        // a column of each lane's, 32 positions each
 };
 
-template <bool BF, int D, int NR>
+template <bool BF, int D, int NR, int NW>
 __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a, const AttnTask& t, StageLds<D> (&l)[2], Rows<BF, D, NR>& r) {
-    constexpr int E = D / 16, NS = (D + 31) / 32;
+    constexpr int E = D / 16, NS = (D + 31) / 32, AHEAD = 1;
     using T = Tile<BF, D>;
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = w * NR * 16;             // the wave's rows of the block
-    // this wave's 16 positions of a stage
-    u32x4 pk[NS];
-    VRow<E> pv[4];
-    auto bring = [&](int p, int id) {
-        p += 16 * w;
-        const char* b = T::spot(c, c.k, c.kp, c.kh, c.ks, t.g, p, id);
-        const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
+    // this wave's 16 positions of a stage, and whether it brings their keys, their values or both
+    const int sub = NW == 8 ? w >> 1 : w;
+    const bool keys = NW == 4 || !(w & 1), vals = NW == 4 || (w & 1);
+    constexpr int KV = NW == 4 ? 2 : 1;       // register sets: keys, values
+    struct Part {
+        u32x4 b[KV][4];
+        int id;
+    } part[AHEAD];
+    auto bring = [&](int p, int id, Part& x) {
+        p += 16 * sub;
+        x.id = id;
+        if (keys) {
+            const char* b = T::spot(c, c.k, c.kp, c.kh, c.ks, t.g, p, id);
+            const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            pk[s] = u32x4{0, 0, 0, 0};
-            if (D % 32 == 0 || gq < 2) pk[s] = *(const u32x4*)(b + 64 * s + lo);
+            for (int s = 0; s < NS; ++s) {
+                x.b[0][s] = u32x4{0, 0, 0, 0};
+                if (D % 32 == 0 || gq < 2) x.b[0][s] = *(const u32x4*)(b + 64 * s + lo);
+            }
         }
-        b = T::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p, id);
-        const uint32_t vo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
+        if (vals) {
+            const char* b = T::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p, id);
+            const uint32_t lo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pv[i].load(b + i * (2 * c.vs), vo);
-    };
-    auto put = [&](int p, int id, StageLds<D>& s) {
-        p += 16 * w;
-        if (id < 0)                           // scores of a page outside the cache are NaN
+            for (int i = 0; i < 4; ++i) {
+                VRow<E> v;
+                v.load(b + i * (2 * c.vs), lo);
 #pragma unroll
-            for (int k = 0; k < NS; ++k) pk[k] = u32x4{~0u, ~0u, ~0u, ~0u};
-        if (p + 16 > t.p1)                    // values that no row sees
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (p + 4 * gq + i >= t.p1) pv[i].zero();
-#pragma unroll
-        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = pk[k];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
-            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(pv[1].w[e / 2], pv[0].w[e / 2], sel),
-                                                          __builtin_amdgcn_perm(pv[3].w[e / 2], pv[2].w[e / 2], sel)};
+                for (int j = 0; j < (E + 1) / 2; ++j) x.b[KV - 1][i][j] = v.w[j];
+            }
         }
     };
-    int p = t.p0, id = T::look(c, t, p + 16 * w);
-    bring(p, id);
-    int nx = T::look(c, t, p + kStage + 16 * w);
+    auto put = [&](int p, Part& x, StageLds<D>& s) {
+        p += 16 * sub;
+        if (keys) {
+            if (x.id < 0)                     // scores of a page outside the cache are NaN
+#pragma unroll
+                for (int k = 0; k < NS; ++k) x.b[0][k] = u32x4{~0u, ~0u, ~0u, ~0u};
+#pragma unroll
+            for (int k = 0; k < NS; ++k) s.k[sub][k][lane] = x.b[0][k];
+        }
+        if (vals) {
+            if (p + 16 > t.p1)                // values that no row sees
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (p + 4 * gq + i >= t.p1) x.b[KV - 1][i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+                const u32x4(&v)[4] = x.b[KV - 1];
+                ((u32x2*)&s.v[e][sub >> 1][lane])[sub & 1] = u32x2{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel),
+                                                                  __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel)};
+            }
+        }
+    };
+    int p = t.p0, id[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) id[i] = T::look(c, t, p + kStage * i + 16 * sub);
+    bring(p, id[0], part[0]);
     u32x4 q[NR][NS];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
@@ -465,10 +487,10 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
     r.start();
     const bool idle = row0 >= t.rows;
     const int lo = idle ? 0 : t.limit(row0, a.per), hi = idle ? 0 : t.limit(min(row0 + NR * 16, t.rows) - 1, a.per);
-    put(p, id, l[0]);
-    id = nx;
-    if (p + kStage < t.p1) bring(p + kStage, id);
-    nx = T::look(c, t, p + 2 * kStage + 16 * w);
+    if (AHEAD == 2 && p + kStage < t.p1) bring(p + kStage, id[1], part[AHEAD - 1]);
+    put(p, part[0], l[0]);
+    if (p + AHEAD * kStage < t.p1) bring(p + AHEAD * kStage, id[AHEAD], part[0]);
+    int nx = T::look(c, t, p + (AHEAD + 1) * kStage + 16 * sub);
     __syncthreads();
 
     f32x4 s[NR][2];
@@ -485,8 +507,9 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 for (int rt = 0; rt < NR; ++rt) s[rt][b] = mfma16<BF>(f, q[rt][k], s[rt][b]);
             }
     };
-    for (int turn = 0;; ++turn, p += kStage) {
-        const StageLds<D>& st = l[turn & 1];
+    // the stage at p, in buffer B; true when it is the last
+    auto work = [&](int B) -> bool {
+        const StageLds<D>& st = l[B];
         if (p + kStage <= lo) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -540,13 +563,16 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 if (__any(!f)) r.add_odd(c, t, ph, lim);
             }
         }
-        if (p + kStage >= t.p1) break;
-        put(p + kStage, id, l[(turn + 1) & 1]);
-        id = nx;
-        if (p + 2 * kStage < t.p1) bring(p + 2 * kStage, id);
-        nx = T::look(c, t, p + 3 * kStage + 16 * w);
+        if (p + kStage >= t.p1) return true;
+        Part& x = part[0];
+        put(p + kStage, x, l[B ^ 1]);
+        if (p + (AHEAD + 1) * kStage < t.p1) bring(p + (AHEAD + 1) * kStage, nx, x);
+        nx = T::look(c, t, p + (AHEAD + 2) * kStage + 16 * sub);
+        p += kStage;
         __syncthreads();
-    }
+        return false;
+    };
+    for (int turn = 0; !work(turn & 1); ++turn) {}
 }
 
 template <int D, int NR>
@@ -605,75 +631,88 @@ __device__ __forceinline__ void meet(const AttnArgs& a, const AttnTask& t, Rows<
 // key/value head).  How many there are only the device knows; whoever asks for
 // rising numbers walks the sequences once.
 struct OwnTasks {
-    int base = 0;                             // sequences [base, base + 64) are in the lanes; those before hold `done` tasks
+    int base = 0;                             // the sequences before it hold `done` tasks
     int64_t done = 0;
 
     __device__ bool find(const PagedCache& c, const PagedBatch& b, const AttnArgs& a, int64_t task, int RT, AttnTask& t) {
+        constexpr int PER = 4;                // sequences a lane takes at a time
         const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
         const int lane = threadIdx.x & 63;
-        int len = 0, start = 0, n = 0, end = 0, blocks = 0, chunks = 0;
-        int64_t upto = 0;
-        int hit = -1;
-        for (; base < b.B; base += 64) {
-            const int s = base + lane;
-            len = 0, start = 0, n = 0, end = 0;
-            if (s < b.B) {
-                len = (int)min((int64_t)max(b.seq_len[s], 0), cap);
-                end = b.q_start ? b.q_start[s + 1] : s + 1;
-                start = min(max(b.q_start ? b.q_start[s] : s, 0), b.T);
-                n = min(max(end, start), b.T) - start;
+        for (; base < b.B; base += 64 * PER) {
+            int len[PER], start[PER], n[PER], raw[PER], end[PER];
+            int64_t mine[PER], all = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int s = base + lane * PER + i;
+                raw[i] = -1, start[i] = 0, end[i] = 0;
+                if (s < b.B) {
+                    raw[i] = b.seq_len[s];
+                    end[i] = b.q_start ? b.q_start[s + 1] : s + 1;
+                    start[i] = b.q_start ? b.q_start[s] : s;
+                }
             }
-            blocks = (n * a.per + RT - 1) / RT;
-            chunks = (len + a.ochunk - 1) / a.ochunk;
-            upto = (int64_t)blocks * chunks * c.G;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                // a token sees its own position and those before it
+                const int64_t first = (int64_t)raw[i] - ((int64_t)end[i] - start[i]) + 1;
+                len[i] = (int)min((int64_t)max(raw[i], 0), cap);
+                raw[i] = (int)max(min(first, (int64_t)INT32_MAX / 2), (int64_t)-INT32_MAX / 2);
+                start[i] = min(max(start[i], 0), b.T);
+                n[i] = min(max(end[i], start[i]), b.T) - start[i];
+                mine[i] = (int64_t)((n[i] * a.per + RT - 1) / RT) * ((len[i] + a.ochunk - 1) / a.ochunk) * c.G;
+                all += mine[i];
+            }
+            int64_t upto = all;
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
                 const int64_t v = __shfl_up(upto, o);
                 if (lane >= o) upto += v;
             }
             const unsigned long long over = __ballot(done + upto > task);
-            if (over) {
-                hit = __ffsll(over) - 1;
-                break;
+            if (!over) {
+                done += (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32) |
+                                  (unsigned)__builtin_amdgcn_readlane((int)upto, 63));
+                continue;
             }
-            done += __shfl(upto, 63);
+            // the sequence among the lane's, then (wave-uniform from here, by readlane) the task among its own
+            int64_t at = done + upto - all;
+            int k = 0;
+#pragma unroll
+            for (int i = 0; i < PER - 1; ++i)
+                if (k == i && at + mine[i] <= task) {
+                    at += mine[i], k = i + 1;
+                    len[0] = len[i + 1], start[0] = start[i + 1], n[0] = n[i + 1], raw[0] = raw[i + 1];
+                }
+            const int hit = __ffsll(over) - 1, seq = base + hit * PER + __builtin_amdgcn_readlane(k, hit);
+            const unsigned rest = (unsigned)__builtin_amdgcn_readlane((int)(task - at), hit), rest_b = rest / c.G;
+            const int own_n = __builtin_amdgcn_readlane(n[0], hit), own_len = __builtin_amdgcn_readlane(len[0], hit);
+            const int blocks = (own_n * a.per + RT - 1) / RT, rb = rest_b % blocks, ch = rest_b / blocks;
+            t.table = b.table + seq * b.table_stride;
+            t.width = b.width;
+            t.g = rest % c.G;
+            t.split = a.NP + ch;
+            t.tok0 = __builtin_amdgcn_readlane(start[0], hit);
+            t.r0 = rb * RT;
+            t.rows = min(RT, own_n * a.per - t.r0);
+            t.lim0 = __builtin_amdgcn_readlane(raw[0], hit);
+            t.causal = true;
+            t.p0 = ch * a.ochunk;
+            t.p1 = min(min(t.p0 + a.ochunk, own_len), t.lim0 + (t.r0 + t.rows - 1) / a.per);
+            return true;
         }
-        if (hit < 0) return false;
-        blocks = __shfl(blocks, hit);
-        chunks = __shfl(chunks, hit);
-        n = __shfl(n, hit), start = __shfl(start, hit), end = __shfl(end, hit), len = __shfl(len, hit);
-        const int64_t all = (int64_t)blocks * chunks * c.G;
-        const unsigned rest = __builtin_amdgcn_readfirstlane((int)(task - (done + __shfl(upto, hit) - all)));
-        const int seq = __builtin_amdgcn_readfirstlane(base + hit);
-        blocks = __builtin_amdgcn_readfirstlane(blocks);
-        const unsigned rest_b = rest / c.G;
-        t.table = b.table + seq * b.table_stride;
-        t.width = b.width;
-        t.g = rest % c.G;
-        const int rb = rest_b % blocks, ch = rest_b / blocks;
-        t.split = a.NP + ch;
-        t.tok0 = __builtin_amdgcn_readfirstlane(start);
-        t.r0 = rb * RT;
-        t.rows = __builtin_amdgcn_readfirstlane(min(RT, n * a.per - t.r0));
-        // a token sees its own position and those before it
-        const int64_t first = (int64_t)b.seq_len[seq] - ((int64_t)end - start) + 1;
-        t.lim0 = __builtin_amdgcn_readfirstlane((int)max(min(first, (int64_t)INT32_MAX / 2), (int64_t)-INT32_MAX / 2));
-        t.causal = true;
-        t.p0 = ch * a.ochunk;
-        t.p1 = __builtin_amdgcn_readfirstlane(min(min(t.p0 + a.ochunk, len), t.lim0 + (t.r0 + t.rows - 1) / a.per));
-        return true;
+        return false;
     }
 };
 
 // One launch.  Workgroups below ptasks take the prefix (key/value head, chunk,
-// row block): up to 32 rows with the four waves on different positions, or
-// (WIDE) up to 64 * NR rows with the four waves on different rows.  The others
-// walk the own positions' tasks: a wave each with 16 rows, or (WIDE_OWN) a
-// workgroup each like the prefix.
-template <bool BF, int D, int NR, bool WIDE, bool WIDE_OWN>
-__global__ void __launch_bounds__(kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
+// row block): up to 32 rows with the four waves on different positions (WIDE =
+// 0), or up to 16 * NR * WIDE rows with the WIDE waves on different rows.  The
+// others walk the own positions' tasks: a wave each with 16 rows, or (WIDE_OWN)
+// a workgroup each like the prefix.
+template <bool BF, int D, int NR, int WIDE, bool WIDE_OWN>
+__global__ void __launch_bounds__(WIDE ? 64 * WIDE : kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
 k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
-    constexpr int ROWS = WIDE ? 64 * NR : 16 * NR;
+    constexpr int ROWS = 16 * NR * (WIDE ? WIDE : 1), NW = WIDE ? WIDE : 4;
     union Lds {
         StageLds<(WIDE ? D : 16)> st[2];
         MeetLds<(WIDE ? 16 : D), (WIDE ? 1 : NR)> m;
@@ -706,7 +745,7 @@ k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
             Rows<BF, D, NR> r;
             if constexpr (WIDE) {
                 __syncthreads();              // an earlier task's LDS is read out
-                walk_wide<BF, D, NR>(c, a, t, l.st, r);
+                walk_wide<BF, D, NR, WIDE>(c, a, t, l.st, r);
                 r.store(a, t, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
             } else {
                 walk<BF, D, NR>(c, a, t, t.p0 + kATile * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kAStep, r);
@@ -718,7 +757,7 @@ k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
     if constexpr (!WIDE_OWN) {
         OwnTasks own;
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        for (int64_t task = ((int)blockIdx.x - a.ptasks) * 4 + w;; task += ((int)gridDim.x - a.ptasks) * 4) {
+        for (int64_t task = ((int)blockIdx.x - a.ptasks) * NW + w;; task += ((int)gridDim.x - a.ptasks) * NW) {
             AttnTask t;
             if (!own.find(c, b, a, task, 16, t)) return;
             if (t.p1 <= t.p0) continue;
@@ -729,27 +768,30 @@ k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
     }
 }
 
-// One wave per row (token, head): its chunks joined, each group of lanes (four
-// columns a lane) taking every so manieth chunk in order.
-template <bool BF>
-__global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBatch b, AttnArgs a) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), D = c.D;
-    if (row >= b.T * a.H) return;
-    const int t = row / a.H, h = row % a.H;
+// WPR waves per row (token, head) join its chunks: 256 at a time are in the
+// lanes of every wave by their references and sums, a wave takes every WPR-th
+// group of chunks, a group of lanes (four columns a lane) one chunk each.
+template <bool BF, int WPR>
+__global__ void __launch_bounds__(WPR > 4 ? 64 * WPR : kAThreads) k_paged_join(PagedCache c, PagedBatch b, AttnArgs a) {
+    constexpr int ROWS = WPR > 4 ? 1 : 4 / WPR;
+    __shared__ float l[WPR > 1 ? WPR : 1][ROWS][128];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, sub = wv % WPR, rl = wv / WPR, D = c.D;
+    const int row = blockIdx.x * ROWS + rl;
+    const bool in = row < b.T * a.H;
+    const int t = in ? row / a.H : 0, h = row % a.H;
     int64_t place = -1;
-    const int seq = paged_place(b, t, &place);
-    if (seq < 0 || b.seq_len[seq] < 0) return;                      // padding: its output stays as it is
+    const int seq = in ? paged_place(b, t, &place) : -1;
+    const bool live = seq >= 0 && b.seq_len[seq] >= 0;              // padding: its output stays as it is
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, see = max(place + 1, (int64_t)0);
-    const int own = (int)((min(see, cap) + a.ochunk - 1) / a.ochunk), S = a.NP + a.NO, n = a.NP + own;
+    const int own = (int)((min(see, cap) + a.ochunk - 1) / a.ochunk), S = a.NP + a.NO, n = live ? a.NP + own : 0;
     const float* ml = a.ml + (size_t)row * S * 2;
     const float* part = a.part + (size_t)row * S * D;
     const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float top = kNone, sum = 0.f;
     for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = i0 + lane;
         float2 v = {kNone, 0.f};
-        if (i < n) v = *(const float2*)(ml + 2 * i);
+        if (i0 + lane < n) v = *(const float2*)(ml + 2 * (i0 + lane));
         float tp = fmaxf(top, v.x);
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) tp = fmaxf(tp, __shfl_xor(tp, o));
@@ -761,17 +803,17 @@ __global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBat
         acc *= old;
         top = tp;
         const int m = min(64, n - i0);
-        for (int k0 = g; k0 - g < m; k0 += 4 * groups) {
+        for (int k0 = sub * groups; k0 < m; k0 += 4 * WPR * groups) {
             f32x4 x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int k = k0 + j * groups;
+                const int k = k0 + j * WPR * groups + g;
                 x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (k < m && d < D) x[j] = *(const f32x4*)(part + (size_t)(i0 + k) * D + d);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float fk = __shfl(f, min(k0 + j * groups, 63));
+                const float fk = __shfl(f, min(k0 + j * WPR * groups + g, 63));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[j][e], fk, acc[e]);
             }
@@ -780,6 +822,15 @@ __global__ void __launch_bounds__(kAThreads) k_paged_join(PagedCache c, PagedBat
     for (int o = gl; o < 64; o *= 2)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
+    if (WPR > 1) {
+        if (g == 0 && d < D) *(f32x4*)&l[sub][rl][d] = acc;
+        __syncthreads();
+        if (sub == 0 && g == 0 && d < D) {
+#pragma unroll
+            for (int i = 1; i < WPR; ++i) acc += *(const f32x4*)&l[i][rl][d];
+        }
+    }
+    if (!live || sub) return;
     if (see > cap) sum = NAN;                                       // positions that the table does not hold
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
     if (g == 0 && d < D) {
@@ -793,7 +844,8 @@ namespace {
 
 struct AttnPlan {
     int nr;                                   // tiles of 16 rows a wave has
-    bool wide, wide_own;
+    int wide;                                 // 0, or the waves that share positions
+    bool wide_own;
     int rb, rows, NP, pchunk, NO, ochunk, ptasks, otasks;
 };
 
@@ -803,12 +855,9 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > (1 << 30)) return LOOPSPEC_EINVAL;
     pl->wide_own = each > 32;
-    pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32);
-    if (pl->wide)
-        pl->nr = pl->wide_own || rows > 64 ? 2 : 1;
-    else
-        pl->nr = b.prefix > 0 && rows > 16 ? 2 : 1;
-    const int block = pl->nr * (pl->wide ? 64 : 16), slots = 512;
+    pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32) ? 4 : 0;
+    pl->nr = pl->wide ? (pl->wide_own || rows > 64 ? 2 : 1) : b.prefix > 0 && rows > 16 ? 2 : 1;
+    const int nw = pl->wide ? pl->wide : 4, block = 16 * pl->nr * (pl->wide ? pl->wide : 1), slots = 512;
     pl->rb = (int)((rows + block - 1) / block);
     pl->rows = (int)((rows + pl->rb * 16 - 1) / (pl->rb * 16) * 16);
     // prefix: the number of chunks whose rounds of resident workgroups take the least time, a
@@ -829,14 +878,14 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     // own positions: chunks that give a few thousand waves (or several hundred workgroups) work when every
     // table is full, of at least 8 tiles a wave
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, want = pl->wide_own ? 1024 : 4096;
-    const int64_t unit = pl->wide_own ? 8 * kAStep : 8 * kATile;
+    const int64_t unit = pl->wide_own ? 8 * kAStep : 4 * kATile;
     int64_t chunk = (cap * b.B * c.G / want + unit - 1) / unit * unit;
     chunk = std::min<int64_t>(std::max<int64_t>(chunk, unit), 4096);
     pl->ochunk = (int)chunk;
     pl->NO = (int)((cap + chunk - 1) / chunk);
     const int RT = pl->wide_own ? block : 16;
     const int64_t own = ((rows + RT - 1) / RT + b.B) * pl->NO * c.G;
-    pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + 3) / 4, slots);
+    pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + nw - 1) / nw, slots);
     return LOOPSPEC_OK;
 }
 
@@ -846,9 +895,9 @@ uint64_t attn_bytes(const PagedCache& c, const PagedBatch& b, int H, const AttnP
 
 template <bool BF, int D>
 const void* attn_kernel(const AttnPlan& p) {
-    if (p.wide_own) return (const void*)k_paged_attn<BF, D, 2, true, true>;
-    if (!p.wide) return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, false, false> : (const void*)k_paged_attn<BF, D, 2, false, false>;
-    return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, true, false> : (const void*)k_paged_attn<BF, D, 2, true, false>;
+    if (p.wide_own) return (const void*)k_paged_attn<BF, D, 2, 4, true>;
+    if (p.wide == 4) return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, 4, false> : (const void*)k_paged_attn<BF, D, 2, 4, false>;
+    return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, 0, false> : (const void*)k_paged_attn<BF, D, 2, 0, false>;
 }
 template <bool BF>
 const void* attn_kernel(int D, const AttnPlan& p) {
@@ -859,6 +908,11 @@ const void* attn_kernel(int D, const AttnPlan& p) {
         case 96: return attn_kernel<BF, 96>(p);
         default: return attn_kernel<BF, 128>(p);
     }
+}
+
+template <bool BF>
+const void* join_kernel(int wpr) {
+    return wpr == 1 ? (const void*)k_paged_join<BF, 1> : wpr == 4 ? (const void*)k_paged_join<BF, 4> : (const void*)k_paged_join<BF, 16>;
 }
 
 int attn_check(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch, int n_heads, PagedCache* c,
@@ -915,10 +969,14 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     const bool bf = cache->dtype == LOOPSPEC_BF16;
     if (pl.ptasks + pl.otasks > 0) {
         const void* f = bf ? attn_kernel<true>(c.D, pl) : attn_kernel<false>(c.D, pl);
-        if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+        if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(pl.wide ? 64 * pl.wide : kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
     }
-    const void* j = bf ? (const void*)k_paged_join<true> : (const void*)k_paged_join<false>;
-    if (hipLaunchKernel(j, dim3((unsigned)((rows + 3) / 4)), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    // a wave per row has 4 (D = 128) to 64 chunks in flight at once
+    const int S = pl.NP + pl.NO, wpr = S <= 8 || rows > 2048 ? 1 : S <= 64 || rows > 256 ? 4 : 16;
+    const void* j = bf ? join_kernel<true>(wpr) : join_kernel<false>(wpr);
+    const unsigned per_wg = wpr > 4 ? 1 : 4 / wpr;
+    if (hipLaunchKernel(j, dim3((unsigned)((rows + per_wg - 1) / per_wg)), dim3(wpr > 4 ? 64 * wpr : kAThreads), kargs, 0, st) != hipSuccess)
+        return LOOPSPEC_EHIP;
     return LOOPSPEC_OK;
 }
 
