@@ -20,14 +20,12 @@
 // word).  Neither K nor V passes through LDS, and no wave waits for another
 // inside a chunk.
 //
-// Softmax: the reference m is raised only when some score of the tile exceeds
-// it by 8 (in the base-2 exponent), which after the first tiles is rare.
-// Weights are 2^(s - m + 7), so the largest lies in [2^7, 2^15]: inside fp16's
-// range, and the small ones of a long prefix stay 2^31 below it before they
-// vanish.  Sums are fp32; weights are rounded to the cache's type for the
-// second product.
+// Softmax: a weight is 2^(c s - m) with a reference m that gives the largest
+// score of its time 2^7 and is raised only when a weight could reach 2^15,
+// which after the first tiles is rare.  So the largest weight stays inside fp16's
+// range and the small ones of a long prefix keep 2^31 of room below it.  Sums
+// are fp32; weights are rounded to the cache's type for the second product.
 #include <algorithm>
-#include <type_traits>
 
 #include "ls_paged.h"
 
@@ -42,7 +40,8 @@ constexpr int kAThreads = 256;
 constexpr int kATile = 32;                    // positions per wave and step
 constexpr int kAStep = 4 * kATile;            // positions per workgroup and step
 constexpr float kNone = -3e38f;               // the reference before the first score
-constexpr float kRaise = 8.0f, kLift = 7.0f;  // log2 of what a weight may exceed the reference's by; of the reference's weight
+constexpr float kLift = 7.0f;                 // log2 of the weight of the score that set the reference
+constexpr float kHigh = 32768.0f;             // a lane's sum of 8 weights up to which none leaves fp16
 
 struct AttnArgs {
     const uint16_t* q;
@@ -52,13 +51,19 @@ struct AttnArgs {
     float* lse;
     float* part;                              // [rows][splits][D], rows = tokens x heads
     float* ml;                                // [rows][splits][2]: reference (base 2), sum
-    float c, rc;                              // scale * log2(e), and its reciprocal
+    float c;                                  // scale * log2(e)
     int H, per;                               // query heads; per key/value head
     int NP, pchunk;                           // prefix: chunks, positions per chunk
     int NO, ochunk;                           // own positions: chunks at most, positions per chunk
     int rb, rows;                             // prefix: row blocks, rows of a block
     int ptasks;                               // workgroups of the prefix
 };
+
+// Chunks of a sequence's own positions: the last one takes up to half a chunk
+// more rather than leave a short one.
+__host__ __device__ __forceinline__ int64_t own_chunks(int64_t len, int chunk) {
+    return len <= 0 ? 0 : len <= chunk ? 1 : (len + chunk / 2 - 1) / chunk;
+}
 
 template <bool BF>
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -229,12 +234,9 @@ struct Rows {
             if (p + 16 + 4 * gq + i >= lim) s[1][i] = -INFINITY;
         }
     }
-    static __device__ __forceinline__ float top(const f32x4 (&s)[2]) {
-        return fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    }
-    __device__ __forceinline__ bool high(int rt, float mx, const AttnArgs& a) const { return fmaf(mx, a.c, -ref[rt]) > kLift + kRaise; }
     // a new reference: the largest score so far gets the weight 2^kLift
-    __device__ __forceinline__ void raise(int rt, float mx, const AttnArgs& a) {
+    __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         const float now = fmaxf(ref[rt], fmaf(mx, a.c, -kLift)), al = __builtin_amdgcn_exp2f(ref[rt] - now);
@@ -243,13 +245,24 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < E; ++e) o[rt][e] *= al;
     }
+    // The weights of 32 positions as an operand, and their sum.  No maximum is taken: a lane's sum of 8
+    // tells when some weight may leave fp16's range, and then, which is rare after the first tiles, the
+    // reference is raised and the weights are taken again.
     __device__ __forceinline__ u32x4 weights(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
-        float x[2][4];
+        float x[2][4], part;
+        auto take = [&]() {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.c, -ref[rt]));
-        sum[rt] += ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
+                for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.c, -ref[rt]));
+            part = ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
+        };
+        take();
+        if (__any(part > kHigh)) {
+            raise(rt, s, a);
+            take();
+        }
+        sum[rt] += part;
         return u32x4{pack2<BF>(x[0][0], x[0][1]), pack2<BF>(x[0][2], x[0][3]), pack2<BF>(x[1][0], x[1][1]), pack2<BF>(x[1][2], x[1][3])};
     }
     // O += V^T P
@@ -347,14 +360,6 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
             }
         }
     };
-    auto soften = [&]() {
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            const float mx = r.top(s[rt]);
-            if (__any(r.high(rt, mx, a))) r.raise(rt, mx, a);
-            w[rt] = r.weights(rt, s[rt], a);
-        }
-    };
     int bad = 0;
     // a tile that all rows see, with another one behind it
     for (; p + kATile <= lo && p + step < t.p1; p += step) {
@@ -362,7 +367,8 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
         bad |= id[0] | id[1];
         scores();
         x.load_k(c, t, p + step, nx);
-        soften();
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) w[rt] = r.weights(rt, s[rt], a);
         r.add(x, w);
         x.load_v(c, t, p + step, nx);
         id[0] = nx[0], id[1] = nx[1], nx[0] = nn[0], nx[1] = nn[1];
@@ -377,7 +383,8 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
         scores();
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) r.hide(lim[rt], p, s[rt]);
-        soften();
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) w[rt] = r.weights(rt, s[rt], a);
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
@@ -395,11 +402,10 @@ __device__ __forceinline__ void walk(const PagedCache& c, const AttnArgs& a, con
     }
 }
 
-// Many rows: a workgroup's NW waves share the positions and each has its own
-// 16 * NR rows, Q in registers.  A stage of 64 positions comes to LDS in operand
-// order and every wave reads all of it.  Two waves (NW = 8) or one (NW = 4) bring
-// 16 positions each, in registers while the one or two stages before are worked
-// on.
+// Many rows: the four waves share the positions and each has its own 16 * NR
+// rows, Q in registers.  A stage of 64 positions comes to LDS in operand order
+// (a wave brings 16 of them, in registers while the stage before is worked on)
+// and every wave reads all of it.
 constexpr int kStage = 64;
 
 template <int D>
@@ -409,71 +415,50 @@ struct StageLds {
     u32x4 v[E][2][64];                        // a column of each lane's, 32 positions each
 };
 
-template <bool BF, int D, int NR, int NW>
+template <bool BF, int D, int NR>
 __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a, const AttnTask& t, StageLds<D> (&l)[2], Rows<BF, D, NR>& r) {
-    constexpr int E = D / 16, NS = (D + 31) / 32, AHEAD = 1;
+    constexpr int E = D / 16, NS = (D + 31) / 32;
     using T = Tile<BF, D>;
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = w * NR * 16;             // the wave's rows of the block
-    // this wave's 16 positions of a stage, and whether it brings their keys, their values or both
-    const int sub = NW == 8 ? w >> 1 : w;
-    const bool keys = NW == 4 || !(w & 1), vals = NW == 4 || (w & 1);
-    constexpr int KV = NW == 4 ? 2 : 1;       // register sets: keys, values
-    struct Part {
-        u32x4 b[KV][4];
-        int id;
-    } part[AHEAD];
-    auto bring = [&](int p, int id, Part& x) {
-        p += 16 * sub;
-        x.id = id;
-        if (keys) {
-            const char* b = T::spot(c, c.k, c.kp, c.kh, c.ks, t.g, p, id);
-            const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
+    // this wave's 16 positions of a stage
+    u32x4 pk[NS];
+    VRow<E> pv[4];
+    auto bring = [&](int p, int id) {
+        p += 16 * w;
+        const char* b = T::spot(c, c.k, c.kp, c.kh, c.ks, t.g, p, id);
+        const uint32_t lo = (n * (uint32_t)c.ks + 8 * gq) * 2;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                x.b[0][s] = u32x4{0, 0, 0, 0};
-                if (D % 32 == 0 || gq < 2) x.b[0][s] = *(const u32x4*)(b + 64 * s + lo);
-            }
+        for (int s = 0; s < NS; ++s) {
+            pk[s] = u32x4{0, 0, 0, 0};
+            if (D % 32 == 0 || gq < 2) pk[s] = *(const u32x4*)(b + 64 * s + lo);
         }
-        if (vals) {
-            const char* b = T::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p, id);
-            const uint32_t lo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
+        b = T::spot(c, c.v, c.vp, c.vh, c.vs, t.g, p, id);
+        const uint32_t vo = (4 * gq * (uint32_t)c.vs + E * n) * 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                VRow<E> v;
-                v.load(b + i * (2 * c.vs), lo);
+        for (int i = 0; i < 4; ++i) pv[i].load(b + i * (2 * c.vs), vo);
+    };
+    auto put = [&](int p, int id, StageLds<D>& s) {
+        p += 16 * w;
+        if (id < 0)                           // scores of a page outside the cache are NaN
 #pragma unroll
-                for (int j = 0; j < (E + 1) / 2; ++j) x.b[KV - 1][i][j] = v.w[j];
-            }
+            for (int k = 0; k < NS; ++k) pk[k] = u32x4{~0u, ~0u, ~0u, ~0u};
+        if (p + 16 > t.p1)                    // values that no row sees
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (p + 4 * gq + i >= t.p1) pv[i].zero();
+#pragma unroll
+        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = pk[k];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(pv[1].w[e / 2], pv[0].w[e / 2], sel),
+                                                          __builtin_amdgcn_perm(pv[3].w[e / 2], pv[2].w[e / 2], sel)};
         }
     };
-    auto put = [&](int p, Part& x, StageLds<D>& s) {
-        p += 16 * sub;
-        if (keys) {
-            if (x.id < 0)                     // scores of a page outside the cache are NaN
-#pragma unroll
-                for (int k = 0; k < NS; ++k) x.b[0][k] = u32x4{~0u, ~0u, ~0u, ~0u};
-#pragma unroll
-            for (int k = 0; k < NS; ++k) s.k[sub][k][lane] = x.b[0][k];
-        }
-        if (vals) {
-            if (p + 16 > t.p1)                // values that no row sees
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (p + 4 * gq + i >= t.p1) x.b[KV - 1][i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
-                const u32x4(&v)[4] = x.b[KV - 1];
-                ((u32x2*)&s.v[e][sub >> 1][lane])[sub & 1] = u32x2{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel),
-                                                                  __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel)};
-            }
-        }
-    };
-    int p = t.p0, id[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) id[i] = T::look(c, t, p + kStage * i + 16 * sub);
-    bring(p, id[0], part[0]);
+    int p = t.p0, id = T::look(c, t, p + 16 * w);
+    bring(p, id);
+    int nx = T::look(c, t, p + kStage + 16 * w);
     u32x4 q[NR][NS];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
@@ -487,10 +472,10 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
     r.start();
     const bool idle = row0 >= t.rows;
     const int lo = idle ? 0 : t.limit(row0, a.per), hi = idle ? 0 : t.limit(min(row0 + NR * 16, t.rows) - 1, a.per);
-    if (AHEAD == 2 && p + kStage < t.p1) bring(p + kStage, id[1], part[AHEAD - 1]);
-    put(p, part[0], l[0]);
-    if (p + AHEAD * kStage < t.p1) bring(p + AHEAD * kStage, id[AHEAD], part[0]);
-    int nx = T::look(c, t, p + (AHEAD + 1) * kStage + 16 * sub);
+    put(p, id, l[0]);
+    id = nx;
+    if (p + kStage < t.p1) bring(p + kStage, id);
+    nx = T::look(c, t, p + 2 * kStage + 16 * w);
     __syncthreads();
 
     f32x4 s[NR][2];
@@ -507,23 +492,12 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 for (int rt = 0; rt < NR; ++rt) s[rt][b] = mfma16<BF>(f, q[rt][k], s[rt][b]);
             }
     };
-    // the stage at p, in buffer B; true when it is the last
-    auto work = [&](int B) -> bool {
-        const StageLds<D>& st = l[B];
+    for (int turn = 0;; ++turn, p += kStage) {
+        const StageLds<D>& st = l[turn & 1];
         if (p + kStage <= lo) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 scores(h, st);
-                float mx[NR];
-                bool any = false;
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) {
-                    mx[rt] = r.top(s[rt]);
-                    any |= r.high(rt, mx[rt], a);
-                }
-                if (__any(any))
-#pragma unroll
-                    for (int rt = 0; rt < NR; ++rt) r.raise(rt, mx[rt], a);
 #pragma unroll
                 for (int rt = 0; rt < NR; ++rt) wt[rt] = r.weights(rt, s[rt], a);
 #pragma unroll
@@ -543,12 +517,9 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 if (ph >= hi) break;
                 scores(h, st);
 #pragma unroll
-                for (int rt = 0; rt < NR; ++rt) {
-                    r.hide(lim[rt], ph, s[rt]);
-                    const float mx = r.top(s[rt]);
-                    if (__any(r.high(rt, mx, a))) r.raise(rt, mx, a);
-                    wt[rt] = r.weights(rt, s[rt], a);
-                }
+                for (int rt = 0; rt < NR; ++rt) r.hide(lim[rt], ph, s[rt]);
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) wt[rt] = r.weights(rt, s[rt], a);
                 bool f = true;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -563,16 +534,13 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 if (__any(!f)) r.add_odd(c, t, ph, lim);
             }
         }
-        if (p + kStage >= t.p1) return true;
-        Part& x = part[0];
-        put(p + kStage, x, l[B ^ 1]);
-        if (p + (AHEAD + 1) * kStage < t.p1) bring(p + (AHEAD + 1) * kStage, nx, x);
-        nx = T::look(c, t, p + (AHEAD + 2) * kStage + 16 * sub);
-        p += kStage;
+        if (p + kStage >= t.p1) break;
+        put(p + kStage, id, l[(turn + 1) & 1]);
+        id = nx;
+        if (p + 2 * kStage < t.p1) bring(p + 2 * kStage, id);
+        nx = T::look(c, t, p + 3 * kStage + 16 * w);
         __syncthreads();
-        return false;
-    };
-    for (int turn = 0; !work(turn & 1); ++turn) {}
+    }
 }
 
 template <int D, int NR>
@@ -659,7 +627,7 @@ struct OwnTasks {
                 raw[i] = (int)max(min(first, (int64_t)INT32_MAX / 2), (int64_t)-INT32_MAX / 2);
                 start[i] = min(max(start[i], 0), b.T);
                 n[i] = min(max(end[i], start[i]), b.T) - start[i];
-                mine[i] = (int64_t)((n[i] * a.per + RT - 1) / RT) * ((len[i] + a.ochunk - 1) / a.ochunk) * c.G;
+                mine[i] = (int64_t)((n[i] * a.per + RT - 1) / RT) * own_chunks(len[i], a.ochunk) * c.G;
                 all += mine[i];
             }
             int64_t upto = all;
@@ -697,7 +665,8 @@ struct OwnTasks {
             t.lim0 = __builtin_amdgcn_readlane(raw[0], hit);
             t.causal = true;
             t.p0 = ch * a.ochunk;
-            t.p1 = min(min(t.p0 + a.ochunk, own_len), t.lim0 + (t.r0 + t.rows - 1) / a.per);
+            t.p1 = ch + 1 < (int)own_chunks(own_len, a.ochunk) ? t.p0 + a.ochunk : own_len;
+            t.p1 = min(t.p1, t.lim0 + (t.r0 + t.rows - 1) / a.per);
             return true;
         }
         return false;
@@ -706,13 +675,13 @@ struct OwnTasks {
 
 // One launch.  Workgroups below ptasks take the prefix (key/value head, chunk,
 // row block): up to 32 rows with the four waves on different positions (WIDE =
-// 0), or up to 16 * NR * WIDE rows with the WIDE waves on different rows.  The
+// false), or up to 64 * NR rows with the four waves on different rows.  The
 // others walk the own positions' tasks: a wave each with 16 rows, or (WIDE_OWN)
 // a workgroup each like the prefix.
-template <bool BF, int D, int NR, int WIDE, bool WIDE_OWN>
-__global__ void __launch_bounds__(WIDE ? 64 * WIDE : kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
+template <bool BF, int D, int NR, bool WIDE, bool WIDE_OWN>
+__global__ void __launch_bounds__(kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
 k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
-    constexpr int ROWS = 16 * NR * (WIDE ? WIDE : 1), NW = WIDE ? WIDE : 4;
+    constexpr int ROWS = WIDE ? 64 * NR : 16 * NR;
     union Lds {
         StageLds<(WIDE ? D : 16)> st[2];
         MeetLds<(WIDE ? 16 : D), (WIDE ? 1 : NR)> m;
@@ -745,7 +714,7 @@ k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
             Rows<BF, D, NR> r;
             if constexpr (WIDE) {
                 __syncthreads();              // an earlier task's LDS is read out
-                walk_wide<BF, D, NR, WIDE>(c, a, t, l.st, r);
+                walk_wide<BF, D, NR>(c, a, t, l.st, r);
                 r.store(a, t, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
             } else {
                 walk<BF, D, NR>(c, a, t, t.p0 + kATile * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kAStep, r);
@@ -757,7 +726,7 @@ k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
     if constexpr (!WIDE_OWN) {
         OwnTasks own;
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        for (int64_t task = ((int)blockIdx.x - a.ptasks) * NW + w;; task += ((int)gridDim.x - a.ptasks) * NW) {
+        for (int64_t task = ((int)blockIdx.x - a.ptasks) * 4 + w;; task += ((int)gridDim.x - a.ptasks) * 4) {
             AttnTask t;
             if (!own.find(c, b, a, task, 16, t)) return;
             if (t.p1 <= t.p0) continue;
@@ -783,7 +752,9 @@ __global__ void __launch_bounds__(WPR > 4 ? 64 * WPR : kAThreads) k_paged_join(P
     const int seq = in ? paged_place(b, t, &place) : -1;
     const bool live = seq >= 0 && b.seq_len[seq] >= 0;              // padding: its output stays as it is
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, see = max(place + 1, (int64_t)0);
-    const int own = (int)((min(see, cap) + a.ochunk - 1) / a.ochunk), S = a.NP + a.NO, n = live ? a.NP + own : 0;
+    // the sequence's chunks that begin before the row's limit
+    const int own = live ? (int)min(own_chunks(min((int64_t)b.seq_len[seq], cap), a.ochunk), (min(see, cap) + a.ochunk - 1) / a.ochunk) : 0;
+    const int S = a.NP + a.NO, n = live ? a.NP + own : 0;
     const float* ml = a.ml + (size_t)row * S * 2;
     const float* part = a.part + (size_t)row * S * D;
     const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
@@ -844,8 +815,7 @@ namespace {
 
 struct AttnPlan {
     int nr;                                   // tiles of 16 rows a wave has
-    int wide;                                 // 0, or the waves that share positions
-    bool wide_own;
+    bool wide, wide_own;
     int rb, rows, NP, pchunk, NO, ochunk, ptasks, otasks;
 };
 
@@ -855,9 +825,9 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > (1 << 30)) return LOOPSPEC_EINVAL;
     pl->wide_own = each > 32;
-    pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32) ? 4 : 0;
+    pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32);
     pl->nr = pl->wide ? (pl->wide_own || rows > 64 ? 2 : 1) : b.prefix > 0 && rows > 16 ? 2 : 1;
-    const int nw = pl->wide ? pl->wide : 4, block = 16 * pl->nr * (pl->wide ? pl->wide : 1), slots = 512;
+    const int block = pl->nr * (pl->wide ? 64 : 16), slots = 512;
     pl->rb = (int)((rows + block - 1) / block);
     pl->rows = (int)((rows + pl->rb * 16 - 1) / (pl->rb * 16) * 16);
     // prefix: the number of chunks whose rounds of resident workgroups take the least time, a
@@ -878,14 +848,14 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     // own positions: chunks that give a few thousand waves (or several hundred workgroups) work when every
     // table is full, of at least 8 tiles a wave
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, want = pl->wide_own ? 1024 : 4096;
-    const int64_t unit = pl->wide_own ? 8 * kAStep : 4 * kATile;
+    const int64_t unit = pl->wide_own ? 8 * kAStep : 2 * kATile;
     int64_t chunk = (cap * b.B * c.G / want + unit - 1) / unit * unit;
     chunk = std::min<int64_t>(std::max<int64_t>(chunk, unit), 4096);
     pl->ochunk = (int)chunk;
-    pl->NO = (int)((cap + chunk - 1) / chunk);
+    pl->NO = (int)own_chunks(cap, (int)chunk);
     const int RT = pl->wide_own ? block : 16;
     const int64_t own = ((rows + RT - 1) / RT + b.B) * pl->NO * c.G;
-    pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + nw - 1) / nw, slots);
+    pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + 3) / 4, slots);
     return LOOPSPEC_OK;
 }
 
@@ -895,9 +865,9 @@ uint64_t attn_bytes(const PagedCache& c, const PagedBatch& b, int H, const AttnP
 
 template <bool BF, int D>
 const void* attn_kernel(const AttnPlan& p) {
-    if (p.wide_own) return (const void*)k_paged_attn<BF, D, 2, 4, true>;
-    if (p.wide == 4) return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, 4, false> : (const void*)k_paged_attn<BF, D, 2, 4, false>;
-    return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, 0, false> : (const void*)k_paged_attn<BF, D, 2, 0, false>;
+    if (p.wide_own) return (const void*)k_paged_attn<BF, D, 2, true, true>;
+    if (p.wide) return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, true, false> : (const void*)k_paged_attn<BF, D, 2, true, false>;
+    return p.nr == 1 ? (const void*)k_paged_attn<BF, D, 1, false, false> : (const void*)k_paged_attn<BF, D, 2, false, false>;
 }
 template <bool BF>
 const void* attn_kernel(int D, const AttnPlan& p) {
@@ -951,7 +921,7 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     const int rc = attn_check(cache, batch, args->n_heads, &c, &b, &pl);
     if (rc) return rc;
     const float cs = args->scale * 1.44269504088896341f;
-    if (!(args->scale > 0.f) || !(cs < 3e38f) || !(kRaise / cs < 3e38f)) return LOOPSPEC_EINVAL;
+    if (!(args->scale > 0.f) || !(cs < 3e38f)) return LOOPSPEC_EINVAL;
     auto ok = [](const void* p, int64_t token, int64_t head) {
         return p && !((uintptr_t)p & 15) && token >= 0 && head >= 0 && token % 8 == 0 && head % 8 == 0;
     };
@@ -962,14 +932,14 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     AttnArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
-               args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (pl.NP + pl.NO) * c.D, cs, 1.0f / cs,
+               args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (pl.NP + pl.NO) * c.D, cs,
                args->n_heads, args->n_heads / c.G, pl.NP, pl.pchunk, pl.NO, pl.ochunk, pl.rb, pl.rows, pl.ptasks};
     hipStream_t st = (hipStream_t)stream;
     void* kargs[] = {&c, &b, &a};
     const bool bf = cache->dtype == LOOPSPEC_BF16;
     if (pl.ptasks + pl.otasks > 0) {
         const void* f = bf ? attn_kernel<true>(c.D, pl) : attn_kernel<false>(c.D, pl);
-        if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(pl.wide ? 64 * pl.wide : kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+        if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
     }
     // a wave per row has 4 (D = 128) to 64 chunks in flight at once
     const int S = pl.NP + pl.NO, wpr = S <= 8 || rows > 2048 ? 1 : S <= 64 || rows > 256 ? 4 : 16;
