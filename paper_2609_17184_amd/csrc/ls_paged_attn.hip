@@ -54,15 +54,16 @@ struct AttnArgs {
     float c;                                  // scale * log2(e)
     int H, per;                               // query heads; per key/value head
     int NP, pchunk;                           // prefix: chunks, positions per chunk
-    int NO, ochunk;                           // own positions: chunks at most, positions per chunk
+    int NO, oshift;                           // own positions: chunks at most, log2 of the positions per chunk
     int rb, rows;                             // prefix: row blocks, rows of a block
     int ptasks;                               // workgroups of the prefix
 };
 
 // Chunks of a sequence's own positions: the last one takes up to half a chunk
 // more rather than leave a short one.
-__host__ __device__ __forceinline__ int64_t own_chunks(int64_t len, int chunk) {
-    return len <= 0 ? 0 : len <= chunk ? 1 : (len + chunk / 2 - 1) / chunk;
+__host__ __device__ __forceinline__ int own_chunks(int len, int shift) {
+    const int c = (len + (1 << shift) / 2 - 1) >> shift;
+    return len <= 0 ? 0 : c > 1 ? c : 1;
 }
 
 template <bool BF>
@@ -627,7 +628,7 @@ struct OwnTasks {
                 raw[i] = (int)max(min(first, (int64_t)INT32_MAX / 2), (int64_t)-INT32_MAX / 2);
                 start[i] = min(max(start[i], 0), b.T);
                 n[i] = min(max(end[i], start[i]), b.T) - start[i];
-                mine[i] = (int64_t)((n[i] * a.per + RT - 1) / RT) * own_chunks(len[i], a.ochunk) * c.G;
+                mine[i] = (int64_t)((n[i] * a.per + RT - 1) / RT) * own_chunks(len[i], a.oshift) * c.G;
                 all += mine[i];
             }
             int64_t upto = all;
@@ -664,8 +665,8 @@ struct OwnTasks {
             t.rows = min(RT, own_n * a.per - t.r0);
             t.lim0 = __builtin_amdgcn_readlane(raw[0], hit);
             t.causal = true;
-            t.p0 = ch * a.ochunk;
-            t.p1 = ch + 1 < (int)own_chunks(own_len, a.ochunk) ? t.p0 + a.ochunk : own_len;
+            t.p0 = ch << a.oshift;
+            t.p1 = ch + 1 < own_chunks(own_len, a.oshift) ? t.p0 + (1 << a.oshift) : own_len;
             t.p1 = min(t.p1, t.lim0 + (t.r0 + t.rows - 1) / a.per);
             return true;
         }
@@ -753,7 +754,7 @@ __global__ void __launch_bounds__(WPR > 4 ? 64 * WPR : kAThreads) k_paged_join(P
     const bool live = seq >= 0 && b.seq_len[seq] >= 0;              // padding: its output stays as it is
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, see = max(place + 1, (int64_t)0);
     // the sequence's chunks that begin before the row's limit
-    const int own = live ? (int)min(own_chunks(min((int64_t)b.seq_len[seq], cap), a.ochunk), (min(see, cap) + a.ochunk - 1) / a.ochunk) : 0;
+    const int own = live ? min(own_chunks((int)min((int64_t)b.seq_len[seq], cap), a.oshift), ((int)min(see, cap) + (1 << a.oshift) - 1) >> a.oshift) : 0;
     const int S = a.NP + a.NO, n = live ? a.NP + own : 0;
     const float* ml = a.ml + (size_t)row * S * 2;
     const float* part = a.part + (size_t)row * S * D;
@@ -816,7 +817,7 @@ namespace {
 struct AttnPlan {
     int nr;                                   // tiles of 16 rows a wave has
     bool wide, wide_own;
-    int rb, rows, NP, pchunk, NO, ochunk, ptasks, otasks;
+    int rb, rows, NP, pchunk, NO, oshift, ptasks, otasks;
 };
 
 // Rows per block, chunks and workgroups from the sizes that the host knows.
@@ -845,14 +846,12 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int64_t pairs = ((int64_t)c.G * pl->NP + 7) / 8 * 8;
     if (pairs * pl->rb > (1 << 30)) return LOOPSPEC_EINVAL;
     pl->ptasks = (int)(pairs * pl->rb);
-    // own positions: chunks that give a few thousand waves (or several hundred workgroups) work when every
-    // table is full, of at least 8 tiles a wave
-    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, want = pl->wide_own ? 1024 : 4096;
-    const int64_t unit = pl->wide_own ? 8 * kAStep : 2 * kATile;
-    int64_t chunk = (cap * b.B * c.G / want + unit - 1) / unit * unit;
-    chunk = std::min<int64_t>(std::max<int64_t>(chunk, unit), 4096);
-    pl->ochunk = (int)chunk;
-    pl->NO = (int)own_chunks(cap, (int)chunk);
+    // own positions: about two chunks per resident wave (or workgroup) when every table is full, of at
+    // least four tiles a wave
+    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, all = cap * b.B * c.G;
+    pl->oshift = pl->wide_own ? 9 : 7;
+    while (pl->oshift < 12 && (all >> pl->oshift) > (pl->wide_own ? 2 * slots : 8 * slots)) ++pl->oshift;
+    pl->NO = own_chunks((int)cap, pl->oshift);
     const int RT = pl->wide_own ? block : 16;
     const int64_t own = ((rows + RT - 1) / RT + b.B) * pl->NO * c.G;
     pl->otasks = (int)std::min<int64_t>(pl->wide_own ? own : (own + 3) / 4, slots);
@@ -933,7 +932,7 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     AttnArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
                args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (pl.NP + pl.NO) * c.D, cs,
-               args->n_heads, args->n_heads / c.G, pl.NP, pl.pchunk, pl.NO, pl.ochunk, pl.rb, pl.rows, pl.ptasks};
+               args->n_heads, args->n_heads / c.G, pl.NP, pl.pchunk, pl.NO, pl.oshift, pl.rb, pl.rows, pl.ptasks};
     hipStream_t st = (hipStream_t)stream;
     void* kargs[] = {&c, &b, &a};
     const bool bf = cache->dtype == LOOPSPEC_BF16;
