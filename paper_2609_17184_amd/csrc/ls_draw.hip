@@ -14,12 +14,13 @@
 // alone; where the order of adding is not fixed (the histograms' atomics),
 // masses are integers in units of 2^-44 of the largest weight.
 //
-// What top-k and top-p keep is the ranks above a boundary.  A histogram over
-// 2048 bins of 1/32 octave of weight tells the bin that holds it (counts for
-// top-k; masses for top-p, of what top-k kept); the bin's members are listed in
-// LDS and searched the same way over ranges of the logits' order-preserving
-// integer keys until a bin is a single key, where ties are cut by id.  A bin
-// with too many members is searched in place.
+// What top-k and top-p keep is the ranks down to some last one.  A histogram
+// over 2048 bins of 1/32 octave of weight tells the bin that holds it (counts
+// for top-k; masses for top-p, of what top-k kept).  The bin's members, when
+// there are at most 1024, go to LDS and a thread each finds its member's rank
+// against all others; otherwise ranges of the logits' order-preserving integer
+// keys are searched the same way until a bin is a single key, and ties are
+// counted off by id.
 //
 // The token: the kept mass per wave tells the run of ids, then all threads take
 // that run in id order.  A row without filters and of more than 65536 ids is
@@ -38,7 +39,7 @@ typedef uint32_t u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
 
 constexpr int kDThreads = 1024, kDWaves = kDThreads / 64;
 constexpr int kDBins = 2048;                          // two per thread
-constexpr int kDList = 4096;
+constexpr int kDList = kDThreads;
 constexpr int kDHeld = 64;                            // logits a thread holds
 constexpr int kDMaxVocab = 1 << 18;
 
@@ -69,11 +70,14 @@ __device__ __forceinline__ uint32_t order_key(float z) {
     const uint32_t b = __float_as_uint(z + 0.0f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-// 2^(n + up) 2^f of y = n + f <= 0, from 2^-200 on: the polynomial interpolates
-// 2^f at the Chebyshev points of [-1/2, 1/2] and is 1 at 0
+// 2^(y + up), y <= 0 (2^(up - 200) below y = -200): y = n + f, the polynomial
+// interpolates 2^f at the Chebyshev points of [-1/2, 1/2] and is 1 at 0.  n comes
+// from adding 1.5 * 2^52, whose low word it then is, and goes to the exponent as
+// it is: conversions and ldexp take several times an addition's cycles.
 __device__ __forceinline__ double weight(double y, int up = 0) {
+    constexpr double M = 6755399441055744.0;
     y = fmax(y, -200.0);
-    const double n = rint(y), f = y - n;
+    const double t = y + M, f = y - (t - M);
     double p = 7.070977866508138e-09;
     p = fma(p, f, 1.0205905413765595e-07);
     p = fma(p, f, 1.3215451633221434e-06);
@@ -84,17 +88,34 @@ __device__ __forceinline__ double weight(double y, int up = 0) {
     p = fma(p, f, 0.05550410866465167);
     p = fma(p, f, 0.24022650695910075);
     p = fma(p, f, 0.6931471805599462);
-    return ldexp(fma(p, f, 1.0), (int)n + up);
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + ((__double2loint(t) + up) << 20), __double2loint(p));
 }
 // the weight in units of 2^-44, to nearest: adding 2^52 leaves it in the low bits
 __device__ __forceinline__ u64 mass44(double y) {
     return (u64)__double_as_longlong(weight(y, 44) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
+// the last kept rank: logits above f are kept, and those equal to it up to id
+struct Cut {
+    float f = -INFINITY;
+    int id = -1;
+    __device__ __forceinline__ bool keeps(float v, int i) const { return v > f || (v == f && i <= id); }
+};
+
+struct Member {
+    float v;
+    int id;
+    u64 mass;
+};
+
 struct DrawLds {
-    u64 mass[kDBins];
+    union {
+        u64 mass[kDBins];
+        float run[kDBins * 2];                        // the logits of the wave that holds the token
+    };
     unsigned count[kDBins];
-    uint2 list[kDList];                               // key, id
+    Member list[kDList];
     u64 wm[kDWaves];
     double wd[kDWaves];
     unsigned wc[kDWaves];
@@ -102,6 +123,8 @@ struct DrawLds {
     unsigned first, last, listed, lo, hi, cnt, above_cnt;
     u64 bin_mass, above_mass;
     int bad, token;
+    float cut_f;
+    int cut_id;
 };
 
 template <typename T>
@@ -114,7 +137,7 @@ __device__ __forceinline__ T wave_sum(T v) {
 // the row as its workgroup sees it
 template <int DT, bool HELD>
 struct DrawRow {
-    static constexpr int B = 16;                      // logits of a lane's batch: 4 of each of 4 neighbouring rows of 256 ids
+    static constexpr int B = 16;                      // logits of a lane's batch
     const void* z;
     int64_t base;
     int V, seg;                                       // wave w owns ids [w * seg, (w + 1) * seg)
@@ -125,28 +148,33 @@ struct DrawRow {
     float x[HELD ? kDHeld : 1];
 
     __device__ __forceinline__ float at(int id) const { return logit<DT>(z, base + id); }
-    // four logits from id, -infinity outside [., end)
-    __device__ __forceinline__ void load4(int id, int end, float* v) const {
-        if (id + 4 <= end && vec) {
-            if (DT == LOOPSPEC_F32) {
-                const u32x4_a4 u = *(const u32x4_a4*)((const float*)z + base + id);
+    // four logits from id, a load for 4-byte aligned rows
+    __device__ __forceinline__ void load4(int id, float* v) const {
+        if (DT == LOOPSPEC_F32) {
+            const u32x4_a4 u = *(const u32x4_a4*)((const float*)z + base + id);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(u[i]);
-            } else {
-                const u32x2_a4 u = *(const u32x2_a4*)((const uint16_t*)z + base + id);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = half_bits(DT, i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(u[i]);
         } else {
+            const u32x2_a4 u = *(const u32x2_a4*)((const uint16_t*)z + base + id);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = id + i < end ? at(id + i) : -INFINITY;
+            for (int i = 0; i < 4; ++i) v[i] = half_bits(DT, i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu);
         }
     }
-    __device__ __forceinline__ int first() const { return (threadIdx.x >> 6) * seg + (threadIdx.x & 63) * 4; }
+    __device__ __forceinline__ int first() const { return (int)(threadIdx.x >> 6) * seg + (int)(threadIdx.x & 63) * 4; }
     __device__ __forceinline__ int end() const { return min(((int)(threadIdx.x >> 6) + 1) * seg, V); }
+    // batch j: 4 logits in each of 4 consecutive blocks of 256 ids of the wave; -infinity where there is none
     __device__ __forceinline__ void load_batch(int j, float* v) const {
+        const int b = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * seg + j * (64 * B));
+        if (b + 64 * B <= __builtin_amdgcn_readfirstlane(end()) && vec) {
 #pragma unroll
-        for (int k = 0; k < B / 4; ++k) load4(first() + (j * (B / 4) + k) * 256, end(), v + 4 * k);
+            for (int k = 0; k < B / 4; ++k) load4(first() + j * (64 * B) + k * 256, v + 4 * k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int id = first() + j * (64 * B) + (k / 4) * 256 + k % 4;
+                v[k] = id < end() ? at(id) : -INFINITY;
+            }
+        }
     }
     __device__ __forceinline__ void hold() {
         if constexpr (HELD) {
@@ -180,42 +208,60 @@ struct DrawRow {
     }
 };
 
+template <bool MASS, bool COUNT>
 __device__ __forceinline__ void clear_bins(DrawLds& l) {
     __syncthreads();
-    for (int i = threadIdx.x; i < kDBins; i += kDThreads) l.mass[i] = 0, l.count[i] = 0;
-    if (threadIdx.x == 0) l.first = kDBins, l.last = 0;
+    for (int i = threadIdx.x; i < kDBins; i += kDThreads) {
+        if (MASS) l.mass[i] = 0;
+        if (COUNT) l.count[i] = 0;
+    }
+    if (threadIdx.x == 0) l.first = kDBins, l.last = 0, l.listed = 0;
     __syncthreads();
 }
 
-// The bin that holds the boundary: the first one through which the count
-// reaches `need` (by count) or the mass reaches `goal`, the last occupied one
-// when none does.  l.first is its number; l.cnt and l.bin_mass what it holds,
-// l.above_* what lies above it, above_m and above_c included.
-__device__ void pick_bin(DrawLds& l, bool by_count, unsigned need, double goal, u64 above_m, unsigned above_c) {
+// The bin that holds the last kept rank: the first one through which the count
+// reaches `need` (COUNT), or the mass reaches `goal`; the last occupied one when
+// none does.  share > 0: the goal is that share of the bins' whole mass.  What
+// the bin and (above_m and above_c included) all above it hold is left in l.
+template <bool MASS, bool COUNT>
+__device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* goal, u64 above_m, unsigned above_c) {
     __syncthreads();
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, b0 = 2 * tid;
-    const u64 m[2] = {l.mass[b0], l.mass[b0 + 1]};
-    const unsigned c[2] = {l.count[b0], l.count[b0 + 1]};
+    u64 m[2] = {0, 0};
+    unsigned c[2] = {0, 0};
+    if (MASS) m[0] = l.mass[b0], m[1] = l.mass[b0 + 1];
+    if (COUNT) c[0] = l.count[b0], c[1] = l.count[b0 + 1];
     u64 sm = m[0] + m[1];
     unsigned sc = c[0] + c[1];
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
-        const u64 v = __shfl_up(sm, o);
-        const unsigned k = __shfl_up(sc, o);
-        if (lane >= o) sm += v, sc += k;
+        if (MASS) {
+            const u64 v = __shfl_up(sm, o);
+            if (lane >= o) sm += v;
+        }
+        if (COUNT) {
+            const unsigned k = __shfl_up(sc, o);
+            if (lane >= o) sc += k;
+        }
     }
     if (lane == 63) l.wm[wv] = sm, l.wc[wv] = sc;
     __syncthreads();
     sm += above_m - m[0] - m[1];
     sc += above_c - c[0] - c[1];
-    for (int i = 0; i < wv; ++i) sm += l.wm[i], sc += l.wc[i];
-    u64 am[2] = {sm, sm + m[0]};                      // above each of the thread's bins
-    unsigned ac[2] = {sc, sc + c[0]};
+    u64 all = 0;
+    for (int i = 0; i < kDWaves; ++i) {
+        if (i < wv) sm += l.wm[i], sc += l.wc[i];
+        all += l.wm[i];
+    }
+    if (share > 0.0) *goal = share * (double)all;
+    const u64 am[2] = {sm, sm + m[0]};                // above each of the thread's bins
+    const unsigned ac[2] = {sc, sc + c[0]};
 #pragma unroll
     for (int i = 1; i >= 0; --i) {
-        if (!c[i]) continue;
+        if (COUNT ? !c[i] : !m[i]) continue;
+        const bool reach = goal ? (double)(am[i] + m[i]) >= *goal : ac[i] + c[i] >= need;
+        if (reach) atomicMin(&l.first, (unsigned)(b0 + i));
         atomicMax(&l.last, (unsigned)(b0 + i));
-        if (by_count ? ac[i] + c[i] >= need : (double)(am[i] + m[i]) >= goal) atomicMin(&l.first, (unsigned)(b0 + i));
     }
     __syncthreads();
     const unsigned at = l.first < (unsigned)kDBins ? l.first : l.last;
@@ -223,63 +269,94 @@ __device__ void pick_bin(DrawLds& l, bool by_count, unsigned need, double goal, 
     for (int i = 0; i < 2; ++i)
         if (at == (unsigned)(b0 + i)) l.cnt = c[i], l.bin_mass = m[i], l.above_mass = am[i], l.above_cnt = ac[i];
     __syncthreads();
-    if (tid == 0) l.first = at;
-    __syncthreads();
+    return at;
 }
 
-// Boundary of a filter: keys above `key` are kept, and of those equal to it
-// the first `ties` by id of `all`; `mass` is what is kept (by mass only).
-struct Bound {
-    uint32_t key;
-    unsigned ties, all;
-};
-
-// Finds it.  The first `need` ranks (by count), or the ranks whose preceding
-// mass is below `goal`, among the keys from `floor` on (top-k's boundary, which
-// takes `floor_ties` of the keys equal to it: they have ranks, but no effect
-// below, since top-p's boundary never lies behind top-k's).
+// Id of tie number `tie` (from 0, in id order) among the logits equal to f.
 template <int DT, bool HELD>
-__device__ Bound boundary(const DrawRow<DT, HELD>& r, bool by_count, unsigned need, double goal, uint32_t floor) {
+__device__ int tie_id(const DrawRow<DT, HELD>& r, float f, unsigned tie) {
+    DrawLds& l = r.l;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    unsigned n = 0;
+    r.each([&](int, float v) { n += v == f; });
+    n = wave_sum(n);
+    __syncthreads();
+    if (lane == 0) l.wc[wv] = n;
+    __syncthreads();
+    unsigned before = 0;
+    for (int i = 0; i < wv; ++i) before += l.wc[i];
+    if (before <= tie && tie < before + n) {
+        for (int i = wv * r.seg;; i += 64) {
+            const bool eq = i + lane < r.V && r.at(i + lane) == f;
+            const u64 m = __ballot(eq);
+            if (eq && before + __popcll(m & ((1ull << lane) - 1)) == tie) l.token = i + lane;
+            before += __popcll(m);
+            if (before > tie) break;
+        }
+    }
+    __syncthreads();
+    const int id = l.token;
+    __syncthreads();
+    return id;
+}
+
+// The last kept rank of what `from` keeps: the first `need` ranks (BY_COUNT), or
+// the ranks whose preceding mass is below `share` of all of it.
+template <bool BY_COUNT, int DT, bool HELD>
+__device__ Cut last_kept(const DrawRow<DT, HELD>& r, Cut from, unsigned need, double share) {
     DrawLds& l = r.l;
     const int tid = threadIdx.x;
-    clear_bins(l);
-    r.each([&](int, float v) {
-        if (v == -INFINITY || order_key(v) < floor) return;
-        const int b = r.bin(v);
-        atomicAdd(&l.count[b], 1u);
-        if (!by_count) atomicAdd(&l.mass[b], mass44(r.y(v)));
+    double goal = 0.0, *const goalp = BY_COUNT ? nullptr : &goal;
+    clear_bins<!BY_COUNT, BY_COUNT>(l);
+    r.each([&](int id, float v) {
+        if (!from.keeps(v, id)) return;
+        if (BY_COUNT)
+            atomicAdd(&l.count[r.bin(v)], 1u);
+        else
+            atomicAdd(&l.mass[r.bin(v)], mass44(r.y(v)));
     });
-    pick_bin(l, by_count, need, goal, 0, 0);
-    const int picked = (int)l.first;
+    const int picked = (int)pick_bin<!BY_COUNT, BY_COUNT>(l, need, share, goalp, 0, 0);
     u64 above_m = l.above_mass;
-    unsigned above_c = l.above_cnt, members = l.cnt;
-    const bool list = members <= (unsigned)kDList;
-    if (tid == 0) l.listed = 0;
+    unsigned above_c = l.above_cnt;
+    r.each([&](int id, float v) {
+        if (r.bin(v) != picked || !from.keeps(v, id)) return;
+        const unsigned at = atomicAdd(&l.listed, 1u);
+        if (at < (unsigned)kDList) l.list[at] = Member{v, id, BY_COUNT ? 0 : mass44(r.y(v))};
+    });
+    if (tid == 0) l.cnt = 0;
     __syncthreads();
-    if (list)
-        r.each([&](int id, float v) {
-            if (v == -INFINITY || r.bin(v) != picked || order_key(v) < floor) return;
-            l.list[atomicAdd(&l.listed, 1u)] = make_uint2(__float_as_uint(v), (unsigned)id);
-        });
-    __syncthreads();
-    uint32_t lo = 0, hi = 0xFFFFFFFFu;                // keys of the range that holds the boundary
-    auto members_of = [&](auto f) {
-        if (list) {
-            for (unsigned i = tid; i < members; i += kDThreads) f(__uint_as_float(l.list[i].x));
-        } else {
-            r.each([&](int, float v) {
-                if (v != -INFINITY && r.bin(v) == picked && order_key(v) >= floor) f(v);
-            });
-        }
-    };
+    const unsigned members = l.listed;
+    if (members <= (unsigned)kDList) {
+        const Member me = l.list[tid < (int)members ? tid : 0];
+        unsigned rank = 0;
+        u64 before = 0;
+        if ((tid & ~63) < (int)members)
+            for (unsigned j = 0; j < members; ++j) {
+                const Member o = l.list[j];
+                const bool ahead = o.v > me.v || (o.v == me.v && o.id < me.id);
+                rank += ahead;
+                if (!BY_COUNT) before += ahead ? o.mass : 0;
+            }
+        const bool kept = tid < (int)members && (BY_COUNT ? above_c + rank < need : (double)(above_m + before) < goal);
+        const u64 vote = __ballot(kept);
+        if ((tid & 63) == 0 && vote) atomicAdd(&l.cnt, (unsigned)__popcll(vote));
+        __syncthreads();
+        if (kept && rank + 1 == l.cnt) l.cut_f = me.v, l.cut_id = me.id;
+        __syncthreads();
+        Cut c;
+        c.f = l.cut_f, c.id = l.cut_id;
+        __syncthreads();
+        return c;
+    }
+    uint32_t lo = 0, hi = 0xFFFFFFFFu;                // keys of the range that holds the last rank
     for (;;) {
         // the ends of what is left, then its histogram
         if (tid == 0) l.lo = 0xFFFFFFFFu, l.hi = 0;
-        clear_bins(l);
+        clear_bins<true, true>(l);
         uint32_t a = 0xFFFFFFFFu, b = 0;
-        members_of([&](float v) {
+        r.each([&](int id, float v) {
             const uint32_t k = order_key(v);
-            if (k >= lo && k <= hi) a = min(a, k), b = max(b, k);
+            if (r.bin(v) == picked && k >= lo && k <= hi && from.keeps(v, id)) a = min(a, k), b = max(b, k);
         });
         if (a <= b) {
             atomicMin(&l.lo, a);
@@ -289,64 +366,37 @@ __device__ Bound boundary(const DrawRow<DT, HELD>& r, bool by_count, unsigned ne
         lo = l.lo, hi = l.hi;
         int shift = 0;
         while (((hi - lo) >> shift) >= (uint32_t)kDBins) ++shift;
-        members_of([&](float v) {
+        r.each([&](int id, float v) {
             const uint32_t k = order_key(v);
-            if (k < lo || k > hi) return;
+            if (r.bin(v) != picked || k < lo || k > hi || !from.keeps(v, id)) return;
             const int bin = (int)((hi - k) >> shift);
             atomicAdd(&l.count[bin], 1u);
-            if (!by_count) atomicAdd(&l.mass[bin], mass44(r.y(v)));
+            if (!BY_COUNT) atomicAdd(&l.mass[bin], mass44(r.y(v)));
         });
-        pick_bin(l, by_count, need, goal, above_m, above_c);
+        const uint32_t h = hi - (pick_bin<true, true>(l, need, 0.0, goalp, above_m, above_c) << shift);
         above_m = l.above_mass, above_c = l.above_cnt;
-        const uint32_t h = hi - (l.first << shift);
         const unsigned n = l.cnt;
         const u64 bin_mass = l.bin_mass;
         __syncthreads();
         if (shift == 0) {
-            if (by_count) return Bound{h, min(n, need - above_c), n};
-            const u64 one = bin_mass / n;             // equal keys have equal masses
+            // n equal logits (of equal masses), of which the first e are kept
             unsigned e = n;
-            if (one) {
+            if (BY_COUNT) {
+                e = min(n, need - above_c);
+            } else if (const u64 one = bin_mass / n) {
                 const double want = (goal - (double)above_m) / (double)one;
                 e = want < (double)n ? (unsigned)max(want, 0.0) : n;
                 while (e > 0 && (double)(above_m + (u64)(e - 1) * one) >= goal) --e;
                 while (e < n && (double)(above_m + (u64)e * one) < goal) ++e;
             }
-            return Bound{h, e, n};
+            Cut c;
+            c.f = __uint_as_float(h & 0x80000000u ? h & 0x7FFFFFFFu : ~h);
+            c.id = tie_id(r, c.f, e - 1);
+            return c;
         }
         lo = max(lo, h - ((1u << shift) - 1));
         hi = h;
     }
-}
-
-// The id of tie number `ties` (from 0) among the keys equal to `key`, in id
-// order: the first that is left out.  Every thread gets it.
-template <int DT, bool HELD>
-__device__ int tie_cut(const DrawRow<DT, HELD>& r, uint32_t key, unsigned ties) {
-    DrawLds& l = r.l;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    unsigned n = 0;
-    r.each([&](int, float v) { n += v != -INFINITY && order_key(v) == key; });
-    n = wave_sum(n);
-    __syncthreads();
-    if (lane == 0) l.wc[wv] = n;
-    __syncthreads();
-    unsigned before = 0;
-    for (int i = 0; i < wv; ++i) before += l.wc[i];
-    if (before <= ties && ties < before + n) {
-        for (int i = wv * r.seg;; i += 64) {
-            const float v = i + lane < r.V ? r.at(i + lane) : -INFINITY;
-            const bool tie = v != -INFINITY && order_key(v) == key;
-            const u64 m = __ballot(tie);
-            if (tie && before + __popcll(m & ((1ull << lane) - 1)) == ties) l.token = i + lane;
-            before += __popcll(m);
-            if (before > ties) break;
-        }
-    }
-    __syncthreads();
-    const int cut = l.token;
-    __syncthreads();
-    return cut;
 }
 
 template <int DT, bool HELD>
@@ -434,40 +484,17 @@ __global__ void __launch_bounds__(kDThreads) k_draw(DrawArgs a) {
     }
     r.top = top;
 
-    // what is kept: keys above bd.key, those equal to it below the id `cut`, weights from min_p on
-    Bound bd{0, 0, 0};
-    if (by_k) bd = boundary(r, true, (unsigned)top_k, 0.0, 0);
-    if (by_p) {
-        // the mass that top-k kept, in integers: whatever falls behind its boundary among the equal keys is
-        // taken off again
-        u64 all = 0;
-        r.each([&](int, float v) {
-            if (v != -INFINITY && order_key(v) >= bd.key) all += mass44(r.y(v));
-        });
-        all = wave_sum(all);
-        __syncthreads();
-        if (lane == 0) l.wm[wv] = all;
-        __syncthreads();
-        all = 0;
-        for (int i = 0; i < kDWaves; ++i) all += l.wm[i];
-        if (bd.ties < bd.all) {
-            const uint32_t b = bd.key & 0x80000000u ? bd.key & 0x7FFFFFFFu : ~bd.key;
-            all -= (u64)(bd.all - bd.ties) * mass44(r.y(__uint_as_float(b)));
-        }
-        bd = boundary(r, false, 0u, (double)top_p * (double)all, bd.key);
-    }
-    const int cut = bd.ties < bd.all ? tie_cut(r, bd.key, bd.ties) : 0x7FFFFFFF;
-    auto keeps = [&](int id, float v) {
-        const uint32_t k = order_key(v);
-        return v != -INFINITY && (k > bd.key || (k == bd.key && id < cut));
-    };
+    // what is kept, but for min-p
+    Cut cut;
+    if (by_k) cut = last_kept<true>(r, cut, (unsigned)top_k, 0.0);
+    if (by_p) cut = last_kept<false>(r, cut, 0u, (double)top_p);
 
     // kept mass and count per wave
     if (once) {
         sum *= mine > -INFINITY ? weight(r.y(mine)) : 0.0;
     } else {
         r.each([&](int id, float v) {
-            if (!keeps(id, v)) return;
+            if (!cut.keeps(v, id)) return;
             const double w = weight(r.y(v));
             if (w >= (double)min_p) sum += w, ++cnt;
         });
@@ -492,12 +519,16 @@ __global__ void __launch_bounds__(kDThreads) k_draw(DrawArgs a) {
         before += m;
     }
     // all threads take that run, consecutive ids each
-    const int per = r.seg / kDThreads + (r.seg % kDThreads != 0), s0 = run * r.seg, s1 = min(s0 + r.seg, a.V);
+    const int per = HELD ? kDHeld / 16 : (r.seg + kDThreads - 1) / kDThreads, s0 = run * r.seg, s1 = min(s0 + r.seg, a.V);
     const int i0 = min(s0 + tid * per, s1), i1 = min(i0 + per, s1);
+    if (HELD) {
+        if (wv == run) r.each([&](int id, float v) { l.run[id - s0] = v; });
+        __syncthreads();
+    }
     auto weigh = [&](int id) {
-        const float v = r.at(id);
+        const float v = HELD ? l.run[id - s0] : r.at(id);
         const double w = weight(r.y(v));
-        return keeps(id, v) && w >= (double)min_p ? w : 0.0;
+        return cut.keeps(v, id) && w >= (double)min_p ? w : 0.0;
     };
     double own = 0.0;
     for (int id = i0; id < i1; ++id) own += weigh(id);
