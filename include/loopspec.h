@@ -591,9 +591,16 @@ typedef struct {
  * below half a unit is kept and counted but not drawn.
  * A row with a NaN or +infinity among its logits, without a finite one, or whose
  * settings or number are outside their ranges gives token -1, prob 0, kept 0.
- * Asynchronous, no workspace.  Errors: EINVAL (arguments), EHIP. */
+ * rows: up to 65535.  workspace: 16-byte aligned, its contents on entry do not
+ * matter.  Errors: EINVAL (arguments, workspace too small; checked before any
+ * launch), EHIP. */
 int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* logits_dev, int64_t stride,
-                    const double* u_dev, int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* stream);
+                    const double* u_dev, int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* workspace_dev,
+                    uint64_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace loopspec_sample needs (0 for sizes it refuses):
+ * about 64 KiB a row and 1.6 KiB per 4096 ids of it. */
+uint64_t loopspec_sample_workspace_bytes(int32_t vocab, int32_t rows);
 
 /* Library version string. */
 const char* loopspec_version(void);

@@ -167,9 +167,10 @@ def load_library() -> ctypes.CDLL:
                                                                         ctypes.c_int32]),
         "loopspec_prefix_attention": (ctypes.c_int, [P(PagedCacheC), P(PagedBatchC), P(AttentionArgs),
                                                      ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
+        "loopspec_sample_workspace_bytes": (ctypes.c_uint64, [ctypes.c_int32, ctypes.c_int32]),
         "loopspec_sample": (ctypes.c_int, [P(SampleCfg), ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
-                                           ctypes.c_void_p]),
+                                           ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)

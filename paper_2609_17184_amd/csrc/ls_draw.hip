@@ -6,27 +6,32 @@
 //   mass; min-p, of those, w_v >= min_p.  The token is the smallest id whose kept mass through it exceeds
 //   u * kept mass.  T = 0: the largest logit, lowest id.
 //
-// A row is one workgroup's.  Each of its 16 waves owns a run of ids, four
-// consecutive ones a lane; up to 65536 ids the logits stay in registers from
-// their only read.  Weights are taken in 64 bits (2^f by a polynomial on
-// [-1/2, 1/2], off by 2^-50), since a token is decided by comparing sums with u
-// times a sum.  Sums are 64-bit in an order that depends on the vocabulary
-// alone; where the order of adding is not fixed (the histograms' atomics),
-// masses are integers in units of 2^-44 of the largest weight.
+// One CU reads a row of 49152 fp32 logits in about 19 us, most of it waiting,
+// so a row is spread over shards of 4096 ids.  Three launches:
 //
-// What top-k and top-p keep is the ranks down to some last one.  A histogram
-// over 2048 bins of 1/32 octave of weight tells the bin that holds it (counts
-// for top-k; masses for top-p, of what top-k kept).  The bin's members, when
-// there are at most 1024, go to LDS and a thread each finds its member's rank
-// against all others; otherwise ranges of the logits' order-preserving integer
-// keys are searched the same way until a bin is a single key, and ties are
-// counted off by id.
+//   k_draw_shard  a workgroup per (row, shard): the shard's largest logit, its mass, and, for a row with a
+//                 filter, counts and masses over 128 bins of half an octave of weight
+//   k_draw_list   (rows with filters) the bins of all shards put together tell the few bins in which the last
+//                 kept rank and the min-p threshold lie; each shard adds its logits in them to the row's list
+//                 and sums its mass above them
+//   k_draw_pick   a workgroup per row: the last kept rank on the list, the shard that holds the token, the token
 //
-// The token: the kept mass per wave tells the run of ids, then all threads take
-// that run in id order.  A row without filters and of more than 65536 ids is
-// read once: every lane sums against its own running maximum.
+// A token is decided by comparing sums with u times a sum, so weights are taken
+// in 64 bits (2^f by a polynomial on [-1/2, 1/2], off by 2^-50) and sums have to
+// be the same whatever the order of adding: masses are integers in units of
+// 2^-44 (of a power of two at or above the shard's largest weight, or of the
+// row's largest weight), and sums of doubles run in an order that depends on the
+// vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
+//
+// The last kept rank: up to 1024 listed logits, a thread each finds its logit's
+// rank against all others; more of them first go through a histogram of 2048
+// bins of 1/32 octave, and if one of its bins still holds more than 1024, ranges
+// of the logits' order-preserving integer keys are searched the same way down to
+// a single key, whose ties are counted off by id.  A row whose list overflows is
+// searched in place.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "../../include/loopspec.h"
@@ -37,11 +42,32 @@ typedef unsigned long long u64;
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
 
+constexpr int kShard = 4096, kShardThreads = 256, kShardEach = kShard / kShardThreads;
+constexpr int kCoarse = 128;                          // bins of half an octave, the last one for all below
+constexpr int kListMax = 8192;                        // listed logits of a row
 constexpr int kDThreads = 1024, kDWaves = kDThreads / 64;
 constexpr int kDBins = 2048;                          // two per thread
-constexpr int kDList = kDThreads;
-constexpr int kDHeld = 64;                            // logits a thread holds
-constexpr int kDMaxVocab = 1 << 18;
+constexpr int kMembers = kDThreads;
+constexpr int kDMaxVocab = 1 << 18, kShardsMax = kDMaxVocab / kShard;
+static_assert(kShardsMax == 64, "a shard per lane");
+
+struct Head {                                         // of a shard
+    double e, grid;                                   // masses are in 2^(e - 44); the largest logit's place on the grid
+    u64 mass;
+    float top;
+    int arg, bad;                                     // lowest id of the largest logit; NaN or +infinity met
+    unsigned finite;
+};
+struct Entry {
+    float v;
+    int id;
+};
+struct RowPlan {                                      // what the listing found, for the pick
+    int rank;                                         // the last kept rank lies in the list
+    unsigned above_c;                                 // ranks above the listed bins
+    double above_m, all;                              // mass above them and in the whole row, in 2^ref
+    double ref;
+};
 
 struct DrawArgs {
     const void* z;
@@ -54,8 +80,51 @@ struct DrawArgs {
     int32_t* token;
     float* prob;
     int32_t* kept;
-    int V;
+    int V, S;
+    // workspace
+    Head* head;                                       // [rows][S]
+    u64* mass;                                        // [rows][S][kCoarse]
+    unsigned* count;                                  // [rows][S][kCoarse]
+    u64* above;                                       // [rows][S]: the shard's mass above the listed bins
+    RowPlan* plan;                                    // [rows]
+    Entry* list;                                      // [rows][kListMax]
+    unsigned* listed;                                 // [rows]
 };
+
+// a row's settings
+struct Setting {
+    float T, top_p, min_p;
+    int top_k;
+    double scale;                                     // log2(e) / T
+    bool ok, by_k, by_p, by_m;
+    __device__ __forceinline__ Setting(const DrawArgs& a, int row) {
+        T = a.temperature ? a.temperature[row] : a.temperature1;
+        top_p = a.top_p ? a.top_p[row] : a.top_p1;
+        min_p = a.min_p ? a.min_p[row] : a.min_p1;
+        top_k = a.top_k ? a.top_k[row] : a.top_k1;
+        const double u = a.u[row];
+        ok = T >= 0.f && T < INFINITY && top_p > 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f && u >= 0.0 && u < 1.0;
+        const bool draws = ok && T > 0.f;
+        scale = draws ? 1.4426950408889634074 / (double)T : 0.0;
+        by_k = draws && top_k > 0 && top_k < a.V;
+        by_p = draws && top_p < 1.f;
+        by_m = draws && min_p > 0.f;
+    }
+    __device__ __forceinline__ bool filters() const { return by_k || by_p || by_m; }
+    // the logit in octaves, rounded: not contracted with what is subtracted from it, which at tiny T is the
+    // same product of the largest logit
+    __device__ __forceinline__ double octaves(float v) const {
+        double t = (double)v * scale;
+        asm("" : "+v"(t));
+        return t;
+    }
+    // its place on the grid of half octaves
+    __device__ __forceinline__ double grid(float v) const { return floor(2.0 * octaves(v)); }
+};
+__device__ __forceinline__ int coarse(double grid_top, double grid) {
+    const double d = grid_top - grid;
+    return d < (double)(kCoarse - 1) ? (int)d : kCoarse - 1;
+}
 
 __device__ __forceinline__ float half_bits(int dt, uint32_t b) {
     return dt == LOOPSPEC_BF16 ? __uint_as_float(b << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b);
@@ -65,12 +134,41 @@ __device__ __forceinline__ float logit(const void* p, int64_t i) {
     if (DT == LOOPSPEC_F32) return ((const float*)p)[i];
     return half_bits(DT, ((const uint16_t*)p)[i]);
 }
+// four logits from i, one load: 4-byte aligned rows
+template <int DT>
+__device__ __forceinline__ void load4(const void* p, int64_t i, float* v) {
+    if (DT == LOOPSPEC_F32) {
+        const u32x4_a4 u = *(const u32x4_a4*)((const float*)p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(u[k]);
+    } else {
+        const u32x2_a4 u = *(const u32x2_a4*)((const uint16_t*)p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = half_bits(DT, k & 1 ? u[k >> 1] >> 16 : u[k >> 1] & 0xFFFFu);
+    }
+}
+// logits id0 + 1024 k + 4 t + (0 .. 3) of thread t and k = 0 .. 3, -infinity from V on
+template <int DT>
+__device__ __forceinline__ void load_shard(const DrawArgs& a, int64_t base, int id0, float (&v)[kShardEach]) {
+    const int id = id0 + 4 * (int)threadIdx.x;
+    const bool vec = ((uintptr_t)a.z + (uint64_t)base * (DT == LOOPSPEC_F32 ? 4 : 2)) % 4 == 0;
+    if (vec && id0 + kShard <= a.V) {
+#pragma unroll
+        for (int k = 0; k < kShardEach / 4; ++k) load4<DT>(a.z, base + id + 1024 * k, v + 4 * k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kShardEach; ++k) {
+            const int i = id + 1024 * (k / 4) + k % 4;
+            v[k] = i < a.V ? logit<DT>(a.z, base + i) : -INFINITY;
+        }
+    }
+}
 // order-preserving integer of a float that is no NaN; both zeros alike
 __device__ __forceinline__ uint32_t order_key(float z) {
     const uint32_t b = __float_as_uint(z + 0.0f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-// 2^(y + up), y <= 0 (2^(up - 200) below y = -200): y = n + f, the polynomial
+// 2^(y + up), y small or negative (2^(up - 200) below y = -200): y = n + f, the polynomial
 // interpolates 2^f at the Chebyshev points of [-1/2, 1/2] and is 1 at 0.  n comes
 // from adding 1.5 * 2^52, whose low word it then is, and goes to the exponent as
 // it is: conversions and ldexp take several times an addition's cycles.
@@ -96,6 +194,241 @@ __device__ __forceinline__ u64 mass44(double y) {
     return (u64)__double_as_longlong(weight(y, 44) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
+    return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+__device__ __forceinline__ double wave_max(double v) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v = fmax(v, __shfl_xor(v, o));
+    return v;
+}
+// x * 2^n for an integral n, 0 from 2^-300 on
+__device__ __forceinline__ double times2(double x, double n) { return n < -300.0 ? 0.0 : ldexp(x, (int)n); }
+
+template <int DT>
+__global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
+    __shared__ u64 mass[kCoarse];
+    __shared__ unsigned count[kCoarse];
+    __shared__ float wf[4];
+    __shared__ u64 wm[4];
+    __shared__ unsigned wc[4];
+    __shared__ int bad, arg;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, s = blockIdx.x, row = blockIdx.y, id0 = s * kShard;
+    float v[kShardEach];
+    load_shard<DT>(a, row * a.stride, id0, v);
+    const Setting set(a, row);
+    if (tid < kCoarse) mass[tid] = 0, count[tid] = 0;
+    if (tid == 0) bad = 0, arg = 0x7FFFFFFF;
+    float top = -INFINITY;
+    bool wrong = false;
+    unsigned n = 0;
+#pragma unroll
+    for (int k = 0; k < kShardEach; ++k) {
+        wrong |= !(v[k] < INFINITY);
+        top = fmaxf(top, v[k]);
+        n += v[k] > -INFINITY;
+    }
+    top = wave_max(top);
+    n = wave_sum(n);
+    if (lane == 0) wf[wv] = top, wc[wv] = n;
+    __syncthreads();
+    if (wrong) bad = 1;
+    top = fmaxf(fmaxf(wf[0], wf[1]), fmaxf(wf[2], wf[3]));
+    const double tt = set.octaves(top), e = top > -INFINITY ? floor(tt) + 1.0 : 0.0, grid = set.grid(top);
+    u64 sum = 0;
+    if (set.T > 0.f && top > -INFINITY) {
+#pragma unroll
+        for (int k0 = 0; k0 < kShardEach; k0 += 4) {
+            u64 m[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m[k] = mass44(set.octaves(v[k0 + k]) - e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += m[k];
+            if (set.filters())
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (v[k0 + k] > -INFINITY) {
+                        const int b = coarse(grid, set.grid(v[k0 + k]));
+                        atomicAdd(&mass[b], m[k]);
+                        atomicAdd(&count[b], 1u);
+                    }
+        }
+        sum = wave_sum(sum);
+        if (lane == 0) wm[wv] = sum;
+    } else {
+        if (lane == 0) wm[wv] = 0;
+        if (set.T == 0.f) {
+            int best = 0x7FFFFFFF;
+#pragma unroll
+            for (int k = kShardEach - 1; k >= 0; --k)
+                if (v[k] == top) best = id0 + 4 * tid + 1024 * (k / 4) + k % 4;
+            if (best < 0x7FFFFFFF) atomicMin(&arg, best);
+        }
+    }
+    __syncthreads();
+    const size_t at = (size_t)row * a.S + s;
+    if (set.filters() && tid < kCoarse) a.mass[at * kCoarse + tid] = mass[tid], a.count[at * kCoarse + tid] = count[tid];
+    if (tid == 0) {
+        a.head[at] = Head{e, grid, wm[0] + wm[1] + wm[2] + wm[3], top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
+        if (s == 0) a.listed[row] = 0;
+    }
+}
+
+// what a row's shards have in common; every wave works it out from the heads
+struct Whole {
+    float top;
+    double grid, ref;                                 // of the row's largest logit; the largest e
+    bool bad;
+    Head mine;                                        // lane s: shard s's (nothing in it behind the last one)
+    __device__ __forceinline__ Whole(const DrawArgs& a, int row) {
+        const int lane = threadIdx.x & 63;
+        mine = Head{-1e300, -INFINITY, 0, -INFINITY, 0x7FFFFFFF, 0, 0};
+        if (lane < a.S) mine = a.head[(size_t)row * a.S + lane];
+        if (!(mine.top > -INFINITY)) mine.e = -1e300, mine.grid = -INFINITY;
+        top = wave_max(mine.top);
+        grid = wave_max(mine.grid);
+        ref = wave_max(mine.e);
+        bad = __any(mine.bad);
+    }
+};
+
+template <int DT>
+__global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
+    __shared__ double he[kShardsMax], part_m[2][kCoarse];
+    __shared__ int ho[kShardsMax];
+    __shared__ unsigned part_c[2][kCoarse];
+    __shared__ int range[2];
+    __shared__ u64 wm[4];
+    __shared__ unsigned n, base;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, s = blockIdx.x, row = blockIdx.y;
+    const Setting set(a, row);
+    if (!set.filters()) return;
+    const Whole r(a, row);
+    if (r.bad || !(r.top > -INFINITY)) return;
+    const size_t row0 = (size_t)row * a.S;
+    if (tid < a.S) {
+        // (a shard without a finite logit has empty bins, wherever they go)
+        he[tid] = r.mine.e;
+        ho[tid] = r.mine.grid > -INFINITY ? coarse(r.grid, r.mine.grid) : 0;
+    }
+    if (tid == 0) n = 0;
+    __syncthreads();
+    // the row's bins: a thread per bin and half of the shards
+    {
+        const int b = tid & (kCoarse - 1), h = tid / kCoarse, half = (a.S + 1) / 2;
+        double m = 0.0;
+        unsigned c = 0;
+        for (int k = h * half; k < min(a.S, (h + 1) * half); ++k) {
+            const u64* sm = a.mass + (row0 + k) * kCoarse;
+            const unsigned* sc = a.count + (row0 + k) * kCoarse;
+            const int own = b - ho[k];
+            if (b < kCoarse - 1) {
+                if (own >= 0) m += times2((double)sm[own], he[k] - r.ref), c += sc[own];
+            } else {
+                for (int i = max(own, 0); i < kCoarse; ++i) m += times2((double)sm[i], he[k] - r.ref), c += sc[i];
+            }
+        }
+        part_m[h][b] = m, part_c[h][b] = c;
+    }
+    __syncthreads();
+    if (wv == 0) {
+        const double m0 = part_m[0][2 * lane] + part_m[1][2 * lane], m1 = part_m[0][2 * lane + 1] + part_m[1][2 * lane + 1];
+        const unsigned c0 = part_c[0][2 * lane] + part_c[1][2 * lane], c1 = part_c[0][2 * lane + 1] + part_c[1][2 * lane + 1];
+        double sm = m0 + m1;
+        unsigned sc = c0 + c1;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const double x = __shfl_up(sm, o);
+            const unsigned y = __shfl_up(sc, o);
+            if (lane >= o) sm += x, sc += y;
+        }
+        const double all = __shfl(sm, 63);
+        const unsigned long long used = __ballot(c0 + c1 > 0);
+        const int last_lane = 63 - __clzll(used), last = 2 * last_lane + (__shfl(c1, last_lane) > 0);
+        // first bin that meets a condition on (mass through, count through), the last occupied one when none does
+        auto first = [&](auto meets) {
+            const bool low = meets(sm - m1, sc - c1), high = meets(sm, sc);
+            const unsigned long long hit = __ballot(high);
+            if (!hit) return last;
+            const int l = __ffsll(hit) - 1;
+            return min(2 * l + (__shfl((int)low, l) ? 0 : 1), last);
+        };
+        int lo = kCoarse, hi = -1;
+        double share = all;                           // bounds of the mass that top-k keeps, as far as known
+        if (set.by_k) {
+            hi = lo = first([&](double, unsigned c) { return c >= (unsigned)set.top_k; });
+            const double above = __shfl(sm - m0 - m1, hi / 2) + (hi & 1 ? __shfl(m0, hi / 2) : 0.0);
+            share = above;
+        }
+        if (set.by_p) {
+            // (a hair of slack: these sums of doubles and the exact ones need not round alike)
+            const double p = (double)set.top_p;
+            const int b = first([&](double m, unsigned) { return m >= p * share * (1.0 - 1e-9); });
+            const int b2 = first([&](double m, unsigned) { return m >= p * share * (1.0 + 1e-9); });
+            lo = min(lo, b);
+            hi = max(hi, b2);
+        }
+        bool rank = set.by_k || set.by_p;
+        if (set.by_m) {
+            // both bins that the threshold may lie in
+            const double t = set.octaves(r.top) + log2((double)set.min_p);
+            const int b = min(coarse(r.grid, floor(2.0 * t + 1e-6)), last), b2 = min(coarse(r.grid, floor(2.0 * t - 1e-6)), last);
+            if (!rank || b2 < lo) {
+                rank = false;
+                lo = b, hi = b2;
+            } else if (b < lo) {
+                lo = b;
+            }
+        }
+        const double am = __shfl(sm - m0 - m1, lo / 2) + (lo & 1 ? __shfl(m0, lo / 2) : 0.0);
+        const unsigned ac = __shfl(sc - c0 - c1, lo / 2) + (lo & 1 ? __shfl(c0, lo / 2) : 0u);
+        if (lane == 0) {
+            range[0] = lo, range[1] = hi;
+            if (s == 0) a.plan[row] = RowPlan{rank, ac, am, all, r.ref};
+        }
+    }
+    __syncthreads();
+    const int lo = range[0], hi = range[1];
+    // this shard: its mass above the listed bins, its members in them
+    u64 above = 0;
+    bool some = false;
+    if (tid < kCoarse) {
+        const int b = min(ho[s] + tid, kCoarse - 1);
+        if (b < lo) above = a.mass[(row0 + s) * kCoarse + tid];
+        some = b >= lo && b <= hi && a.count[(row0 + s) * kCoarse + tid] > 0;
+    }
+    above = wave_sum(above);
+    if (lane == 0) wm[wv] = above;
+    const bool any = __syncthreads_or(some);
+    if (tid == 0) a.above[row0 + s] = wm[0] + wm[1];
+    if (!any) return;
+    float v[kShardEach];
+    load_shard<DT>(a, row * a.stride, s * kShard, v);
+    unsigned at[kShardEach];
+#pragma unroll
+    for (int k = 0; k < kShardEach; ++k) {
+        at[k] = ~0u;
+        if (!(v[k] > -INFINITY)) continue;
+        const int b = coarse(r.grid, set.grid(v[k]));
+        if (b >= lo && b <= hi) at[k] = atomicAdd(&n, 1u);
+    }
+    __syncthreads();
+    if (tid == 0) base = atomicAdd(&a.listed[row], n);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kShardEach; ++k)
+        if (at[k] != ~0u && base + at[k] < (unsigned)kListMax)
+            a.list[(size_t)row * kListMax + base + at[k]] = Entry{v[k], s * kShard + 4 * tid + 1024 * (k / 4) + k % 4};
+}
+
 // the last kept rank: logits above f are kept, and those equal to it up to id
 struct Cut {
     float f = -INFINITY;
@@ -110,95 +443,40 @@ struct Member {
 };
 
 struct DrawLds {
-    union {
-        u64 mass[kDBins];
-        float run[kDBins * 2];                        // the logits of the wave that holds the token
-    };
+    u64 mass[kDBins];
     unsigned count[kDBins];
-    Member list[kDList];
+    Member list[kMembers];
+    u64 shard[kShardsMax];                            // kept mass of the searched logits, per shard
+    double ws[kShardsMax];                            // kept mass per shard
     u64 wm[kDWaves];
     double wd[kDWaves];
     unsigned wc[kDWaves];
-    float wf[kDWaves];
-    unsigned first, last, listed, lo, hi, cnt, above_cnt;
-    u64 bin_mass, above_mass;
-    int bad, token;
+    unsigned first, last, listed, lo, hi, cnt, above_cnt, kept;
+    u64 above_mass;
     float cut_f;
     int cut_id;
 };
 
-template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-    return v;
-}
-
-// the row as its workgroup sees it
-template <int DT, bool HELD>
-struct DrawRow {
-    static constexpr int B = 16;                      // logits of a lane's batch
-    const void* z;
+// Logits among which a rank is searched: the row's list, or the whole row.
+template <int DT>
+struct Search {
+    const DrawArgs& a;
     int64_t base;
-    int V, seg;                                       // wave w owns ids [w * seg, (w + 1) * seg)
-    bool vec;                                         // 4-byte aligned: four logits a load
+    const Entry* list;                                // null: the whole row
+    int n;
+    float top;
+    double scale;
     DrawLds& l;
-    float top = 0.f;                                  // the largest logit
-    double scale = 0.0;                               // log2(e) / T
-    float x[HELD ? kDHeld : 1];
-
-    __device__ __forceinline__ float at(int id) const { return logit<DT>(z, base + id); }
-    // four logits from id, a load for 4-byte aligned rows
-    __device__ __forceinline__ void load4(int id, float* v) const {
-        if (DT == LOOPSPEC_F32) {
-            const u32x4_a4 u = *(const u32x4_a4*)((const float*)z + base + id);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(u[i]);
-        } else {
-            const u32x2_a4 u = *(const u32x2_a4*)((const uint16_t*)z + base + id);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = half_bits(DT, i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu);
-        }
-    }
-    __device__ __forceinline__ int first() const { return (int)(threadIdx.x >> 6) * seg + (int)(threadIdx.x & 63) * 4; }
-    __device__ __forceinline__ int end() const { return min(((int)(threadIdx.x >> 6) + 1) * seg, V); }
-    // batch j: 4 logits in each of 4 consecutive blocks of 256 ids of the wave; -infinity where there is none
-    __device__ __forceinline__ void load_batch(int j, float* v) const {
-        const int b = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * seg + j * (64 * B));
-        if (b + 64 * B <= __builtin_amdgcn_readfirstlane(end()) && vec) {
-#pragma unroll
-            for (int k = 0; k < B / 4; ++k) load4(first() + j * (64 * B) + k * 256, v + 4 * k);
-        } else {
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int id = first() + j * (64 * B) + (k / 4) * 256 + k % 4;
-                v[k] = id < end() ? at(id) : -INFINITY;
-            }
-        }
-    }
-    __device__ __forceinline__ void hold() {
-        if constexpr (HELD) {
-#pragma unroll
-            for (int j = 0; j < kDHeld / B; ++j) load_batch(j, x + j * B);
-        }
-    }
-    // f(id, logit) for every id of the thread, and -infinity for places without one
+    // f(id, logit)
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        if constexpr (HELD) {
-#pragma unroll
-            for (int j = 0; j < kDHeld / 4; ++j) {
-                if (j * 256 >= seg) break;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f(first() + j * 256 + i, x[j * 4 + i]);
+        if (list) {
+            for (int i = threadIdx.x; i < n; i += kDThreads) {
+                const Entry e = list[i];
+                f(e.id, e.v);
             }
         } else {
-            for (int j = 0; j * 64 * B < seg; ++j) {
-                float v[B];
-                load_batch(j, v);
-#pragma unroll
-                for (int i = 0; i < B; ++i) f(first() + (j * (B / 4) + i / 4) * 256 + i % 4, v[i]);
-            }
+            for (int i = threadIdx.x; i < a.V; i += kDThreads) f(i, logit<DT>(a.z, base + i));
         }
     }
     __device__ __forceinline__ double y(float v) const { return ((double)v - (double)top) * scale; }
@@ -221,8 +499,9 @@ __device__ __forceinline__ void clear_bins(DrawLds& l) {
 
 // The bin that holds the last kept rank: the first one through which the count
 // reaches `need` (COUNT), or the mass reaches `goal`; the last occupied one when
-// none does.  share > 0: the goal is that share of the bins' whole mass.  What
-// the bin and (above_m and above_c included) all above it hold is left in l.
+// none does.  share > 0: the goal is that share of the bins' whole mass and what
+// is above them.  What lies above the bin (above_m and above_c included) is left
+// in l, and the bin's count.
 template <bool MASS, bool COUNT>
 __device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* goal, u64 above_m, unsigned above_c) {
     __syncthreads();
@@ -253,7 +532,7 @@ __device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* go
         if (i < wv) sm += l.wm[i], sc += l.wc[i];
         all += l.wm[i];
     }
-    if (share > 0.0) *goal = share * (double)all;
+    if (share > 0.0) *goal = share * (double)(above_m + all);
     const u64 am[2] = {sm, sm + m[0]};                // above each of the thread's bins
     const unsigned ac[2] = {sc, sc + c[0]};
 #pragma unroll
@@ -267,66 +546,69 @@ __device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* go
     const unsigned at = l.first < (unsigned)kDBins ? l.first : l.last;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (at == (unsigned)(b0 + i)) l.cnt = c[i], l.bin_mass = m[i], l.above_mass = am[i], l.above_cnt = ac[i];
+        if (at == (unsigned)(b0 + i)) l.cnt = c[i], l.above_mass = am[i], l.above_cnt = ac[i];
     __syncthreads();
     return at;
 }
 
-// Id of tie number `tie` (from 0, in id order) among the logits equal to f.
-template <int DT, bool HELD>
-__device__ int tie_id(const DrawRow<DT, HELD>& r, float f, unsigned tie) {
+// Id of the tie with `ties` ids up to its own among the logits equal to f: by
+// halving the ids.
+template <int DT>
+__device__ int tie_id(const Search<DT>& r, Cut from, float f, unsigned ties) {
     DrawLds& l = r.l;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    unsigned n = 0;
-    r.each([&](int, float v) { n += v == f; });
-    n = wave_sum(n);
-    __syncthreads();
-    if (lane == 0) l.wc[wv] = n;
-    __syncthreads();
-    unsigned before = 0;
-    for (int i = 0; i < wv; ++i) before += l.wc[i];
-    if (before <= tie && tie < before + n) {
-        for (int i = wv * r.seg;; i += 64) {
-            const bool eq = i + lane < r.V && r.at(i + lane) == f;
-            const u64 m = __ballot(eq);
-            if (eq && before + __popcll(m & ((1ull << lane) - 1)) == tie) l.token = i + lane;
-            before += __popcll(m);
-            if (before > tie) break;
-        }
+    int lo = 0, hi = r.a.V - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        unsigned c = 0;
+        r.each([&](int id, float v) { c += v == f && id <= mid && from.keeps(v, id); });
+        c = wave_sum(c);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) l.wc[threadIdx.x >> 6] = c;
+        __syncthreads();
+        c = 0;
+        for (int i = 0; i < kDWaves; ++i) c += l.wc[i];
+        if (c >= ties)
+            hi = mid;
+        else
+            lo = mid + 1;
     }
     __syncthreads();
-    const int id = l.token;
-    __syncthreads();
-    return id;
+    return lo;
 }
 
 // The last kept rank of what `from` keeps: the first `need` ranks (BY_COUNT), or
-// the ranks whose preceding mass is below `share` of all of it.
-template <bool BY_COUNT, int DT, bool HELD>
-__device__ Cut last_kept(const DrawRow<DT, HELD>& r, Cut from, unsigned need, double share) {
+// the ranks whose preceding mass is below the goal: `share` of the whole mass
+// (above and searched) or, share 0, the given one.  above_c ranks of mass above_m
+// lie above all that is searched.
+template <bool BY_COUNT, int DT>
+__device__ Cut last_kept(const Search<DT>& r, Cut from, unsigned need, double share, double goal, u64 above_m, unsigned above_c) {
     DrawLds& l = r.l;
     const int tid = threadIdx.x;
-    double goal = 0.0, *const goalp = BY_COUNT ? nullptr : &goal;
-    clear_bins<!BY_COUNT, BY_COUNT>(l);
+    double* const goalp = BY_COUNT ? nullptr : &goal;
+    int picked = -1;                                  // bin of the members; -1: any
+    if (r.n > kMembers || share > 0.0) {
+        clear_bins<!BY_COUNT, BY_COUNT>(l);
+        r.each([&](int id, float v) {
+            if (!from.keeps(v, id)) return;
+            if (BY_COUNT)
+                atomicAdd(&l.count[r.bin(v)], 1u);
+            else
+                atomicAdd(&l.mass[r.bin(v)], mass44(r.y(v)));
+        });
+        picked = (int)pick_bin<!BY_COUNT, BY_COUNT>(l, need, share, goalp, above_m, above_c);
+        above_m = l.above_mass, above_c = l.above_cnt;
+    }
+    __syncthreads();
+    if (tid == 0) l.listed = 0, l.cnt = 0;
+    __syncthreads();
     r.each([&](int id, float v) {
-        if (!from.keeps(v, id)) return;
-        if (BY_COUNT)
-            atomicAdd(&l.count[r.bin(v)], 1u);
-        else
-            atomicAdd(&l.mass[r.bin(v)], mass44(r.y(v)));
-    });
-    const int picked = (int)pick_bin<!BY_COUNT, BY_COUNT>(l, need, share, goalp, 0, 0);
-    u64 above_m = l.above_mass;
-    unsigned above_c = l.above_cnt;
-    r.each([&](int id, float v) {
-        if (r.bin(v) != picked || !from.keeps(v, id)) return;
+        if ((picked >= 0 && r.bin(v) != picked) || !from.keeps(v, id)) return;
         const unsigned at = atomicAdd(&l.listed, 1u);
-        if (at < (unsigned)kDList) l.list[at] = Member{v, id, BY_COUNT ? 0 : mass44(r.y(v))};
+        if (at < (unsigned)kMembers) l.list[at] = Member{v, id, BY_COUNT ? 0 : mass44(r.y(v))};
     });
-    if (tid == 0) l.cnt = 0;
     __syncthreads();
     const unsigned members = l.listed;
-    if (members <= (unsigned)kDList) {
+    if (members <= (unsigned)kMembers) {
         const Member me = l.list[tid < (int)members ? tid : 0];
         unsigned rank = 0;
         u64 before = 0;
@@ -341,7 +623,8 @@ __device__ Cut last_kept(const DrawRow<DT, HELD>& r, Cut from, unsigned need, do
         const u64 vote = __ballot(kept);
         if ((tid & 63) == 0 && vote) atomicAdd(&l.cnt, (unsigned)__popcll(vote));
         __syncthreads();
-        if (kept && rank + 1 == l.cnt) l.cut_f = me.v, l.cut_id = me.id;
+        // (none kept: sums of doubles put the goal just above the members; their first one it is)
+        if (tid < (int)members && rank == (l.cnt ? l.cnt - 1 : 0u)) l.cut_f = me.v, l.cut_id = me.id;
         __syncthreads();
         Cut c;
         c.f = l.cut_f, c.id = l.cut_id;
@@ -376,22 +659,22 @@ __device__ Cut last_kept(const DrawRow<DT, HELD>& r, Cut from, unsigned need, do
         const uint32_t h = hi - (pick_bin<true, true>(l, need, 0.0, goalp, above_m, above_c) << shift);
         above_m = l.above_mass, above_c = l.above_cnt;
         const unsigned n = l.cnt;
-        const u64 bin_mass = l.bin_mass;
         __syncthreads();
         if (shift == 0) {
-            // n equal logits (of equal masses), of which the first e are kept
+            // n equal logits, of which the first e are kept
+            Cut c;
+            c.f = __uint_as_float(h & 0x80000000u ? h & 0x7FFFFFFFu : ~h);
             unsigned e = n;
             if (BY_COUNT) {
                 e = min(n, need - above_c);
-            } else if (const u64 one = bin_mass / n) {
+            } else if (const u64 one = mass44(r.y(c.f))) {
                 const double want = (goal - (double)above_m) / (double)one;
-                e = want < (double)n ? (unsigned)max(want, 0.0) : n;
-                while (e > 0 && (double)(above_m + (u64)(e - 1) * one) >= goal) --e;
+                e = want < (double)n ? (unsigned)max(want, 1.0) : n;
+                while (e > 1 && (double)(above_m + (u64)(e - 1) * one) >= goal) --e;
                 while (e < n && (double)(above_m + (u64)e * one) < goal) ++e;
             }
-            Cut c;
-            c.f = __uint_as_float(h & 0x80000000u ? h & 0x7FFFFFFFu : ~h);
-            c.id = tie_id(r, c.f, e - 1);
+            c.id = e < n ? tie_id(r, from, c.f, e) : 0x7FFFFFFF;
+            if (e == n && c.f == from.f) c.id = from.id;
             return c;
         }
         lo = max(lo, h - ((1u << shift) - 1));
@@ -399,181 +682,173 @@ __device__ Cut last_kept(const DrawRow<DT, HELD>& r, Cut from, unsigned need, do
     }
 }
 
-template <int DT, bool HELD>
-__global__ void __launch_bounds__(kDThreads) k_draw(DrawArgs a) {
+template <int DT>
+__global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     __shared__ DrawLds l;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const float T = a.temperature ? a.temperature[row] : a.temperature1;
-    const float top_p = a.top_p ? a.top_p[row] : a.top_p1, min_p = a.min_p ? a.min_p[row] : a.min_p1;
-    const int top_k = a.top_k ? a.top_k[row] : a.top_k1;
-    const double u = a.u[row];
-    bool ok = T >= 0.f && T < INFINITY && top_p > 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f && u >= 0.0 && u < 1.0;
-    DrawRow<DT, HELD> r{a.z, row * a.stride, a.V, ((a.V + kDWaves - 1) / kDWaves + 255) / 256 * 256, false, l};
-    r.vec = ((uintptr_t)a.z + (uint64_t)r.base * (DT == LOOPSPEC_F32 ? 4 : 2)) % 4 == 0;
-    if (T > 0.f) r.scale = 1.4426950408889634074 / (double)T;
-    const bool by_k = top_k > 0 && top_k < a.V, by_p = top_p < 1.f, by_m = min_p > 0.f;
-    // rows read once: the lane's sum against its own maximum
-    const bool once = !HELD && T > 0.f && !by_k && !by_p && !by_m;
-
-    float top = -INFINITY;
-    bool bad = false;
-    double sum = 0.0;
-    unsigned cnt = 0;
-    if (once) {
-        constexpr int B = DrawRow<DT, HELD>::B;
-        float v[B], nx[B];
-        r.load_batch(0, v);
-        for (int j = 0; j * 64 * B < r.seg; ++j) {
-            if ((j + 1) * 64 * B < r.seg) r.load_batch(j + 1, nx);
-            float m = v[0];
+    const Setting set(a, row);
+    const Whole w(a, row);
+    const size_t row0 = (size_t)row * a.S;
+    if (!set.ok || w.bad || !(w.top > -INFINITY) || set.T == 0.f) {
+        const bool greedy = set.ok && !w.bad && w.top > -INFINITY;
+        int best = w.mine.top == w.top ? w.mine.arg : 0x7FFFFFFF;
 #pragma unroll
-            for (int i = 0; i < B; ++i) {
-                bad |= !(v[i] < INFINITY);
-                m = fmaxf(m, v[i]);
-            }
-            if (__any(m > top)) {
-                const float now = fmaxf(top, m);
-                if (top > -INFINITY) sum *= weight(((double)top - (double)now) * r.scale);
-                top = now;
-            }
-#pragma unroll
-            for (int i = 0; i < B; ++i) {
-                const double w = weight(((double)v[i] - (double)top) * r.scale);
-                if (v[i] != -INFINITY) sum += w, ++cnt;
-            }
-#pragma unroll
-            for (int i = 0; i < B; ++i) v[i] = nx[i];
-        }
-    } else {
-        r.hold();
-        r.each([&](int, float v) {
-            bad |= !(v < INFINITY);
-            top = fmaxf(top, v);
-        });
-    }
-    const float mine = top;
-    for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
-    if (tid == 0) l.bad = 0, l.token = 0x7FFFFFFF, l.first = kDThreads, l.last = 0;
-    if (lane == 0) l.wf[wv] = top;
-    __syncthreads();
-    if (bad) l.bad = 1;
-    for (int i = 0; i < kDWaves; ++i) top = fmaxf(top, l.wf[i]);
-    __syncthreads();
-    ok = ok && !l.bad && top > -INFINITY;
-    if (!ok) {
+        for (int o = 1; o < 64; o *= 2) best = min(best, __shfl_xor(best, o));
         if (tid == 0) {
-            a.token[row] = -1;
-            if (a.prob) a.prob[row] = 0.f;
-            if (a.kept) a.kept[row] = 0;
+            a.token[row] = greedy ? best : -1;
+            if (a.prob) a.prob[row] = greedy ? 1.f : 0.f;
+            if (a.kept) a.kept[row] = greedy ? 1 : 0;
         }
         return;
     }
-    if (T == 0.f) {
-        int best = 0x7FFFFFFF;
-        r.each([&](int i, float v) {
-            if (v == top) best = min(best, i);
-        });
-        if (best < 0x7FFFFFFF) atomicMin(&l.token, best);
-        __syncthreads();
-        if (tid == 0) {
-            a.token[row] = l.token;
-            if (a.prob) a.prob[row] = 1.f;
-            if (a.kept) a.kept[row] = 1;
-        }
-        return;
-    }
-    r.top = top;
-
-    // what is kept, but for min-p
+    const double top = set.octaves(w.top);
+    const bool filters = set.filters();
+    const unsigned listed = filters ? a.listed[row] : 0u;
+    const bool fits = listed <= (unsigned)kListMax;
+    Search<DT> r{a, row * a.stride, fits ? a.list + (size_t)row * kListMax : nullptr, fits ? (int)listed : a.V, w.top, set.scale, l};
+    if (tid < kShardsMax) l.shard[tid] = 0;
+    if (tid == 0) l.kept = 0;
+    __syncthreads();
     Cut cut;
-    if (by_k) cut = last_kept<true>(r, cut, (unsigned)top_k, 0.0);
-    if (by_p) cut = last_kept<false>(r, cut, 0u, (double)top_p);
-
-    // kept mass and count per wave
-    if (once) {
-        sum *= mine > -INFINITY ? weight(r.y(mine)) : 0.0;
-    } else {
+    unsigned above_c = 0;
+    if (filters) {
+        RowPlan plan = a.plan[row];
+        // masses in units of 2^-44 of the row's largest weight
+        const double unit = weight(plan.ref - top);
+        u64 above_m = (u64)rint(plan.above_m * unit);
+        above_c = plan.above_c;
+        if (!fits) above_m = 0, above_c = 0, plan.rank = set.by_k || set.by_p;
+        if (plan.rank && set.by_k) cut = last_kept<true>(r, cut, (unsigned)set.top_k, 0.0, 0.0, above_m, above_c);
+        if (plan.rank && set.by_p) {
+            // (the list alone holds what top-k kept; without top-k the row's mass is known)
+            const bool whole = fits && !set.by_k;
+            cut = last_kept<false>(r, cut, 0u, whole ? 0.0 : (double)set.top_p, whole ? (double)set.top_p * (plan.all * unit) : 0.0, above_m, above_c);
+        }
+        unsigned n = 0;
         r.each([&](int id, float v) {
             if (!cut.keeps(v, id)) return;
-            const double w = weight(r.y(v));
-            if (w >= (double)min_p) sum += w, ++cnt;
+            const double y = r.y(v);
+            if (weight(y) < (double)set.min_p) return;
+            atomicAdd(&l.shard[id / kShard], mass44(y));
+            ++n;
         });
+        n = wave_sum(n);
+        if (lane == 0 && n) atomicAdd(&l.kept, n);
+        __syncthreads();
     }
-    sum = wave_sum(sum);
-    cnt = wave_sum(cnt);
-    __syncthreads();
+    // kept mass per shard, in 2^-44 of the row's largest weight
+    if (tid < a.S) {
+        double m = 0.0;
+        if (w.mine.top > -INFINITY && (!filters || fits))
+            m = (double)(filters ? a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
+        l.ws[tid] = m + (double)l.shard[tid];
+    }
+    const unsigned finite = wave_sum(w.mine.finite);
     if (tid == 0) l.first = kDThreads, l.last = 0;
-    if (lane == 0) l.wd[wv] = sum, l.wc[wv] = cnt;
     __syncthreads();
+    const unsigned kept = filters ? above_c + l.kept : finite;
     double all = 0.0;
-    unsigned kept = 0;
-    for (int i = 0; i < kDWaves; ++i) all += l.wd[i], kept += l.wc[i];
-    // the wave whose run of ids holds the token (sums may round up to the goal: then the last run with any mass)
-    const double goal = u * all;
+    for (int i = 0; i < a.S; ++i) all += l.ws[i];
+    // the shard that holds the token (sums may round up to the goal: then the last one with any mass)
+    const double goal = a.u[row] * all;
     double before = 0.0, rest = 0.0;
-    int run = -1;
-    for (int i = 0; i < kDWaves; ++i) {
-        const double m = l.wd[i];
-        if (m > 0.0 && (run < 0 || before <= goal)) run = i, rest = goal - before;
+    int run = 0;
+    bool found = false;
+    for (int i = 0; i < a.S; ++i) {
+        const double m = l.ws[i];
+        if (m > 0.0 && (!found || before <= goal)) run = i, rest = goal - before, found = true;
         if (m > 0.0 && before + m > goal) break;
         before += m;
     }
-    // all threads take that run, consecutive ids each
-    const int per = HELD ? kDHeld / 16 : (r.seg + kDThreads - 1) / kDThreads, s0 = run * r.seg, s1 = min(s0 + r.seg, a.V);
-    const int i0 = min(s0 + tid * per, s1), i1 = min(i0 + per, s1);
-    if (HELD) {
-        if (wv == run) r.each([&](int id, float v) { l.run[id - s0] = v; });
-        __syncthreads();
+    // its ids in order, four a thread
+    double own[4], sum = 0.0;
+    const int id0 = run * kShard + 4 * tid;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float v = id0 + k < a.V ? logit<DT>(a.z, r.base + id0 + k) : -INFINITY;
+        const double x = weight(r.y(v));
+        own[k] = cut.keeps(v, id0 + k) && x >= (double)set.min_p ? x * 17592186044416.0 : 0.0;
+        sum += own[k];
     }
-    auto weigh = [&](int id) {
-        const float v = HELD ? l.run[id - s0] : r.at(id);
-        const double w = weight(r.y(v));
-        return cut.keeps(v, id) && w >= (double)min_p ? w : 0.0;
-    };
-    double own = 0.0;
-    for (int id = i0; id < i1; ++id) own += weigh(id);
-    double upto = own;
+    double upto = sum;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
         const double v = __shfl_up(upto, o);
         if (lane >= o) upto += v;
     }
-    __syncthreads();
     if (lane == 63) l.wd[wv] = upto;
     __syncthreads();
-    double at = 0.0;
-    for (int i = 0; i < wv; ++i) at += l.wd[i];
-    upto += at;
-    if (own > 0.0) {
+    for (int i = 0; i < wv; ++i) upto += l.wd[i];
+    if (sum > 0.0) {
         atomicMax(&l.last, (unsigned)tid);
         if (upto > rest) atomicMin(&l.first, (unsigned)tid);
     }
     __syncthreads();
     if (tid == (int)(l.first < (unsigned)kDThreads ? l.first : l.last)) {
         // the first id of the thread's whose mass passes the rest, or its last with any mass
-        double m = upto - own, w = 0.0;
+        double m = upto - sum, x = 0.0;
         int token = -1;
-        for (int id = i0; id < i1; ++id) {
-            const double x = weigh(id);
-            if (!(x > 0.0)) continue;
-            m += x;
-            token = id, w = x;
-            if (m > rest) break;
-        }
+        bool done = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (own[k] > 0.0 && !done) {
+                m += own[k];
+                token = id0 + k, x = own[k];
+                done = m > rest;
+            }
         a.token[row] = token;
-        if (a.prob) a.prob[row] = (float)(w / all);
+        if (a.prob) a.prob[row] = (float)(x / all);
         if (a.kept) a.kept[row] = (int)kept;
     }
 }
 
+namespace {
+
+// the workspace's parts, each 16-byte aligned; null: its size
+uint64_t draw_workspace(int V, int64_t rows, char* p, DrawArgs* a) {
+    const int64_t S = (V + kShard - 1) / kShard;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        char* const q = p ? p + at : nullptr;
+        at += (bytes + 15) / 16 * 16;
+        return q;
+    };
+    a->S = (int)S;
+    a->head = (Head*)take(rows * S * sizeof(Head));
+    a->mass = (u64*)take(rows * S * kCoarse * 8);
+    a->count = (unsigned*)take(rows * S * kCoarse * 4);
+    a->above = (u64*)take(rows * S * 8);
+    a->plan = (RowPlan*)take(rows * sizeof(RowPlan));
+    a->list = (Entry*)take(rows * kListMax * sizeof(Entry));
+    a->listed = (unsigned*)take(rows * 4);
+    return at;
+}
+
+template <int DT>
+int draw_launch(DrawArgs& a, int rows, bool filters, hipStream_t st) {
+    void* args[] = {&a};
+    const dim3 grid(a.S, rows);
+    if (hipLaunchKernel((const void*)k_draw_shard<DT>, grid, dim3(kShardThreads), args, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    if (filters && hipLaunchKernel((const void*)k_draw_list<DT>, grid, dim3(kShardThreads), args, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    return hipLaunchKernel((const void*)k_draw_pick<DT>, dim3(rows), dim3(kDThreads), args, 0, st) == hipSuccess ? LOOPSPEC_OK : LOOPSPEC_EHIP;
+}
+
+}  // namespace
 }  // namespace ls
 
 extern "C" {
 
+uint64_t loopspec_sample_workspace_bytes(int32_t vocab, int32_t rows) {
+    if (vocab < 1 || vocab > ls::kDMaxVocab || rows < 1 || rows > 65535) return 0;
+    ls::DrawArgs a{};
+    return ls::draw_workspace(vocab, rows, nullptr, &a);
+}
+
 int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* logits_dev, int64_t stride, const double* u_dev,
-                    int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* stream) {
+                    int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* workspace_dev, uint64_t workspace_bytes,
+                    void* stream) {
     using namespace ls;
-    if (!cfg || rows < 0 || !logits_dev || !u_dev || !token_dev || stride < 0) return LOOPSPEC_EINVAL;
+    if (!cfg || rows < 0 || rows > 65535 || !logits_dev || !u_dev || !token_dev || stride < 0) return LOOPSPEC_EINVAL;
     if (cfg->vocab < 1 || cfg->vocab > kDMaxVocab) return LOOPSPEC_EINVAL;
     if (cfg->dtype != LOOPSPEC_F32 && cfg->dtype != LOOPSPEC_BF16 && cfg->dtype != LOOPSPEC_F16) return LOOPSPEC_EINVAL;
     if ((uintptr_t)logits_dev % (cfg->dtype == LOOPSPEC_F32 ? 4 : 2)) return LOOPSPEC_EINVAL;
@@ -583,13 +858,14 @@ int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* lo
     if (!rows) return LOOPSPEC_OK;
     DrawArgs a{logits_dev, stride, u_dev, cfg->temperature_dev, cfg->top_p_dev, cfg->min_p_dev, cfg->top_k_dev,
                cfg->temperature, cfg->top_p, cfg->min_p, cfg->top_k, token_dev, prob_dev, kept_dev, cfg->vocab};
-    const bool held = cfg->vocab <= kDHeld * kDThreads;
-    const void* f = cfg->dtype == LOOPSPEC_F32    ? held ? (const void*)k_draw<LOOPSPEC_F32, true> : (const void*)k_draw<LOOPSPEC_F32, false>
-                    : cfg->dtype == LOOPSPEC_BF16 ? held ? (const void*)k_draw<LOOPSPEC_BF16, true> : (const void*)k_draw<LOOPSPEC_BF16, false>
-                    : held                        ? (const void*)k_draw<LOOPSPEC_F16, true>
-                                                  : (const void*)k_draw<LOOPSPEC_F16, false>;
-    void* args[] = {&a};
-    return hipLaunchKernel(f, dim3(rows), dim3(kDThreads), args, 0, (hipStream_t)stream) == hipSuccess ? LOOPSPEC_OK : LOOPSPEC_EHIP;
+    if (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < draw_workspace(cfg->vocab, rows, (char*)workspace_dev, &a))
+        return LOOPSPEC_EINVAL;
+    const bool filters = cfg->top_k_dev || cfg->top_p_dev || cfg->min_p_dev || (cfg->top_k > 0 && cfg->top_k < cfg->vocab) ||
+                         cfg->top_p < 1.f || cfg->min_p > 0.f;
+    hipStream_t st = (hipStream_t)stream;
+    if (cfg->dtype == LOOPSPEC_F32) return draw_launch<LOOPSPEC_F32>(a, rows, filters, st);
+    if (cfg->dtype == LOOPSPEC_BF16) return draw_launch<LOOPSPEC_BF16>(a, rows, filters, st);
+    return draw_launch<LOOPSPEC_F16>(a, rows, filters, st);
 }
 
 }  // extern "C"

@@ -198,7 +198,9 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     cfg = B.SampleCfg(vocab, _dtype(logits), *values, *arrays)
     token, kept = torch.empty((2, rows), dtype=torch.int32, device=dev)
     prob = torch.empty(rows, dtype=torch.float32, device=dev)
-    _check(_launch(dev, B.load_library().loopspec_sample, ctypes.byref(cfg), rows, logits.data_ptr(),
-                   logits.stride(0), u.data_ptr(), token.data_ptr(), prob.data_ptr(), kept.data_ptr()),
-           "loopspec_sample")
+    L = B.load_library()
+    nbytes = L.loopspec_sample_workspace_bytes(vocab, rows)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _check(_launch(dev, L.loopspec_sample, ctypes.byref(cfg), rows, logits.data_ptr(), logits.stride(0), u.data_ptr(),
+                   token.data_ptr(), prob.data_ptr(), kept.data_ptr(), ws.data_ptr(), nbytes), "loopspec_sample")
     return token, prob, kept

@@ -76,7 +76,7 @@ def test_bad_append(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(n_heads=0), dict(n_heads=5), dict(scale=0.0), dict(scale=-1.0),
-                                 dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e-45), dict(q=None),
+                                 dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None),
                                  dict(out=None), dict(q=FAKE + 2), dict(q_head=12), dict(out_token=8), dict(out_head=0)],
                          ids=str)
 def test_bad_attention(bad):
@@ -114,17 +114,18 @@ def test_binding_checks_tensors():
         serving.Batch(torch.zeros(3, dtype=torch.int32), torch.zeros((3, 4), dtype=torch.int32))
 
 
-def _sample_rc(rows=4, logits=FAKE, stride=1000, u=FAKE, token=FAKE, **kw):
+def _sample_rc(rows=4, logits=FAKE, stride=1000, u=FAKE, token=FAKE, ws=FAKE, nbytes=1 << 40, **kw):
     c = dict(vocab=1000, dtype=B.F32, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
     c.update(kw)
     cfg = B.SampleCfg(**c)
-    return B.load_library().loopspec_sample(ctypes.byref(cfg), rows, logits, stride, u, token, None, None, None)
+    return B.load_library().loopspec_sample(ctypes.byref(cfg), rows, logits, stride, u, token, None, None, ws,
+                                            nbytes, None)
 
 
 @pytest.mark.parametrize("bad", [dict(vocab=0), dict(vocab=262145), dict(dtype=3), dict(temperature=-0.5),
                                  dict(temperature=float("nan")), dict(temperature=float("inf")), dict(top_p=0.0),
                                  dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1),
-                                 dict(rows=-1), dict(logits=None), dict(logits=FAKE + 2), dict(stride=-1), dict(u=None),
+                                 dict(rows=-1), dict(rows=65536), dict(ws=None), dict(ws=FAKE + 8), dict(nbytes=1000), dict(logits=None), dict(logits=FAKE + 2), dict(stride=-1), dict(u=None),
                                  dict(token=None)], ids=str)
 def test_bad_samples(bad):
     assert _sample_rc(**bad) == B.EINVAL
@@ -132,4 +133,8 @@ def test_bad_samples(bad):
 
 def test_sample_of_no_rows():
     assert _sample_rc(rows=0) == B.OK
-    assert B.load_library().loopspec_sample(None, 1, FAKE, 10, FAKE, FAKE, None, None, None) == B.EINVAL
+    assert B.load_library().loopspec_sample(None, 1, FAKE, 10, FAKE, FAKE, None, None, FAKE, 1 << 40, None) == B.EINVAL
+    L = B.load_library()
+    assert L.loopspec_sample_workspace_bytes(0, 1) == 0 and L.loopspec_sample_workspace_bytes(1000, 0) == 0
+    need = L.loopspec_sample_workspace_bytes(1000, 4)
+    assert need > 0 and _sample_rc(nbytes=need - 1) == B.EINVAL
