@@ -23,12 +23,12 @@
 // row's largest weight), and sums of doubles run in an order that depends on the
 // vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
 //
-// The last kept rank: up to 1024 listed logits, a thread each finds its logit's
-// rank against all others; more of them first go through a histogram of 2048
-// bins of 1/32 octave, and if one of its bins still holds more than 1024, ranges
-// of the logits' order-preserving integer keys are searched the same way down to
-// a single key, whose ties are counted off by id.  A row whose list overflows is
-// searched in place.
+// The last kept rank: a thread each finds its logit's rank against all others.
+// More than 256 listed logits first go through a histogram of 2048 bins of 1/32
+// octave (900 of them took 12 us against each other), and if the bin that it
+// leaves still holds more than 1024, ranges of the logits' order-preserving
+// integer keys are searched the same way down to a single key, whose ties are
+// counted off by id.  A row whose list overflows is searched in place.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -47,13 +47,13 @@ constexpr int kCoarse = 128;                          // bins of half an octave,
 constexpr int kListMax = 8192;                        // listed logits of a row
 constexpr int kDThreads = 1024, kDWaves = kDThreads / 64;
 constexpr int kDBins = 2048;                          // two per thread
-constexpr int kMembers = kDThreads;
+constexpr int kMembers = kDThreads, kDirect = 256;    // logits ranked against each other; those for which that needs no bins
 constexpr int kDMaxVocab = 1 << 18, kShardsMax = kDMaxVocab / kShard;
 static_assert(kShardsMax == 64, "a shard per lane");
 
 struct Head {                                         // of a shard
     double e, grid;                                   // masses are in 2^(e - 44); the largest logit's place on the grid
-    u64 mass;
+    double mass;
     float top;
     int arg, bad;                                     // lowest id of the largest logit; NaN or +infinity met
     unsigned finite;
@@ -210,15 +210,15 @@ __device__ __forceinline__ double wave_max(double v) {
     for (int o = 1; o < 64; o *= 2) v = fmax(v, __shfl_xor(v, o));
     return v;
 }
-// x * 2^n for an integral n, 0 from 2^-300 on
-__device__ __forceinline__ double times2(double x, double n) { return n < -300.0 ? 0.0 : ldexp(x, (int)n); }
+// 2^n for an integral n <= 0, 0 below -300
+__device__ __forceinline__ double power2(double n) { return n < -300.0 ? 0.0 : ldexp(1.0, (int)n); }
 
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     __shared__ u64 mass[kCoarse];
     __shared__ unsigned count[kCoarse];
     __shared__ float wf[4];
-    __shared__ u64 wm[4];
+    __shared__ double wm[4];
     __shared__ unsigned wc[4];
     __shared__ int bad, arg;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, s = blockIdx.x, row = blockIdx.y, id0 = s * kShard;
@@ -243,28 +243,37 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     if (wrong) bad = 1;
     top = fmaxf(fmaxf(wf[0], wf[1]), fmaxf(wf[2], wf[3]));
     const double tt = set.octaves(top), e = top > -INFINITY ? floor(tt) + 1.0 : 0.0, grid = set.grid(top);
-    u64 sum = 0;
     if (set.T > 0.f && top > -INFINITY) {
+        double sum = 0.0;
+        if (set.filters()) {
+            u64 exact = 0;
 #pragma unroll
-        for (int k0 = 0; k0 < kShardEach; k0 += 4) {
-            u64 m[4];
+            for (int k0 = 0; k0 < kShardEach; k0 += 4) {
+                u64 m[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) m[k] = mass44(set.octaves(v[k0 + k]) - e);
+                for (int k = 0; k < 4; ++k) m[k] = mass44(set.octaves(v[k0 + k]) - e);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum += m[k];
-            if (set.filters())
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 4; ++k) {
+                    exact += m[k];
                     if (v[k0 + k] > -INFINITY) {
                         const int b = coarse(grid, set.grid(v[k0 + k]));
                         atomicAdd(&mass[b], m[k]);
                         atomicAdd(&count[b], 1u);
                     }
+                }
+            }
+            sum = (double)exact;
+        } else {
+            // (-infinity weighs 2^-200)
+            double part[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int k = 0; k < kShardEach; ++k) part[k & 3] += weight(set.octaves(v[k]) - e, 44);
+            sum = (part[0] + part[1]) + (part[2] + part[3]);
         }
         sum = wave_sum(sum);
         if (lane == 0) wm[wv] = sum;
     } else {
-        if (lane == 0) wm[wv] = 0;
+        if (lane == 0) wm[wv] = 0.0;
         if (set.T == 0.f) {
             int best = 0x7FFFFFFF;
 #pragma unroll
@@ -277,7 +286,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     const size_t at = (size_t)row * a.S + s;
     if (set.filters() && tid < kCoarse) a.mass[at * kCoarse + tid] = mass[tid], a.count[at * kCoarse + tid] = count[tid];
     if (tid == 0) {
-        a.head[at] = Head{e, grid, wm[0] + wm[1] + wm[2] + wm[3], top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
+        a.head[at] = Head{e, grid, (wm[0] + wm[1]) + (wm[2] + wm[3]), top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
         if (s == 0) a.listed[row] = 0;
     }
 }
@@ -290,7 +299,7 @@ struct Whole {
     Head mine;                                        // lane s: shard s's (nothing in it behind the last one)
     __device__ __forceinline__ Whole(const DrawArgs& a, int row) {
         const int lane = threadIdx.x & 63;
-        mine = Head{-1e300, -INFINITY, 0, -INFINITY, 0x7FFFFFFF, 0, 0};
+        mine = Head{-1e300, -INFINITY, 0.0, -INFINITY, 0x7FFFFFFF, 0, 0};
         if (lane < a.S) mine = a.head[(size_t)row * a.S + lane];
         if (!(mine.top > -INFINITY)) mine.e = -1e300, mine.grid = -INFINITY;
         top = wave_max(mine.top);
@@ -302,7 +311,7 @@ struct Whole {
 
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
-    __shared__ double he[kShardsMax], part_m[2][kCoarse];
+    __shared__ double he[kShardsMax], part_m[2][kCoarse];   // a shard's unit over the row's; halves of the row's bins
     __shared__ int ho[kShardsMax];
     __shared__ unsigned part_c[2][kCoarse];
     __shared__ int range[2];
@@ -316,32 +325,41 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     const size_t row0 = (size_t)row * a.S;
     if (tid < a.S) {
         // (a shard without a finite logit has empty bins, wherever they go)
-        he[tid] = r.mine.e;
+        he[tid] = power2(r.mine.e - r.ref);
         ho[tid] = r.mine.grid > -INFINITY ? coarse(r.grid, r.mine.grid) : 0;
     }
     if (tid == 0) n = 0;
     __syncthreads();
-    // the row's bins: a thread per bin and half of the shards
+    // the row's bins: a thread per bin and half of the shards, 8 of them under way; what the last bin holds
+    // follows from the whole
     {
-        const int b = tid & (kCoarse - 1), h = tid / kCoarse, half = (a.S + 1) / 2;
+        const int b = tid & (kCoarse - 1), h = tid / kCoarse, half = (a.S + 1) / 2, end = min(a.S, (h + 1) * half);
         double m = 0.0;
         unsigned c = 0;
-        for (int k = h * half; k < min(a.S, (h + 1) * half); ++k) {
-            const u64* sm = a.mass + (row0 + k) * kCoarse;
-            const unsigned* sc = a.count + (row0 + k) * kCoarse;
-            const int own = b - ho[k];
-            if (b < kCoarse - 1) {
-                if (own >= 0) m += times2((double)sm[own], he[k] - r.ref), c += sc[own];
-            } else {
-                for (int i = max(own, 0); i < kCoarse; ++i) m += times2((double)sm[i], he[k] - r.ref), c += sc[i];
+        for (int k0 = h * half; k0 < end; k0 += 8) {
+            u64 sm[8];
+            unsigned sc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = min(k0 + i, end - 1);
+                const size_t at = (row0 + k) * kCoarse + max(b - ho[k], 0);
+                sm[i] = a.mass[at], sc[i] = a.count[at];
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k0 + i < end && b >= ho[k0 + i]) m += (double)sm[i] * he[k0 + i], c += sc[i];
         }
-        part_m[h][b] = m, part_c[h][b] = c;
+        part_m[h][b] = b < kCoarse - 1 ? m : 0.0, part_c[h][b] = b < kCoarse - 1 ? c : 0u;
     }
     __syncthreads();
     if (wv == 0) {
-        const double m0 = part_m[0][2 * lane] + part_m[1][2 * lane], m1 = part_m[0][2 * lane + 1] + part_m[1][2 * lane + 1];
-        const unsigned c0 = part_c[0][2 * lane] + part_c[1][2 * lane], c1 = part_c[0][2 * lane + 1] + part_c[1][2 * lane + 1];
+        const double m0 = part_m[0][2 * lane] + part_m[1][2 * lane];
+        double m1 = part_m[0][2 * lane + 1] + part_m[1][2 * lane + 1];
+        const unsigned c0 = part_c[0][2 * lane] + part_c[1][2 * lane];
+        unsigned c1 = part_c[0][2 * lane + 1] + part_c[1][2 * lane + 1];
+        const double all = wave_sum(lane < a.S ? r.mine.mass * he[lane] : 0.0), most = wave_sum(m0 + m1);
+        const unsigned finite = wave_sum(r.mine.finite), counted = wave_sum(c0 + c1);
+        if (lane == 63) m1 = fmax(all - most, 0.0), c1 = finite - counted;
         double sm = m0 + m1;
         unsigned sc = c0 + c1;
 #pragma unroll
@@ -350,7 +368,6 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
             const unsigned y = __shfl_up(sc, o);
             if (lane >= o) sm += x, sc += y;
         }
-        const double all = __shfl(sm, 63);
         const unsigned long long used = __ballot(c0 + c1 > 0);
         const int last_lane = 63 - __clzll(used), last = 2 * last_lane + (__shfl(c1, last_lane) > 0);
         // first bin that meets a condition on (mass through, count through), the last occupied one when none does
@@ -497,6 +514,15 @@ __device__ __forceinline__ void clear_bins(DrawLds& l) {
     __syncthreads();
 }
 
+// l.first and l.last become the smallest `low` and the largest `high` of the
+// workgroup that are not -1; both rise with the thread, so a wave has one say
+__device__ __forceinline__ void note_first_last(DrawLds& l, int low, int high) {
+    const int lane = threadIdx.x & 63;
+    const u64 a = __ballot(low >= 0), b = __ballot(high >= 0);
+    if (a && lane == __ffsll(a) - 1) atomicMin(&l.first, (unsigned)low);
+    if (b && lane == 63 - __clzll(b)) atomicMax(&l.last, (unsigned)high);
+}
+
 // The bin that holds the last kept rank: the first one through which the count
 // reaches `need` (COUNT), or the mass reaches `goal`; the last occupied one when
 // none does.  share > 0: the goal is that share of the bins' whole mass and what
@@ -535,13 +561,14 @@ __device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* go
     if (share > 0.0) *goal = share * (double)(above_m + all);
     const u64 am[2] = {sm, sm + m[0]};                // above each of the thread's bins
     const unsigned ac[2] = {sc, sc + c[0]};
+    int low = -1, high = -1;                          // the thread's first bin that reaches it, its last occupied one
 #pragma unroll
     for (int i = 1; i >= 0; --i) {
         if (COUNT ? !c[i] : !m[i]) continue;
-        const bool reach = goal ? (double)(am[i] + m[i]) >= *goal : ac[i] + c[i] >= need;
-        if (reach) atomicMin(&l.first, (unsigned)(b0 + i));
-        atomicMax(&l.last, (unsigned)(b0 + i));
+        if (goal ? (double)(am[i] + m[i]) >= *goal : ac[i] + c[i] >= need) low = b0 + i;
+        high = max(high, b0 + i);
     }
+    note_first_last(l, low, high);
     __syncthreads();
     const unsigned at = l.first < (unsigned)kDBins ? l.first : l.last;
 #pragma unroll
@@ -586,7 +613,7 @@ __device__ Cut last_kept(const Search<DT>& r, Cut from, unsigned need, double sh
     const int tid = threadIdx.x;
     double* const goalp = BY_COUNT ? nullptr : &goal;
     int picked = -1;                                  // bin of the members; -1: any
-    if (r.n > kMembers || share > 0.0) {
+    if (r.n > kDirect || share > 0.0) {
         clear_bins<!BY_COUNT, BY_COUNT>(l);
         r.each([&](int id, float v) {
             if (!from.keeps(v, id)) return;
@@ -740,7 +767,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid < a.S) {
         double m = 0.0;
         if (w.mine.top > -INFINITY && (!filters || fits))
-            m = (double)(filters ? a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
+            m = (filters ? (double)a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
         l.ws[tid] = m + (double)l.shard[tid];
     }
     const unsigned finite = wave_sum(w.mine.finite);
@@ -779,10 +806,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (lane == 63) l.wd[wv] = upto;
     __syncthreads();
     for (int i = 0; i < wv; ++i) upto += l.wd[i];
-    if (sum > 0.0) {
-        atomicMax(&l.last, (unsigned)tid);
-        if (upto > rest) atomicMin(&l.first, (unsigned)tid);
-    }
+    note_first_last(l, sum > 0.0 && upto > rest ? tid : -1, sum > 0.0 ? tid : -1);
     __syncthreads();
     if (tid == (int)(l.first < (unsigned)kDThreads ? l.first : l.last)) {
         // the first id of the thread's whose mass passes the rest, or its last with any mass
