@@ -23,12 +23,12 @@
 // row's largest weight), and sums of doubles run in an order that depends on the
 // vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
 //
-// The last kept rank: a thread each finds its logit's rank against all others.
-// More than 256 listed logits first go through a histogram of 2048 bins of 1/32
-// octave (900 of them took 12 us against each other), and if the bin that it
-// leaves still holds more than 1024, ranges of the logits' order-preserving
-// integer keys are searched the same way down to a single key, whose ties are
-// counted off by id.  A row whose list overflows is searched in place.
+// The last kept rank: up to 1024 listed logits are sorted, one a thread.  More
+// go through a histogram of 2048 bins of 1/32 octave; if the bin that it leaves
+// holds no more than 1024, a thread each finds its logit's rank against all
+// others, else ranges of the logits' order-preserving integer keys are searched
+// the same way down to a single key, whose ties are counted off by id.  A row
+// whose list overflows is searched in place.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -39,15 +39,15 @@
 namespace ls {
 
 typedef unsigned long long u64;
-typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kShard = 4096, kShardThreads = 256, kShardEach = kShard / kShardThreads;
 constexpr int kCoarse = 128;                          // bins of half an octave, the last one for all below
 constexpr int kListMax = 8192;                        // listed logits of a row
 constexpr int kDThreads = 1024, kDWaves = kDThreads / 64;
 constexpr int kDBins = 2048;                          // two per thread
-constexpr int kMembers = kDThreads, kDirect = 256;    // logits ranked against each other; those for which that needs no bins
+constexpr int kMembers = kDThreads;
 constexpr int kDMaxVocab = 1 << 18, kShardsMax = kDMaxVocab / kShard;
 static_assert(kShardsMax == 64, "a shard per lane");
 
@@ -134,33 +134,52 @@ __device__ __forceinline__ float logit(const void* p, int64_t i) {
     if (DT == LOOPSPEC_F32) return ((const float*)p)[i];
     return half_bits(DT, ((const uint16_t*)p)[i]);
 }
-// four logits from i, one load: 4-byte aligned rows
+// four logits from i, one load of its alignment
 template <int DT>
 __device__ __forceinline__ void load4(const void* p, int64_t i, float* v) {
     if (DT == LOOPSPEC_F32) {
-        const u32x4_a4 u = *(const u32x4_a4*)((const float*)p + i);
+        const u32x4 u = *(const u32x4*)((const float*)p + i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(u[k]);
     } else {
-        const u32x2_a4 u = *(const u32x2_a4*)((const uint16_t*)p + i);
+        const u32x2 u = *(const u32x2*)((const uint16_t*)p + i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = half_bits(DT, k & 1 ? u[k >> 1] >> 16 : u[k >> 1] & 0xFFFFu);
     }
 }
-// logits id0 + 1024 k + 4 t + (0 .. 3) of thread t and k = 0 .. 3, -infinity from V on
+// logits id0 + 1024 k + 4 t + (0 .. 3) of thread t and k = 0 .. 3, -infinity from V on.  Four of them are one
+// aligned load; rows that lie off that alignment (odd vocabularies) pass through LDS, since a shard of
+// unaligned loads took 1.6 times as long.
 template <int DT>
-__device__ __forceinline__ void load_shard(const DrawArgs& a, int64_t base, int id0, float (&v)[kShardEach]) {
-    const int id = id0 + 4 * (int)threadIdx.x;
-    const bool vec = ((uintptr_t)a.z + (uint64_t)base * (DT == LOOPSPEC_F32 ? 4 : 2)) % 4 == 0;
-    if (vec && id0 + kShard <= a.V) {
-#pragma unroll
-        for (int k = 0; k < kShardEach / 4; ++k) load4<DT>(a.z, base + id + 1024 * k, v + 4 * k);
-    } else {
+__device__ __forceinline__ void load_shard(const DrawArgs& a, int64_t base, int id0, float (&v)[kShardEach], float (&l)[kShard + 4]) {
+    const int tid = threadIdx.x, id = id0 + 4 * tid;
+    const int off = (int)(((uintptr_t)a.z / (DT == LOOPSPEC_F32 ? 4 : 2) + (uint64_t)base + id0) % 4);
+    if (id0 + kShard > a.V) {
 #pragma unroll
         for (int k = 0; k < kShardEach; ++k) {
             const int i = id + 1024 * (k / 4) + k % 4;
             v[k] = i < a.V ? logit<DT>(a.z, base + i) : -INFINITY;
         }
+    } else if (off == 0) {
+#pragma unroll
+        for (int k = 0; k < kShardEach / 4; ++k) load4<DT>(a.z, base + id + 1024 * k, v + 4 * k);
+    } else {
+        // place i of l holds id0 - off + i; the vectors that reach over the shard's ends are taken singly
+        float e = 0.f;
+        const int i = tid < 4 - off ? tid : kShard - 2 * 4 + tid;   // 4 - off ids at the front, off at the back
+        if (tid < 4) e = logit<DT>(a.z, base + id0 + i + (tid < 4 - off ? 0 : 4));
+#pragma unroll
+        for (int k = 0; k < kShardEach / 4; ++k)
+            if (k || tid) load4<DT>(a.z, base + id - off + 1024 * k, v + 4 * k);
+        if (tid < 4) l[off + i + (tid < 4 - off ? 0 : 4)] = e;
+#pragma unroll
+        for (int k = 0; k < kShardEach / 4; ++k)
+            if (k || tid)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) l[4 * tid + 1024 * k + m] = v[4 * k + m];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kShardEach; ++k) v[k] = l[off + 4 * tid + 1024 * (k / 4) + k % 4];
     }
 }
 // order-preserving integer of a float that is no NaN; both zeros alike
@@ -215,6 +234,7 @@ __device__ __forceinline__ double power2(double n) { return n < -300.0 ? 0.0 : l
 
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
+    __shared__ float shifted[kShard + 4];
     __shared__ u64 mass[kCoarse];
     __shared__ unsigned count[kCoarse];
     __shared__ float wf[4];
@@ -223,7 +243,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     __shared__ int bad, arg;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, s = blockIdx.x, row = blockIdx.y, id0 = s * kShard;
     float v[kShardEach];
-    load_shard<DT>(a, row * a.stride, id0, v);
+    load_shard<DT>(a, row * a.stride, id0, v, shifted);
     const Setting set(a, row);
     if (tid < kCoarse) mass[tid] = 0, count[tid] = 0;
     if (tid == 0) bad = 0, arg = 0x7FFFFFFF;
@@ -312,6 +332,7 @@ struct Whole {
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     __shared__ double he[kShardsMax], part_m[2][kCoarse];   // a shard's unit over the row's; halves of the row's bins
+    __shared__ float shifted[kShard + 4];
     __shared__ int ho[kShardsMax];
     __shared__ unsigned part_c[2][kCoarse];
     __shared__ int range[2];
@@ -428,7 +449,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     if (tid == 0) a.above[row0 + s] = wm[0] + wm[1];
     if (!any) return;
     float v[kShardEach];
-    load_shard<DT>(a, row * a.stride, s * kShard, v);
+    load_shard<DT>(a, row * a.stride, s * kShard, v, shifted);
     unsigned at[kShardEach];
 #pragma unroll
     for (int k = 0; k < kShardEach; ++k) {
@@ -612,24 +633,21 @@ __device__ Cut last_kept(const Search<DT>& r, Cut from, unsigned need, double sh
     DrawLds& l = r.l;
     const int tid = threadIdx.x;
     double* const goalp = BY_COUNT ? nullptr : &goal;
-    int picked = -1;                                  // bin of the members; -1: any
-    if (r.n > kDirect || share > 0.0) {
-        clear_bins<!BY_COUNT, BY_COUNT>(l);
-        r.each([&](int id, float v) {
-            if (!from.keeps(v, id)) return;
-            if (BY_COUNT)
-                atomicAdd(&l.count[r.bin(v)], 1u);
-            else
-                atomicAdd(&l.mass[r.bin(v)], mass44(r.y(v)));
-        });
-        picked = (int)pick_bin<!BY_COUNT, BY_COUNT>(l, need, share, goalp, above_m, above_c);
-        above_m = l.above_mass, above_c = l.above_cnt;
-    }
+    clear_bins<!BY_COUNT, BY_COUNT>(l);
+    r.each([&](int id, float v) {
+        if (!from.keeps(v, id)) return;
+        if (BY_COUNT)
+            atomicAdd(&l.count[r.bin(v)], 1u);
+        else
+            atomicAdd(&l.mass[r.bin(v)], mass44(r.y(v)));
+    });
+    const int picked = (int)pick_bin<!BY_COUNT, BY_COUNT>(l, need, share, goalp, above_m, above_c);
+    above_m = l.above_mass, above_c = l.above_cnt;
     __syncthreads();
     if (tid == 0) l.listed = 0, l.cnt = 0;
     __syncthreads();
     r.each([&](int id, float v) {
-        if ((picked >= 0 && r.bin(v) != picked) || !from.keeps(v, id)) return;
+        if (r.bin(v) != picked || !from.keeps(v, id)) return;
         const unsigned at = atomicAdd(&l.listed, 1u);
         if (at < (unsigned)kMembers) l.list[at] = Member{v, id, BY_COUNT ? 0 : mass44(r.y(v))};
     });
@@ -709,6 +727,64 @@ __device__ Cut last_kept(const Search<DT>& r, Cut from, unsigned need, double sh
     }
 }
 
+// Up to 1024 listed logits, one a thread, put in the order of their ranks (a
+// bitonic sort of key and id; strides below a wave's width by shuffles) and
+// their masses summed in it: both filters then are places in that order.
+// Returns the last kept rank; e and m are the thread's logit and its mass.
+template <int DT>
+__device__ Cut sorted_cut(const Search<DT>& r, const Setting& set, double all, u64 above_m, unsigned above_c, Entry* e, u64* m) {
+    DrawLds& l = r.l;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    u64 key = ~0ull;
+    if (tid < r.n) {
+        const Entry x = r.list[tid];
+        key = (u64)~order_key(x.v) << 32 | (unsigned)x.id;
+    }
+    for (int k = 2; k / 2 < r.n; k *= 2)
+        for (int j = k / 2; j; j /= 2) {
+            u64 o;
+            if (j < 64) {
+                o = __shfl_xor(key, j);
+            } else {
+                __syncthreads();
+                l.mass[tid] = key;
+                __syncthreads();
+                o = l.mass[tid ^ j];
+            }
+            if ((o < key) == (((tid & j) == 0) == ((tid & k) == 0))) key = o;
+        }
+    const uint32_t h = ~(uint32_t)(key >> 32);
+    const bool in = tid < r.n;
+    e->v = in ? __uint_as_float(h & 0x80000000u ? h & 0x7FFFFFFFu : ~h) : -INFINITY;
+    e->id = (int)(unsigned)key;
+    *m = in ? mass44(r.y(e->v)) : 0;
+    u64 upto = *m;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const u64 x = __shfl_up(upto, o);
+        if (lane >= o) upto += x;
+    }
+    __syncthreads();
+    if (lane == 63) l.wm[wv] = upto;
+    if (tid == 0) l.above_mass = 0;
+    __syncthreads();
+    upto += above_m;
+    for (int i = 0; i < wv; ++i) upto += l.wm[i];
+    const unsigned rank = above_c + tid;
+    auto in_k = [&](unsigned x) { return !set.by_k || x < (unsigned)set.top_k; };
+    if (in && in_k(rank) && (tid == r.n - 1 || !in_k(rank + 1))) l.above_mass = upto;
+    __syncthreads();
+    const double goal = (double)set.top_p * (set.by_k ? (double)l.above_mass : all);
+    // (the first listed rank is kept whatever the roundings of sums above it)
+    auto in_p = [&](u64 before) { return !set.by_p || (double)before < goal; };
+    const bool kept = in && (tid == 0 || (in_k(rank) && in_p(upto - *m)));
+    if (kept && (tid == r.n - 1 || !in_k(rank + 1) || !in_p(upto))) l.cut_f = e->v, l.cut_id = e->id;
+    __syncthreads();
+    Cut c;
+    c.f = l.cut_f, c.id = l.cut_id;
+    return c;
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     __shared__ DrawLds l;
@@ -745,20 +821,31 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
         u64 above_m = (u64)rint(plan.above_m * unit);
         above_c = plan.above_c;
         if (!fits) above_m = 0, above_c = 0, plan.rank = set.by_k || set.by_p;
-        if (plan.rank && set.by_k) cut = last_kept<true>(r, cut, (unsigned)set.top_k, 0.0, 0.0, above_m, above_c);
-        if (plan.rank && set.by_p) {
-            // (the list alone holds what top-k kept; without top-k the row's mass is known)
-            const bool whole = fits && !set.by_k;
-            cut = last_kept<false>(r, cut, 0u, whole ? 0.0 : (double)set.top_p, whole ? (double)set.top_p * (plan.all * unit) : 0.0, above_m, above_c);
-        }
+        auto count = [&](int id, float v, u64 m) -> unsigned {
+            if (!cut.keeps(v, id) || weight(r.y(v)) < (double)set.min_p) return 0u;
+            atomicAdd(&l.shard[id / kShard], m);
+            return 1u;
+        };
         unsigned n = 0;
-        r.each([&](int id, float v) {
-            if (!cut.keeps(v, id)) return;
-            const double y = r.y(v);
-            if (weight(y) < (double)set.min_p) return;
-            atomicAdd(&l.shard[id / kShard], mass44(y));
-            ++n;
-        });
+        if (fits && listed <= (unsigned)kMembers) {
+            Entry e{-INFINITY, 0};
+            u64 m = 0;
+            if (plan.rank) {
+                cut = sorted_cut(r, set, plan.all * unit, above_m, above_c, &e, &m);
+            } else if (tid < r.n) {
+                e = r.list[tid];
+                m = mass44(r.y(e.v));
+            }
+            if (e.v > -INFINITY) n = count(e.id, e.v, m);
+        } else {
+            if (plan.rank && set.by_k) cut = last_kept<true>(r, cut, (unsigned)set.top_k, 0.0, 0.0, above_m, above_c);
+            if (plan.rank && set.by_p) {
+                // (without top-k the row's mass is known; the list alone holds what top-k kept)
+                const bool whole = fits && !set.by_k;
+                cut = last_kept<false>(r, cut, 0u, whole ? 0.0 : (double)set.top_p, whole ? (double)set.top_p * (plan.all * unit) : 0.0, above_m, above_c);
+            }
+            r.each([&](int id, float v) { n += count(id, v, mass44(r.y(v))); });
+        }
         n = wave_sum(n);
         if (lane == 0 && n) atomicAdd(&l.kept, n);
         __syncthreads();
@@ -774,19 +861,19 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid == 0) l.first = kDThreads, l.last = 0;
     __syncthreads();
     const unsigned kept = filters ? above_c + l.kept : finite;
-    double all = 0.0;
-    for (int i = 0; i < a.S; ++i) all += l.ws[i];
-    // the shard that holds the token (sums may round up to the goal: then the last one with any mass)
-    const double goal = a.u[row] * all;
-    double before = 0.0, rest = 0.0;
-    int run = 0;
-    bool found = false;
-    for (int i = 0; i < a.S; ++i) {
-        const double m = l.ws[i];
-        if (m > 0.0 && (!found || before <= goal)) run = i, rest = goal - before, found = true;
-        if (m > 0.0 && before + m > goal) break;
-        before += m;
+    // the shard that holds the token, found by every wave (sums may round up to the goal: then the last one
+    // with any mass)
+    const double here = lane < a.S ? l.ws[lane] : 0.0;
+    double through = here;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const double x = __shfl_up(through, o);
+        if (lane >= o) through += x;
     }
+    const double all = __shfl(through, 63), goal = a.u[row] * all;
+    const u64 past = __ballot(here > 0.0 && through > goal), some = __ballot(here > 0.0);
+    const int run = past ? __ffsll(past) - 1 : 63 - __clzll(some);
+    const double rest = goal - __shfl(through - here, run);
     // its ids in order, four a thread
     double own[4], sum = 0.0;
     const int id0 = run * kShard + 4 * tid;
