@@ -586,9 +586,8 @@ typedef struct {
  * is the smallest id whose kept weight through it exceeds u * kept weight.
  * Logits of -infinity are never kept.  token_dev[i]: the token; prob_dev[i] (may
  * be NULL): its share of the kept weight; kept_dev[i] (may be NULL): how many
- * ids were kept.  Weights are 64-bit, sums exact in units of 2^-44 of the
- * largest weight, so the draw does not depend on the order of adding; a weight
- * below half a unit is kept and counted but not drawn.
+ * ids were kept.  Weights are 64-bit (off by 2^-38) and sums do not depend on
+ * the order of adding, so a row's draw is repeatable and its own.
  * A row with a NaN or +infinity among its logits, without a finite one, or whose
  * settings or number are outside their ranges gives token -1, prob 0, kept 0.
  * rows: up to 65535.  workspace: 16-byte aligned, its contents on entry do not
@@ -599,7 +598,7 @@ int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* lo
                     uint64_t workspace_bytes, void* stream);
 
 /* Bytes of device workspace loopspec_sample needs (0 for sizes it refuses):
- * about 64 KiB a row and 1.6 KiB per 4096 ids of it. */
+ * about 64 KiB a row and 1.1 KiB per 4096 ids of it. */
 uint64_t loopspec_sample_workspace_bytes(int32_t vocab, int32_t rows);
 
 /* Library version string. */

@@ -17,11 +17,12 @@
 //   k_draw_pick   a workgroup per row: the last kept rank on the list, the shard that holds the token, the token
 //
 // A token is decided by comparing sums with u times a sum, so weights are taken
-// in 64 bits (2^f by a polynomial on [-1/2, 1/2], off by 2^-50) and sums have to
-// be the same whatever the order of adding: masses are integers in units of
-// 2^-44 (of a power of two at or above the shard's largest weight, or of the
-// row's largest weight), and sums of doubles run in an order that depends on the
-// vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
+// in 64 bits (2^f by a polynomial on [-1/2, 1/2], off by 2^-38.8: each two degrees
+// more are a tenth of a large batch's time) and sums have to
+// be the same whatever the order of adding: what atomics add are integers, in
+// units of 2^-38 (in a bin, of a power of two above the shard's largest weight) or
+// 2^-44 (of the row's largest weight), and sums of doubles run in an order that
+// depends on the vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
 //
 // The last kept rank: up to 1024 listed logits are sorted, one a thread.  More
 // go through a histogram of 2048 bins of 1/32 octave; if the bin that it leaves
@@ -83,9 +84,8 @@ struct DrawArgs {
     int V, S;
     // workspace
     Head* head;                                       // [rows][S]
-    u64* mass;                                        // [rows][S][kCoarse]
-    unsigned* count;                                  // [rows][S][kCoarse]
-    u64* above;                                       // [rows][S]: the shard's mass above the listed bins
+    u64* bins;                                        // [rows][S][kCoarse]
+    u64* above;                                       // [rows][S]: the shard's mass above the listed bins, in 2^(e - 38)
     RowPlan* plan;                                    // [rows]
     Entry* list;                                      // [rows][kListMax]
     unsigned* listed;                                 // [rows]
@@ -195,16 +195,14 @@ __device__ __forceinline__ double weight(double y, int up = 0) {
     constexpr double M = 6755399441055744.0;
     y = fmax(y, -200.0);
     const double t = y + M, f = y - (t - M);
-    double p = 7.070977866508138e-09;
-    p = fma(p, f, 1.0205905413765595e-07);
-    p = fma(p, f, 1.3215451633221434e-06);
-    p = fma(p, f, 1.5252672924850737e-05);
-    p = fma(p, f, 0.00015403530424776529);
-    p = fma(p, f, 0.0013333558200794592);
-    p = fma(p, f, 0.009618129107618665);
-    p = fma(p, f, 0.05550410866465167);
-    p = fma(p, f, 0.24022650695910075);
-    p = fma(p, f, 0.6931471805599462);
+    double p = 1.325080551750225e-06;
+    p = fma(p, f, 1.5303700711365693e-05);
+    p = fma(p, f, 0.00015403475186530786);
+    p = fma(p, f, 0.0013333478473685416);
+    p = fma(p, f, 0.00961812913523614);
+    p = fma(p, f, 0.055504109063258665);
+    p = fma(p, f, 0.24022650695888503);
+    p = fma(p, f, 0.6931471805568324);
     p = fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + ((__double2loint(t) + up) << 20), __double2loint(p));
 }
@@ -212,6 +210,12 @@ __device__ __forceinline__ double weight(double y, int up = 0) {
 __device__ __forceinline__ u64 mass44(double y) {
     return (u64)__double_as_longlong(weight(y, 44) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
+
+// a bin: how many logits (from bit 51) and their mass in units of 2^-38, which 4096 of them keep below bit 51
+__device__ __forceinline__ u64 binned(double y) {
+    return (u64)__double_as_longlong(weight(y, 38) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+}
+constexpr u64 kOne = 1ull << 51, kMassBits = kOne - 1;
 
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v) {
@@ -235,8 +239,7 @@ __device__ __forceinline__ double power2(double n) { return n < -300.0 ? 0.0 : l
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     __shared__ float shifted[kShard + 4];
-    __shared__ u64 mass[kCoarse];
-    __shared__ unsigned count[kCoarse];
+    __shared__ u64 bins[kCoarse];
     __shared__ float wf[4];
     __shared__ double wm[4];
     __shared__ unsigned wc[4];
@@ -245,7 +248,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     float v[kShardEach];
     load_shard<DT>(a, row * a.stride, id0, v, shifted);
     const Setting set(a, row);
-    if (tid < kCoarse) mass[tid] = 0, count[tid] = 0;
+    if (tid < kCoarse) bins[tid] = 0;
     if (tid == 0) bad = 0, arg = 0x7FFFFFFF;
     float top = -INFINITY;
     bool wrong = false;
@@ -271,18 +274,15 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
             for (int k0 = 0; k0 < kShardEach; k0 += 4) {
                 u64 m[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) m[k] = mass44(set.octaves(v[k0 + k]) - e);
+                for (int k = 0; k < 4; ++k) m[k] = binned(set.octaves(v[k0 + k]) - e);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    exact += m[k];
+                for (int k = 0; k < 4; ++k)
                     if (v[k0 + k] > -INFINITY) {
-                        const int b = coarse(grid, set.grid(v[k0 + k]));
-                        atomicAdd(&mass[b], m[k]);
-                        atomicAdd(&count[b], 1u);
+                        exact += m[k];
+                        atomicAdd(&bins[coarse(grid, set.grid(v[k0 + k]))], m[k] + kOne);
                     }
-                }
             }
-            sum = (double)exact;
+            sum = (double)exact * 64.0;
         } else {
             // (-infinity weighs 2^-200)
             double part[4] = {0.0, 0.0, 0.0, 0.0};
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     }
     __syncthreads();
     const size_t at = (size_t)row * a.S + s;
-    if (set.filters() && tid < kCoarse) a.mass[at * kCoarse + tid] = mass[tid], a.count[at * kCoarse + tid] = count[tid];
+    if (set.filters() && tid < kCoarse) a.bins[at * kCoarse + tid] = bins[tid];
     if (tid == 0) {
         a.head[at] = Head{e, grid, (wm[0] + wm[1]) + (wm[2] + wm[3]), top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
         if (s == 0) a.listed[row] = 0;
@@ -358,17 +358,15 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
         double m = 0.0;
         unsigned c = 0;
         for (int k0 = h * half; k0 < end; k0 += 8) {
-            u64 sm[8];
-            unsigned sc[8];
+            u64 x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int k = min(k0 + i, end - 1);
-                const size_t at = (row0 + k) * kCoarse + max(b - ho[k], 0);
-                sm[i] = a.mass[at], sc[i] = a.count[at];
+                x[i] = a.bins[(row0 + k) * kCoarse + max(b - ho[k], 0)];
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k0 + i < end && b >= ho[k0 + i]) m += (double)sm[i] * he[k0 + i], c += sc[i];
+                if (k0 + i < end && b >= ho[k0 + i]) m += (double)(x[i] & kMassBits) * (64.0 * he[k0 + i]), c += (unsigned)(x[i] / kOne);
         }
         part_m[h][b] = b < kCoarse - 1 ? m : 0.0, part_c[h][b] = b < kCoarse - 1 ? c : 0u;
     }
@@ -440,8 +438,9 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     bool some = false;
     if (tid < kCoarse) {
         const int b = min(ho[s] + tid, kCoarse - 1);
-        if (b < lo) above = a.mass[(row0 + s) * kCoarse + tid];
-        some = b >= lo && b <= hi && a.count[(row0 + s) * kCoarse + tid] > 0;
+        const u64 x = a.bins[(row0 + s) * kCoarse + tid];
+        if (b < lo) above = x & kMassBits;
+        some = b >= lo && b <= hi && x >= kOne;
     }
     above = wave_sum(above);
     if (lane == 0) wm[wv] = above;
@@ -854,7 +853,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid < a.S) {
         double m = 0.0;
         if (w.mine.top > -INFINITY && (!filters || fits))
-            m = (filters ? (double)a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
+            m = (filters ? 64.0 * (double)a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
         l.ws[tid] = m + (double)l.shard[tid];
     }
     const unsigned finite = wave_sum(w.mine.finite);
@@ -926,8 +925,7 @@ uint64_t draw_workspace(int V, int64_t rows, char* p, DrawArgs* a) {
     };
     a->S = (int)S;
     a->head = (Head*)take(rows * S * sizeof(Head));
-    a->mass = (u64*)take(rows * S * kCoarse * 8);
-    a->count = (unsigned*)take(rows * S * kCoarse * 4);
+    a->bins = (u64*)take(rows * S * kCoarse * 8);
     a->above = (u64*)take(rows * S * 8);
     a->plan = (RowPlan*)take(rows * sizeof(RowPlan));
     a->list = (Entry*)take(rows * kListMax * sizeof(Entry));
