@@ -18,11 +18,11 @@
 //
 // A token is decided by comparing sums with u times a sum, so weights are taken
 // in 64 bits (2^f by a polynomial on [-1/2, 1/2], off by 2^-38.8: each two degrees
-// more are a tenth of a large batch's time) and sums have to
-// be the same whatever the order of adding: what atomics add are integers, in
-// units of 2^-38 (in a bin, of a power of two above the shard's largest weight) or
-// 2^-44 (of the row's largest weight), and sums of doubles run in an order that
-// depends on the vocabulary alone.  Bins lie on a grid of z log2(e) / T that all shards share.
+// more are a tenth of a large batch's time) and sums have to be the same whatever
+// the order of adding: what atomics add are integers, in units of 2^-38 of a power
+// of two at a bin's upper end, or 2^-44 of the row's largest weight, and sums of
+// doubles run in an order that depends on the vocabulary alone.  Bins lie on a
+// grid of z log2(e) / T that all shards share.
 //
 // The last kept rank: up to 1024 listed logits are sorted, one a thread.  More
 // go through a histogram of 2048 bins of 1/32 octave; if the bin that it leaves
@@ -85,7 +85,7 @@ struct DrawArgs {
     // workspace
     Head* head;                                       // [rows][S]
     u64* bins;                                        // [rows][S][kCoarse]
-    u64* above;                                       // [rows][S]: the shard's mass above the listed bins, in 2^(e - 38)
+    double* above;                                    // [rows][S]: the shard's mass above the listed bins, in 2^(e - 44)
     RowPlan* plan;                                    // [rows]
     Entry* list;                                      // [rows][kListMax]
     unsigned* listed;                                 // [rows]
@@ -211,11 +211,15 @@ __device__ __forceinline__ u64 mass44(double y) {
     return (u64)__double_as_longlong(weight(y, 44) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
-// a bin: how many logits (from bit 51) and their mass in units of 2^-38, which 4096 of them keep below bit 51
-__device__ __forceinline__ u64 binned(double y) {
-    return (u64)__double_as_longlong(weight(y, 38) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+// A bin: how many logits (from bit 51) and their mass in units of 2^-38 of
+// 2^-(b / 2), which no weight of bin b exceeds: each is off by 2^-37 of itself at
+// most, however far down, and 4096 of them stay below bit 51.
+constexpr u64 kOne = 1ull << 51;
+__device__ __forceinline__ u64 binned(double y, int b) {
+    return kOne + ((u64)__double_as_longlong(weight(y, 38 + b / 2) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull);
 }
-constexpr u64 kOne = 1ull << 51, kMassBits = kOne - 1;
+// its mass in 2^-44
+__device__ __forceinline__ double bin_mass(u64 x, int b) { return (double)(x & (kOne - 1)) * __hiloint2double((1029 - b / 2) << 20, 0); }
 
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v) {
@@ -269,20 +273,21 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     if (set.T > 0.f && top > -INFINITY) {
         double sum = 0.0;
         if (set.filters()) {
-            u64 exact = 0;
 #pragma unroll
             for (int k0 = 0; k0 < kShardEach; k0 += 4) {
                 u64 m[4];
+                int b[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) m[k] = binned(set.octaves(v[k0 + k]) - e);
+                for (int k = 0; k < 4; ++k) {
+                    b[k] = coarse(grid, set.grid(v[k0 + k]));
+                    m[k] = binned(set.octaves(v[k0 + k]) - e, b[k]);
+                }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (v[k0 + k] > -INFINITY) {
-                        exact += m[k];
-                        atomicAdd(&bins[coarse(grid, set.grid(v[k0 + k]))], m[k] + kOne);
-                    }
+                    if (v[k0 + k] > -INFINITY) atomicAdd(&bins[b[k]], m[k]);
             }
-            sum = (double)exact * 64.0;
+            __syncthreads();
+            if (tid < kCoarse) sum = bin_mass(bins[tid], tid);
         } else {
             // (-infinity weighs 2^-200)
             double part[4] = {0.0, 0.0, 0.0, 0.0};
@@ -336,7 +341,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     __shared__ int ho[kShardsMax];
     __shared__ unsigned part_c[2][kCoarse];
     __shared__ int range[2];
-    __shared__ u64 wm[4];
+    __shared__ double wm[4];
     __shared__ unsigned n, base;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, s = blockIdx.x, row = blockIdx.y;
     const Setting set(a, row);
@@ -366,7 +371,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k0 + i < end && b >= ho[k0 + i]) m += (double)(x[i] & kMassBits) * (64.0 * he[k0 + i]), c += (unsigned)(x[i] / kOne);
+                if (k0 + i < end && b >= ho[k0 + i]) m += bin_mass(x[i], b - ho[k0 + i]) * he[k0 + i], c += (unsigned)(x[i] / kOne);
         }
         part_m[h][b] = b < kCoarse - 1 ? m : 0.0, part_c[h][b] = b < kCoarse - 1 ? c : 0u;
     }
@@ -434,12 +439,12 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     __syncthreads();
     const int lo = range[0], hi = range[1];
     // this shard: its mass above the listed bins, its members in them
-    u64 above = 0;
+    double above = 0.0;
     bool some = false;
     if (tid < kCoarse) {
         const int b = min(ho[s] + tid, kCoarse - 1);
         const u64 x = a.bins[(row0 + s) * kCoarse + tid];
-        if (b < lo) above = x & kMassBits;
+        if (b < lo) above = bin_mass(x, tid);
         some = b >= lo && b <= hi && x >= kOne;
     }
     above = wave_sum(above);
@@ -853,7 +858,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid < a.S) {
         double m = 0.0;
         if (w.mine.top > -INFINITY && (!filters || fits))
-            m = (filters ? 64.0 * (double)a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
+            m = (filters ? a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
         l.ws[tid] = m + (double)l.shard[tid];
     }
     const unsigned finite = wave_sum(w.mine.finite);
@@ -926,7 +931,7 @@ uint64_t draw_workspace(int V, int64_t rows, char* p, DrawArgs* a) {
     a->S = (int)S;
     a->head = (Head*)take(rows * S * sizeof(Head));
     a->bins = (u64*)take(rows * S * kCoarse * 8);
-    a->above = (u64*)take(rows * S * 8);
+    a->above = (double*)take(rows * S * 8);
     a->plan = (RowPlan*)take(rows * sizeof(RowPlan));
     a->list = (Entry*)take(rows * kListMax * sizeof(Entry));
     a->listed = (unsigned*)take(rows * 4);

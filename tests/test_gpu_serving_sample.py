@@ -1,5 +1,7 @@
 """Draws from logits on the GPU against a plain 64-bit implementation, row by row: tokens and kept counts equal,
 probabilities within fp32's rounding."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -35,9 +37,9 @@ def draw(z, u, t, k, p, m):
 
 
 def check(z, u, t, k, p, m):
-    """Runs the batch and compares every row.  Masses are integers of 2^-44 of the largest weight (off by at most
-    2^-45 each, V <= 2^18 of them: 2^-27 of the largest weight), so a probability is off by 2^-26 and fp32's half
-    step."""
+    """Runs the batch and compares every row.  A weight is off by 2^-38.8 of itself, in a bin's sum by 2^-37 more, in
+    the list's by 2^-45 of the row's largest weight, of which there are at most V <= 2^18: sums are off by 2^-27 of
+    themselves (none is smaller than the largest weight), a probability by 2^-26 and fp32's half step."""
     from paper_2609_17184_amd import serving
     rows = len(z)
 
@@ -109,6 +111,25 @@ def test_wide_spread_and_odd_values():
     for t, k, p, m in [(1.0, 3000, 1.0, 0.0), (1.0, 0, 0.7, 0.0), (1.0, 7000, 0.5, 0.0), (1e-30, 100, 1.0, 0.0),
                        (1e30, 4000, 0.9, 0.0), (1e-42, 0, 0.9, 0.0)]:
         check(torch.tensor(z), rng.random(len(z)), t, k, p, m)
+
+
+@pytest.mark.parametrize("low", [-24.3, -27.7, -29.9, -40.0])
+def test_flat_tail(low):
+    """One logit and a vocabulary of equal ones far below, whose mass only counts together: the kept mass is top_p's
+    within 2^-26 of the whole (sums are off by 2^-27), and no tie more than that."""
+    from paper_2609_17184_amd import serving
+    V = 262144
+    p = np.float32(1 - 2.0 ** -24)
+    z = torch.full((2, V), low)
+    z[:, 100000] = 0.0
+    w = math.exp(low)
+    whole = 1 + (V - 1) * w
+    token, prob, kept = serving.sample(z.to(DEV), torch.tensor([0.5, 0.9], dtype=torch.float64, device=DEV), 1.0, 0, float(p))
+    assert token.tolist() == [100000] * 2
+    for k, pr in zip(kept.tolist(), prob.tolist()):
+        mass, before = 1 + (k - 1) * w, 1 + (k - 2) * w if k > 1 else 0.0     # with and without the last kept rank
+        assert mass >= (float(p) - 2.0 ** -26) * whole and before < (float(p) + 2.0 ** -26) * whole
+        assert abs(pr - 1 / mass) <= 2.0 ** -26 + 2.0 ** -24
 
 
 def test_masked_rows():
