@@ -48,7 +48,7 @@ def _ints(t, shape, device, what: str):
 def _launch(device, call, *args) -> int:
     """One call of the library on the device's current stream."""
     import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
+    stream = torch._C._cuda_getCurrentRawStream(device.index)   # torch.cuda.current_stream without its object, 2 us
     if torch.cuda.current_device() == device.index:
         return call(*args, stream)
     with torch.cuda.device(device):
@@ -92,12 +92,13 @@ class Batch:
                                 _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table"),
                                 table.stride(0), table.shape[1], self.prefix_len,
                                 None if prefix_table is None else _ints(prefix_table, (None,), dev, "prefix_table"))
-        self._ref = ctypes.byref(self._c)
 
     def _with(self, tokens: int, cache: PagedCache):
-        _need(self.device == cache.device, "batch and cache: on one device")
-        self._c.n_tokens = tokens
-        return self._ref
+        if self.device != cache.device:
+            raise ValueError("batch and cache: on one device")
+        c = B.PagedBatchC.from_buffer_copy(self._c)      # a call's own: threads may share the batch
+        c.n_tokens = tokens
+        return ctypes.byref(c)
 
 
 def rope_frequencies(rot_dim: int, base: float = 1e4, device="cuda:0"):
@@ -106,10 +107,24 @@ def rope_frequencies(rot_dim: int, base: float = 1e4, device="cuda:0"):
     return base ** (-torch.arange(rot_dim // 2, dtype=torch.float64, device=device) * 2 / rot_dim)
 
 
-def _rows(t, heads: Optional[int], cache: PagedCache, tokens: Optional[int], what: str):
-    _need(t.dim() == 3 and t.shape[2] == cache.head_dim and (heads is None or t.shape[1] == heads)
-          and (tokens is None or t.shape[0] == tokens) and t.dtype == cache.dtype and t.device == cache.device
-          and t.stride(2) == 1, f"{what}: [tokens, heads, head_dim] of the cache's type and device, elements adjacent")
+def _rows(t, heads: int, cache: PagedCache, tokens: int, what: str):
+    if not (t.shape == (tokens, heads, cache.head_dim) and t.dtype is cache.dtype and t.device == cache.device
+            and t.stride(2) == 1):
+        raise ValueError(f"{what}: [tokens, heads, head_dim] of the cache's type and device, elements adjacent")
+
+
+def _heads(q, cache: PagedCache):
+    """(tokens, heads) of the queries."""
+    if q.dim() != 3:
+        raise ValueError("q: [tokens, heads, head_dim]")
+    tokens, heads, _ = q.shape
+    _rows(q, heads, cache, tokens, "q")
+    return tokens, heads
+
+
+def _like(q):
+    import torch
+    return torch.empty_like(q, memory_format=torch.contiguous_format)
 
 
 def rope_append(q, k, v, cache: PagedCache, batch: Batch, freq=None, q_norm=None, k_norm=None, eps: float = 1e-6,
@@ -120,23 +135,23 @@ def rope_append(q, k, v, cache: PagedCache, batch: Batch, freq=None, q_norm=None
     (None: no rotation), the first rot_dim elements of a head being rotated in halves.  Returns the queries: `out`
     (which may be q) or a new tensor, whose padding rows are then undefined."""
     import torch
-    tokens = q.shape[0]
-    _rows(q, None, cache, tokens, "q")
+    tokens, heads = _heads(q, cache)
     _rows(k, cache.n_kv_heads, cache, tokens, "k")
     _rows(v, cache.n_kv_heads, cache, tokens, "v")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _like(q)
     else:
-        _rows(out, q.shape[1], cache, tokens, "out")
+        _rows(out, heads, cache, tokens, "out")
     rot = 0
     if freq is not None:
         _need(freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous() and freq.device == cache.device,
               "freq: float64 [rot_dim / 2] on the cache's device")
         rot = 2 * freq.shape[0]
     for g in (q_norm, k_norm):
-        _need(g is None or (g.dtype == torch.float32 and g.shape == (cache.head_dim,) and g.is_contiguous()
-                            and g.device == cache.device), "q_norm, k_norm: float32 [head_dim] on the cache's device")
-    a = B.RopeArgs(q.shape[1], rot, eps, q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1),
+        if g is not None:
+            _need(g.dtype == torch.float32 and g.shape == (cache.head_dim,) and g.is_contiguous()
+                  and g.device == cache.device, "q_norm, k_norm: float32 [head_dim] on the cache's device")
+    a = B.RopeArgs(heads, rot, eps, q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1),
                    k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
                    None if freq is None else freq.data_ptr(), None if q_norm is None else q_norm.data_ptr(),
                    None if k_norm is None else k_norm.data_ptr())
@@ -152,10 +167,9 @@ def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] 
     tensor whose padding rows are undefined), with return_lse also the log of each row's sum of exp(score) (float32
     [tokens, n_heads])."""
     import torch
-    _rows(q, None, cache, None, "q")
-    tokens, heads = q.shape[0], q.shape[1]
+    tokens, heads = _heads(q, cache)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _like(q)
     else:
         _rows(out, heads, cache, tokens, "out")
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
@@ -196,8 +210,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
             values.append(x)
             arrays.append(None)
     cfg = B.SampleCfg(vocab, _dtype(logits), *values, *arrays)
-    token, kept = torch.empty((2, rows), dtype=torch.int32, device=dev)
-    prob = torch.empty(rows, dtype=torch.float32, device=dev)
+    token = torch.empty((rows,), dtype=torch.int32, device=dev)
+    kept, prob = torch.empty_like(token), torch.empty_like(token, dtype=torch.float32)
     L = B.load_library()
     nbytes = L.loopspec_sample_workspace_bytes(vocab, rows)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)

@@ -210,6 +210,35 @@ def test_attention_hidden_values_have_no_influence(bad):
         assert out[3:6].isnan().all()
 
 
+@pytest.mark.parametrize("tokens", [4, 5, 8, 9, 16, 17, 31, 33, 64])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_row_counts(tokens, D):
+    """Rows of a head's queries on either side of every block size, one token per sequence and all in one."""
+    from paper_2609_17184_amd import serving
+    for new, lens in (([1] * tokens, [1 + 7 * i for i in range(tokens)]), ([tokens], [tokens + 150])):
+        c = Case(8, 2, D, 16, "f16", new, lens, 333, seed=tokens)
+        out, lse = serving.prefix_attention(c.q.to(DEV), c.cache, c.batch, return_lse=True)
+        check_attention(c, D ** -0.5, out, lse, out.cpu())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_attention_long_prompt_hides_its_end(bad):
+    """Blocks of many rows of one sequence, in which some rows see what others must not."""
+    from paper_2609_17184_amd import serving
+    c = Case(4, 2, 128, 32, "bf16", [70, 40], [200, 40], 100, seed=12)
+    q = c.q.to(DEV)
+    ref, rlse = serving.prefix_attention(q, c.cache, c.batch, return_lse=True)
+    check_attention(c, 128 ** -0.5, ref, rlse, ref.cpu())
+    for t in (c.kd, c.vd):
+        for b, first, n in ((0, 150, 200), (1, 20, 40)):
+            for place in range(first, n):
+                t[c.tables[b][place // 32], :, place % 32] = bad
+    out, lse = serving.prefix_attention(q, c.cache, c.batch, return_lse=True)
+    see = list(range(20)) + list(range(70, 90))
+    err = (out[see].double() - ref[see].double()).abs().max().item()
+    assert err <= half(c.dtype) * ref[see].abs().max().item() and torch.equal(lse[see], rlse[see])
+
+
 def test_attention_pages_outside_the_cache_make_nan():
     """A visible page that is none of the cache's, or that the table does not hold: NaN for the rows that see it."""
     from paper_2609_17184_amd import serving
