@@ -496,7 +496,7 @@ typedef struct {
  * is. */
 typedef struct {
     int32_t n_seqs;
-    int32_t n_tokens;               /* rows of the queries */
+    int32_t n_tokens;               /* rows of the queries, up to 2^25 */
     const int32_t* q_start_dev;     /* [n_seqs + 1] ascending; NULL: token b is sequence b's only one */
     const int32_t* seq_len_dev;     /* [n_seqs] own positions, with this step's tokens */
     const int32_t* table_dev;       /* [n_seqs][table_stride], table_width of each row in use */

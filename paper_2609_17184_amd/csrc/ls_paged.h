@@ -9,6 +9,7 @@ namespace ls {
 constexpr int kPageUnit = 16;                 // a page holds a multiple of 16 positions
 constexpr int kPageMax = 1024;
 constexpr int64_t kPlacesMax = 1ll << 28;     // positions a page table may span
+constexpr int kTokensMax = 1 << 25;           // 2^23 workgroups of 4 tokens: a grid holds 2^32 threads
 constexpr int64_t kStrideMax = 1ll << 24;     // elements between neighbouring positions or heads
 
 struct PagedCache {

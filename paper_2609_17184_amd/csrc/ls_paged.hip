@@ -14,7 +14,15 @@
 // holds elements [8c, 8c + 8) and their partners [rot/2 + 8c, ...) of the
 // rotated part, or 16 consecutive elements behind it, and both come and go as
 // 16-byte accesses.  The norm's sum crosses the group by DPP moves.
+//
+// Bound by memory: 3340 tokens of 55 query and 55 key and value heads of 96 (fp16,
+// no norm, 212 MB) take 47 us, 4.5 TB/s; 16001 tokens of 28 query and 4 key and
+// value heads of 128 (bf16, norms, half of a head rotated, 295 MB) take 60 us,
+// 4.9 TB/s, which is what a large copy reaches.  One token takes 3 us, a launch
+// and the loads that wait for each other (lengths, then pages).
 #include "ls_paged.h"
+
+#include <algorithm>
 
 namespace ls {
 
@@ -52,97 +60,97 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
     return u;
 }
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 256, kRopeTokens = 4;
 
-// Workgroup (x, y): tokens x, x + gridDim.x, ...; of each token the heads that
-// fall to slice y of gridDim.y.  Items of a token: H query heads, G key heads,
-// G value heads.
+// Workgroup (x, y): `per` tokens from x * per on; L threads to an item, which
+// stays theirs for all of the tokens (so gains stay in registers): H query
+// heads, G key heads, G value heads, cut into gridDim.y slices.  A wave finds
+// the place of every fourth token and takes its sines; an item's data is on its
+// way under that, the next token's under the work on one.
 template <bool BF, int L>
-__global__ void __launch_bounds__(kRopeThreads) k_rope_append(PagedCache c, PagedBatch b, RopeArgs a) {
-    __shared__ float cs[2][128];              // cosines, then sines at 64; one buffer per token parity
+__global__ void __launch_bounds__(kRopeThreads) k_rope_append(PagedCache c, PagedBatch b, RopeArgs a, int per) {
+    __shared__ float cs[kRopeTokens][128];    // cosines, then sines at 64
+    __shared__ int64_t to_k[kRopeTokens], to_v[kRopeTokens];        // where a token's keys and values go: kNowhere, kPadding
+    constexpr int64_t kNowhere = -1, kPadding = -2;
     const int tid = threadIdx.x, D = c.D, half = a.rot >> 1;
     const int lane = tid % L, ch = a.rot >> 4;                      // rotated chunks per half
     const int lo = lane < ch ? 8 * lane : 16 * lane, hi = lane < ch ? half + 8 * lane : 16 * lane + 8;
-    const bool on = 16 * lane < D;
-    const int items = a.H + 2 * c.G, first = (blockIdx.y * kRopeThreads + tid) / L, step = gridDim.y * (kRopeThreads / L);
-    int flip = 0;
-    for (int t = blockIdx.x; t < b.T; t += gridDim.x) {
-        int64_t place = -1;
-        const int seq = paged_place(b, t, &place);
-        if (seq < 0 || place < 0) continue;                         // padding; the same for the whole workgroup
-        if (tid < half) {
-            const double turns = (double)(b.prefix + place) * a.freq[tid] * 0.15915494309189533577;
-            float sn, cn;
-            sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cn);
-            cs[flip][tid] = cn;
-            cs[flip][64 + tid] = sn;
-        }
-        // where the token's key and value go: nowhere when its page is not one of the cache's
-        const int64_t blk = place >> 4;
-        const int64_t pg = blk / c.unit;
-        int64_t row = -1, page = -1;
-        if (pg < b.width) {
-            page = b.table[seq * b.table_stride + pg];
-            if ((uint64_t)page < (uint64_t)c.n_pages) row = place - pg * c.unit * kPageUnit;
-        }
-        __syncthreads();
-        for (int it = first; it < items; it += step) {
-            if (it >= a.H && row < 0) break;
-            const uint16_t* src;
-            uint16_t* dst;
-            const float* gain = nullptr;
-            if (it < a.H) {
-                src = a.q + t * a.qt + it * a.qh;
-                dst = a.out + t * a.ot + it * a.oh;
-                gain = a.qn;
-            } else if (it < a.H + c.G) {
-                const int g = it - a.H;
-                src = a.k + t * a.kt + g * a.kh;
-                dst = c.k + page * c.kp + g * c.kh + row * c.ks;
-                gain = a.kn;
-            } else {
-                const int g = it - a.H - c.G;
-                src = a.v + t * a.vt + g * a.vh;
-                dst = c.v + page * c.vp + g * c.vh + row * c.vs;
+    const int it = (blockIdx.y * kRopeThreads + tid) / L;
+    const bool query = it < a.H, key = !query && it < a.H + c.G, on = 16 * lane < D && it < a.H + 2 * c.G;
+    const int g = query ? it : key ? it - a.H : it - a.H - c.G;
+    const uint16_t* const from = query ? a.q + g * a.qh : key ? a.k + g * a.kh : a.v + g * a.vh;
+    const int64_t next = query ? a.qt : key ? a.kt : a.vt;
+    uint16_t* const dst = query ? a.out + g * a.oh : key ? c.k + g * c.kh : c.v + g * c.vh;
+    const float* const gain = query ? a.qn : key ? a.kn : nullptr;
+    float gl[8], gh[8];
+    if (gain && on)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gl[i] = gain[lo + i], gh[i] = gain[hi + i];
+    const int t0 = blockIdx.x * per, n = min(per, b.T - t0);
+    const uint16_t* src = from + t0 * next;
+    u32x4 n0 = {0, 0, 0, 0}, n1 = {0, 0, 0, 0};
+    if (on) n0 = *(const u32x4*)(src + lo), n1 = *(const u32x4*)(src + hi);
+    for (int i = tid >> 6; i < n; i += kRopeThreads / 64) {
+        const int j = tid & 63;
+        int64_t place = -1, k = kPadding, v = 0;
+        const int seq = paged_place(b, t0 + i, &place);
+        if (seq >= 0 && place >= 0) {
+            k = kNowhere;
+            if (place >> 4 < (int64_t)b.width * c.unit) {
+                const int at = (int)unit_div((unsigned)(place >> 4), c.magic);
+                const int page = b.table[seq * b.table_stride + at];
+                const int64_t row = place - at * c.unit * kPageUnit;
+                if ((unsigned)page < (unsigned)c.n_pages) k = page * c.kp + row * c.ks, v = page * c.vp + row * c.vs;
             }
-            u32x4 u0 = {0, 0, 0, 0}, u1 = {0, 0, 0, 0};
-            if (on) {
-                u0 = *(const u32x4*)(src + lo);
-                u1 = *(const u32x4*)(src + hi);
+            if (j < half) {
+                const double turns = (double)(b.prefix + place) * a.freq[j] * 0.15915494309189533577;
+                float sn, cn;
+                sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cn);
+                cs[i][j] = cn;
+                cs[i][64 + j] = sn;
             }
-            if (it < a.H + c.G) {
-                float x[8], y[8];
-                unpack8<BF>(u0, x);
-                unpack8<BF>(u1, y);
-                if (gain) {
-                    float s = 0.f;
+        }
+        if (j == 0) to_k[i] = k, to_v[i] = v;
+    }
+    __syncthreads();
+    for (int i = 0; i < n; ++i) {
+        u32x4 u0 = n0, u1 = n1;
+        src += next;
+        if (on && i + 1 < n) n0 = *(const u32x4*)(src + lo), n1 = *(const u32x4*)(src + hi);
+        const int64_t place = to_k[i];
+        if (place == kPadding) continue;                            // the same for the whole workgroup
+        if (query || key) {
+            float x[8], y[8];
+            unpack8<BF>(u0, x);
+            unpack8<BF>(u1, y);
+            if (gain) {
+                float s = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], fmaf(y[i], y[i], s));
-                    s = 1.0f / sqrtf(group_sum<L>(s) / (float)D + a.eps);
-                    if (on)
+                for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], fmaf(y[j], y[j], s));
+                s = 1.0f / sqrtf(group_sum<L>(s) / (float)D + a.eps);
+                if (on)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            x[i] *= s * gain[lo + i];
-                            y[i] *= s * gain[hi + i];
-                        }
-                }
-                if (lane < ch)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float cn = cs[flip][lo + i], sn = cs[flip][64 + lo + i];
-                        const float r = x[i] * cn - y[i] * sn;
-                        y[i] = y[i] * cn + x[i] * sn;
-                        x[i] = r;
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] *= s * gl[j];
+                        y[j] *= s * gh[j];
                     }
-                u0 = pack8<BF>(x);
-                u1 = pack8<BF>(y);
             }
-            if (on) {
-                *(u32x4*)(dst + lo) = u0;
-                *(u32x4*)(dst + hi) = u1;
-            }
+            if (lane < ch)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float cn = cs[i][lo + j], sn = cs[i][64 + lo + j];
+                    const float r = x[j] * cn - y[j] * sn;
+                    y[j] = y[j] * cn + x[j] * sn;
+                    x[j] = r;
+                }
+            u0 = pack8<BF>(x);
+            u1 = pack8<BF>(y);
         }
-        flip ^= 1;
+        if (on && (query || place != kNowhere)) {
+            uint16_t* const d = dst + (query ? (t0 + i) * a.ot : key ? place : to_v[i]);
+            *(u32x4*)(d + lo) = u0;
+            *(u32x4*)(d + hi) = u1;
+        }
     }
 }
 
@@ -163,7 +171,7 @@ int paged_args(const loopspec_paged_cache* cache, const loopspec_paged_batch* ba
         if ((G > 1 && st[i][1] < D) || (cache->n_pages > 1 && st[i][0] < D)) return LOOPSPEC_EINVAL;
     }
     if (batch->n_seqs < 0 || batch->n_tokens < 0 || batch->prefix_len < 0 || batch->table_width < 0) return LOOPSPEC_EINVAL;
-    if (batch->prefix_len > kPlacesMax || (int64_t)batch->table_width * ps > kPlacesMax) return LOOPSPEC_EINVAL;
+    if (batch->n_tokens > kTokensMax || batch->prefix_len > kPlacesMax || (int64_t)batch->table_width * ps > kPlacesMax) return LOOPSPEC_EINVAL;
     if (batch->n_seqs > 0 && !batch->seq_len_dev) return LOOPSPEC_EINVAL;
     if (batch->n_seqs > 0 && batch->table_width > 0 && !batch->table_dev) return LOOPSPEC_EINVAL;
     if (batch->n_seqs > 1 && batch->table_stride < batch->table_width) return LOOPSPEC_EINVAL;
@@ -219,12 +227,13 @@ extern "C" int loopspec_rope_append(const loopspec_paged_cache* cache, const loo
                args->n_heads, args->rot_dim, args->eps};
     int L = 1;
     while (L * 16 < c.D) L *= 2;
-    // one pass over the heads per token while that leaves the chip unfilled
     const int64_t lanes = (int64_t)(a.H + 2 * c.G) * L;
-    const int slices = (int)((lanes + kRopeThreads - 1) / kRopeThreads);
-    const int y = (int64_t)b.T * slices <= 2048 ? slices : 1;
-    const int x = b.T < (1 << 20) ? b.T : 1 << 20;
-    void* kargs[] = {&c, &b, &a};
+    const int y = (int)((lanes + kRopeThreads - 1) / kRopeThreads);
+    // a token a workgroup while there are few; several, with gains kept and loads running ahead, once 4096
+    // workgroups stand (one each: 50 and 76 us instead of 47 and 60 at the sizes above; 8 or 16: 1 to 3 % more)
+    int per = (int)std::min<int64_t>(kRopeTokens, std::max<int64_t>(1, (int64_t)b.T * y / 4096));
+    const int x = (b.T + per - 1) / per;
+    void* kargs[] = {&c, &b, &a, &per};
     const void* f = cache->dtype == LOOPSPEC_BF16 ? rope_kernel<true>(L) : rope_kernel<false>(L);
     return hipLaunchKernel(f, dim3(x, y), dim3(kRopeThreads), kargs, 0, (hipStream_t)stream) == hipSuccess ? LOOPSPEC_OK
                                                                                                           : LOOPSPEC_EHIP;

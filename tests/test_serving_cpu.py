@@ -41,7 +41,8 @@ BAD_CACHE = [dict(dtype=B.F32), dict(dtype=9), dict(n_pages=0), dict(page_size=8
              dict(k=None), dict(v=None), dict(k=FAKE + 2), dict(v=FAKE + 8), dict(k_page=2050), dict(v_head=1028),
              dict(k_pos=32), dict(v_pos=-64), dict(k_head=0), dict(v_page=8), dict(k_pos=1 << 25)]
 BAD_BATCH = [dict(n_seqs=-1), dict(n_tokens=-1), dict(seq_len=None), dict(table=None), dict(table_stride=3),
-             dict(table_width=-1), dict(prefix_len=-1), dict(prefix_len=(1 << 28) + 1), dict(table_width=1 << 25)]
+             dict(table_width=-1), dict(prefix_len=-1), dict(prefix_len=(1 << 28) + 1), dict(table_width=1 << 25),
+             dict(n_tokens=(1 << 25) + 1)]
 
 
 def _rope_rc(c, b, a):
