@@ -249,22 +249,47 @@ struct Rows {
     // The weights of 32 positions as an operand, and their sum.  No maximum is taken: a lane's sum of 8
     // tells when some weight may leave fp16's range, and then, which is rare after the first tiles, the
     // reference is raised and the weights are taken again.
-    __device__ __forceinline__ u32x4 weights(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
+    struct Weights {
         float x[2][4], part;
-        auto take = [&]() {
+        __device__ __forceinline__ void take(const f32x4 (&s)[2], float ref, const AttnArgs& a) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.c, -ref[rt]));
+                for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.c, -ref));
             part = ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
-        };
-        take();
-        if (__any(part > kHigh)) {
-            raise(rt, s, a);
-            take();
         }
-        sum[rt] += part;
-        return u32x4{pack2<BF>(x[0][0], x[0][1]), pack2<BF>(x[0][2], x[0][3]), pack2<BF>(x[1][0], x[1][1]), pack2<BF>(x[1][2], x[1][3])};
+        __device__ __forceinline__ u32x4 packed() const {
+            return u32x4{pack2<BF>(x[0][0], x[0][1]), pack2<BF>(x[0][2], x[0][3]), pack2<BF>(x[1][0], x[1][1]), pack2<BF>(x[1][2], x[1][3])};
+        }
+    };
+    __device__ __forceinline__ u32x4 weights(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
+        Weights w;
+        w.take(s, ref[rt], a);
+        if (__any(w.part > kHigh)) {
+            raise(rt, s, a);
+            w.take(s, ref[rt], a);
+        }
+        sum[rt] += w.part;
+        return w.packed();
+    }
+    // the same for all row tiles with one branch, which leaves the products' code whole
+    __device__ __forceinline__ void weights(const f32x4 (&s)[NR][2], u32x4 (&p)[NR], const AttnArgs& a) {
+        Weights w[NR];
+        bool high = false;
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            w[rt].take(s[rt], ref[rt], a);
+            high |= w[rt].part > kHigh;
+        }
+        if (__builtin_expect(__any(high), 0))
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt)
+                if (__any(w[rt].part > kHigh)) {
+                    raise(rt, s[rt], a);
+                    w[rt].take(s[rt], ref[rt], a);
+                }
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) sum[rt] += w[rt].part, p[rt] = w[rt].packed();
     }
     // O += V^T P
     __device__ __forceinline__ void add(const Tile<BF, D>& x, const u32x4 (&p)[NR]) {
@@ -416,6 +441,21 @@ struct StageLds {
     u32x4 v[E][2][64];                        // a column of each lane's, 32 positions each
 };
 
+// The order of a run of N reads of operands from LDS, each for NR products: 4
+// reads lead.  Left to itself the compiler waits for every read before its
+// products, and that and accumulators which did not stay in place cost 8 %.
+template <int N, int NR>
+__device__ __forceinline__ void ahead() {
+    constexpr int LEAD = N < 4 ? N : 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, LEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N - LEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, NR, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, NR * LEAD, 0);
+}
+
 template <bool BF, int D, int NR>
 __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a, const AttnTask& t, StageLds<D> (&l)[2], Rows<BF, D, NR>& r) {
     constexpr int E = D / 16, NS = (D + 31) / 32;
@@ -493,54 +533,64 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
                 for (int rt = 0; rt < NR; ++rt) s[rt][b] = mfma16<BF>(f, q[rt][k], s[rt][b]);
             }
     };
-    for (int turn = 0;; ++turn, p += kStage) {
-        const StageLds<D>& st = l[turn & 1];
-        if (p + kStage <= lo) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                scores(h, st);
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) wt[rt] = r.weights(rt, s[rt], a);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const u32x4 v = st.v[e][h][lane];
-#pragma unroll
-                    for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
-                }
-            }
-        } else {
-            int lim[NR];
-#pragma unroll
-            for (int rt = 0; rt < NR; ++rt) lim[rt] = row0 + rt * 16 + n < t.rows ? t.limit(row0 + rt * 16 + n, a.per) : 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int ph = p + kATile * h;
-                if (ph >= hi) break;
-                scores(h, st);
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) r.hide(lim[rt], ph, s[rt]);
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) wt[rt] = r.weights(rt, s[rt], a);
-                bool f = true;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    u32x4 v = st.v[e][h][lane];
-                    if (lo != hi) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &f);
-                    }
-#pragma unroll
-                    for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
-                }
-                if (__any(!f)) r.add_odd(c, t, ph, lim);
-            }
-        }
-        if (p + kStage >= t.p1) break;
+    // the stage after p's to LDS, the one after that on its way
+    int turn = 0;
+    auto next = [&]() {
         put(p + kStage, id, l[(turn + 1) & 1]);
         id = nx;
         if (p + 2 * kStage < t.p1) bring(p + 2 * kStage, id);
         nx = T::look(c, t, p + 3 * kStage + 16 * w);
         __syncthreads();
+        ++turn, p += kStage;
+    };
+    // stages that all rows of the wave see (waves of a workgroup may leave at different ones: both loops
+    // have one barrier a stage)
+    while (p + kStage <= lo) {
+        const StageLds<D>& st = l[turn & 1];
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            scores(h, st);
+            ahead<2 * NS, NR>();
+            r.weights(s, wt, a);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const u32x4 v = st.v[e][h][lane];
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
+            }
+            ahead<E, NR>();
+        }
+        if (p + kStage >= t.p1) return;
+        next();
+    }
+    int lim[NR];
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) lim[rt] = row0 + rt * 16 + n < t.rows ? t.limit(row0 + rt * 16 + n, a.per) : 0;
+    for (;;) {
+        const StageLds<D>& st = l[turn & 1];
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int ph = p + kATile * h;
+            if (ph >= hi) break;
+            scores(h, st);
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) r.hide(lim[rt], ph, s[rt]);
+            r.weights(s, wt, a);
+            bool f = true;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                u32x4 v = st.v[e][h][lane];
+                if (lo != hi) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &f);
+                }
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
+            }
+            if (__any(!f)) r.add_odd(c, t, ph, lim);
+        }
+        if (p + kStage >= t.p1) return;
+        next();
     }
 }
 
@@ -679,8 +729,10 @@ struct OwnTasks {
 // false), or up to 64 * NR rows with the four waves on different rows.  The
 // others walk the own positions' tasks: a wave each with 16 rows, or (WIDE_OWN)
 // a workgroup each like the prefix.
+// Three workgroups a CU where registers and LDS suffice (heads up to 96): 88 -> 83 us
+// for 240 rows over 4007 positions of 55 heads of 96; at 128 the registers are two's.
 template <bool BF, int D, int NR, bool WIDE, bool WIDE_OWN>
-__global__ void __launch_bounds__(kAThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ void __launch_bounds__(kAThreads) __attribute__((amdgpu_waves_per_eu(WIDE && D <= 96 ? 3 : 2)))
 k_paged_attn(PagedCache c, PagedBatch b, AttnArgs a) {
     constexpr int ROWS = WIDE ? 64 * NR : 16 * NR;
     union Lds {
