@@ -877,9 +877,14 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int per = H / c.G;
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > (1 << 30)) return LOOPSPEC_EINVAL;
+    // Both sides at heads of 128 (us): 4 sequences of 40 rows a head over 2000 own positions, a wave's
+    // 16 rows at a time 34, a workgroup's 128 34; of 128 rows 52 and 45.
     pl->wide_own = each > 32;
+    // 48 rows over 8192 positions of 16 heads, 32 at a time 32.2, all at a time 32.0 (64 rows: 33.1, 34.3)
     pl->wide = pl->wide_own || (b.prefix > 0 && rows > 32);
-    pl->nr = pl->wide ? (pl->wide_own || rows > 64 ? 2 : 1) : b.prefix > 0 && rows > 16 ? 2 : 1;
+    // 32 rows a wave halve what passes through LDS, 16 spread better: 96 rows 43.7 and 38.9, 240 rows
+    // 58.6 and 58.0, 768 rows of 8 heads over 32768 positions 151 and 181
+    pl->nr = pl->wide ? (pl->wide_own || rows > 256 ? 2 : 1) : b.prefix > 0 && rows > 16 ? 2 : 1;
     const int block = pl->nr * (pl->wide ? 64 : 16), slots = 512;
     pl->rb = (int)((rows + block - 1) / block);
     pl->rows = (int)((rows + pl->rb * 16 - 1) / (pl->rb * 16) * 16);
@@ -899,7 +904,7 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     if (pairs * pl->rb > (1 << 30)) return LOOPSPEC_EINVAL;
     pl->ptasks = (int)(pairs * pl->rb);
     // own positions: about two chunks per resident wave (or workgroup) when every table is full, of at
-    // least four tiles a wave
+    // least four tiles a wave (16 instead, or 16 stages for 8: 4 x 40 rows over 2000 positions 34 -> 45 us)
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit, all = cap * b.B * c.G;
     pl->oshift = pl->wide_own ? 9 : 7;
     while (pl->oshift < 12 && (all >> pl->oshift) > (pl->wide_own ? 2 * slots : 8 * slots)) ++pl->oshift;
@@ -992,8 +997,10 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
         const void* f = bf ? attn_kernel<true>(c.D, pl) : attn_kernel<false>(c.D, pl);
         if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
     }
-    // a wave per row has 4 (D = 128) to 64 chunks in flight at once
-    const int S = pl.NP + pl.NO, wpr = S <= 8 || rows > 2048 ? 1 : S <= 64 || rows > 256 ? 4 : 16;
+    // Waves per row: one has 4 (D = 128) to 64 chunks in flight at once, several are more launches' worth of
+    // work.  In all (us) with 1, 4 and 16: 8 rows of 128 chunks 37.5, 33.4, 32.6; 512 rows 39.2, 37.6, 40.0;
+    // 1024 rows 35.1, 34.2, 41.6; 1536 rows 42.0, 43.8, 53.9; 13200 rows 77, 91, 148.
+    const int S = pl.NP + pl.NO, wpr = S <= 8 || rows > 1024 ? 1 : S <= 64 || rows > 256 ? 4 : 16;
     const void* j = bf ? join_kernel<true>(wpr) : join_kernel<false>(wpr);
     const unsigned per_wg = wpr > 4 ? 1 : 4 / wpr;
     if (hipLaunchKernel(j, dim3((unsigned)((rows + per_wg - 1) / per_wg)), dim3(wpr > 4 ? 64 * wpr : kAThreads), kargs, 0, st) != hipSuccess)
