@@ -548,8 +548,8 @@ uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* c
 
 /* Attention of the step's queries: each sees the whole prefix and its own
  * sequence's positions up to its own place.  The prefix's keys and values are
- * read once for all sequences (once per 64 rows, rows = tokens x query heads
- * of a key/value head).  A row that sees nothing gives zeros and an lse of
+ * read once for all sequences (once per block of up to 128 rows, rows = tokens
+ * x query heads of a key/value head).  A row that sees nothing gives zeros and an lse of
  * -infinity.  What lies behind a sequence's positions in its pages, and the
  * positions that a row does not see, have no influence on it, whatever they
  * hold.  A visible position whose page lies outside the table or the cache
@@ -558,7 +558,7 @@ uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* c
  * rounded to that type.  A row's result does not depend on the other
  * sequences' contents.  workspace: 16-byte aligned, its contents on entry do
  * not matter.  Errors: EINVAL (arguments, workspace too small; checked before
- * any launch), EHIP. */
+ * any launch; tokens x heads up to 2^25), EHIP. */
 int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch,
                               const loopspec_attention_args* args, void* workspace_dev, uint64_t workspace_bytes,
                               void* stream);
@@ -586,10 +586,11 @@ typedef struct {
  * is the smallest id whose kept weight through it exceeds u * kept weight.
  * Logits of -infinity are never kept.  token_dev[i]: the token; prob_dev[i] (may
  * be NULL): its share of the kept weight; kept_dev[i] (may be NULL): how many
- * ids were kept.  Weights are 64-bit (off by 2^-38) and sums do not depend on
- * the order of adding, so a row's draw is repeatable and its own.
- * A row with a NaN or +infinity among its logits, without a finite one, or whose
- * settings or number are outside their ranges gives token -1, prob 0, kept 0.
+ * ids were kept.  Weights are 64-bit (off by 2^-36 of themselves and 2^-45 of
+ * the largest) and sums do not depend on the order of adding, so a row's draw is
+ * repeatable and its own.  A row with a NaN or +infinity among its logits, without
+ * a finite one, or whose settings or number are outside their ranges gives token
+ * -1, prob 0, kept 0.
  * rows: up to 65535.  workspace: 16-byte aligned, its contents on entry do not
  * matter.  Errors: EINVAL (arguments, workspace too small; checked before any
  * launch), EHIP. */

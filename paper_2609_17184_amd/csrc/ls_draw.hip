@@ -962,14 +962,14 @@ int loopspec_sample(const loopspec_sample_cfg* cfg, int32_t rows, const void* lo
                     int32_t* token_dev, float* prob_dev, int32_t* kept_dev, void* workspace_dev, uint64_t workspace_bytes,
                     void* stream) {
     using namespace ls;
-    if (!cfg || rows < 0 || rows > 65535 || !logits_dev || !u_dev || !token_dev || stride < 0) return LOOPSPEC_EINVAL;
+    if (!cfg || rows < 0 || rows > 65535 || stride < 0) return LOOPSPEC_EINVAL;
     if (cfg->vocab < 1 || cfg->vocab > kDMaxVocab) return LOOPSPEC_EINVAL;
     if (cfg->dtype != LOOPSPEC_F32 && cfg->dtype != LOOPSPEC_BF16 && cfg->dtype != LOOPSPEC_F16) return LOOPSPEC_EINVAL;
-    if ((uintptr_t)logits_dev % (cfg->dtype == LOOPSPEC_F32 ? 4 : 2)) return LOOPSPEC_EINVAL;
     if (!cfg->temperature_dev && !(cfg->temperature >= 0.f && cfg->temperature < 3e38f)) return LOOPSPEC_EINVAL;
     if (!cfg->top_p_dev && !(cfg->top_p > 0.f && cfg->top_p <= 1.f)) return LOOPSPEC_EINVAL;
     if (!cfg->min_p_dev && !(cfg->min_p >= 0.f && cfg->min_p <= 1.f)) return LOOPSPEC_EINVAL;
-    if (!rows) return LOOPSPEC_OK;
+    if (!rows) return LOOPSPEC_OK;            // (empty tensors have no address)
+    if (!logits_dev || !u_dev || !token_dev || (uintptr_t)logits_dev % (cfg->dtype == LOOPSPEC_F32 ? 4 : 2)) return LOOPSPEC_EINVAL;
     DrawArgs a{logits_dev, stride, u_dev, cfg->temperature_dev, cfg->top_p_dev, cfg->min_p_dev, cfg->top_k_dev,
                cfg->temperature, cfg->top_p, cfg->min_p, cfg->top_k, token_dev, prob_dev, kept_dev, cfg->vocab};
     if (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < draw_workspace(cfg->vocab, rows, (char*)workspace_dev, &a))

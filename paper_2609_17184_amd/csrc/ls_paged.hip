@@ -216,11 +216,11 @@ extern "C" int loopspec_rope_append(const loopspec_paged_cache* cache, const loo
     if (args->rot_dim < 0 || args->rot_dim > c.D || args->rot_dim % 16 || (args->rot_dim && !args->freq_dev))
         return LOOPSPEC_EINVAL;
     if (!(args->eps >= 0.f)) return LOOPSPEC_EINVAL;
+    if (!b.B || !b.T) return LOOPSPEC_OK;     // (empty tensors have no address)
     if (!rows_ok(args->q_dev, args->q_token, args->q_head) || !rows_ok(args->k_dev, args->k_token, args->k_head) ||
         !rows_ok(args->v_dev, args->v_token, args->v_head) || !rows_ok(args->q_out_dev, args->out_token, args->out_head))
         return LOOPSPEC_EINVAL;
     if ((args->n_heads > 1 && args->out_head < c.D) || (b.T > 1 && args->out_token < c.D)) return LOOPSPEC_EINVAL;
-    if (!b.B || !b.T) return LOOPSPEC_OK;
     RopeArgs a{(const uint16_t*)args->q_dev, (const uint16_t*)args->k_dev, (const uint16_t*)args->v_dev,
                (uint16_t*)args->q_out_dev, args->q_token, args->q_head, args->k_token, args->k_head, args->v_token,
                args->v_head, args->out_token, args->out_head, args->freq_dev, args->q_norm_dev, args->k_norm_dev,

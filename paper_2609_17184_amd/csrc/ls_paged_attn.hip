@@ -39,6 +39,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kAThreads = 256;
 constexpr int kATile = 32;                    // positions per wave and step
 constexpr int kAStep = 4 * kATile;            // positions per workgroup and step
+constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
+constexpr int kGroupsMax = 1 << 23;            // workgroups of the prefix, for the same reason
 constexpr float kNone = -3e38f;               // the reference before the first score
 constexpr float kLift = 7.0f;                 // log2 of the weight of the score that set the reference
 constexpr float kHigh = 32768.0f;             // a lane's sum of 8 weights up to which none leaves fp16
@@ -876,7 +878,7 @@ struct AttnPlan {
 int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     const int per = H / c.G;
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
-    if (rows * c.G > (1 << 30)) return LOOPSPEC_EINVAL;
+    if (rows * c.G > kRowsMax) return LOOPSPEC_EINVAL;
     // Both sides at heads of 128 (us): 4 sequences of 40 rows a head over 2000 own positions, a wave's
     // 16 rows at a time 34, a workgroup's 128 34; of 128 rows 52 and 45.
     pl->wide_own = each > 32;
@@ -901,7 +903,7 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
         }
     }
     const int64_t pairs = ((int64_t)c.G * pl->NP + 7) / 8 * 8;
-    if (pairs * pl->rb > (1 << 30)) return LOOPSPEC_EINVAL;
+    if (pairs * pl->rb > kGroupsMax) return LOOPSPEC_EINVAL;
     pl->ptasks = (int)(pairs * pl->rb);
     // own positions: about two chunks per resident wave (or workgroup) when every table is full, of at
     // least four tiles a wave (16 instead, or 16 stages for 8: 4 x 40 rows over 2000 positions 34 -> 45 us)
@@ -981,9 +983,9 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
     auto ok = [](const void* p, int64_t token, int64_t head) {
         return p && !((uintptr_t)p & 15) && token >= 0 && head >= 0 && token % 8 == 0 && head % 8 == 0;
     };
+    if (!b.B || !b.T) return LOOPSPEC_OK;     // (empty tensors have no address)
     if (!ok(args->q_dev, args->q_token, args->q_head) || !ok(args->out_dev, args->out_token, args->out_head)) return LOOPSPEC_EINVAL;
     if ((args->n_heads > 1 && args->out_head < c.D) || (b.T > 1 && args->out_token < c.D)) return LOOPSPEC_EINVAL;
-    if (!b.B || !b.T) return LOOPSPEC_OK;
     const uint64_t need = attn_bytes(c, b, args->n_heads, pl);
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
@@ -997,8 +999,8 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
         const void* f = bf ? attn_kernel<true>(c.D, pl) : attn_kernel<false>(c.D, pl);
         if (hipLaunchKernel(f, dim3(pl.ptasks + pl.otasks), dim3(kAThreads), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
     }
-    // Waves per row: one has 4 (D = 128) to 64 chunks in flight at once, several are more launches' worth of
-    // work.  In all (us) with 1, 4 and 16: 8 rows of 128 chunks 37.5, 33.4, 32.6; 512 rows 39.2, 37.6, 40.0;
+    // Waves per row: one has 4 (D = 128) to 64 chunks in flight at once; with enough rows several each only
+    // make more workgroups.  In all (us) with 1, 4 and 16: 8 rows of 128 chunks 37.5, 33.4, 32.6; 512 rows 39.2, 37.6, 40.0;
     // 1024 rows 35.1, 34.2, 41.6; 1536 rows 42.0, 43.8, 53.9; 13200 rows 77, 91, 148.
     const int S = pl.NP + pl.NO, wpr = S <= 8 || rows > 1024 ? 1 : S <= 64 || rows > 256 ? 4 : 16;
     const void* j = bf ? join_kernel<true>(wpr) : join_kernel<false>(wpr);

@@ -10,7 +10,8 @@ For one layer and one step of a batch:
     tokens, probs, kept = sample(logits, u, temperature, top_k, top_p, min_p)
 
 Argument marshalling only: the work runs in the HIP library, on the current
-stream of the tensors' device, without waiting for it.  Wrong shapes, types or
+stream of the tensors' device, without waiting for it, and records no
+gradients.  Wrong shapes, types or
 devices raise ValueError, what the library refuses raises LoopSpecError.
 """
 from __future__ import annotations
@@ -80,7 +81,7 @@ class PagedCache:
 class Batch:
     """The sequences of a step.  seq_len [n]: own positions of each, with this step's tokens; table [n, pages]: their
     pages; q_start [n + 1] (ascending): first token of each, None when every sequence has one.  All int32 on the GPU,
-    read when the kernels run.  prefix_len positions in the pages prefix_table come before every sequence's own.
+    read when the kernels run (change them in place).  prefix_len positions in the pages prefix_table come before every sequence's own.
     Tokens outside q_start's range and those of a sequence with seq_len < 0 are padding."""
 
     def __init__(self, seq_len, table, q_start=None, prefix_len: int = 0, prefix_table=None):
@@ -173,6 +174,9 @@ def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] 
     else:
         _rows(out, heads, cache, tokens, "out")
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    if batch.prefix_len and (batch.prefix_table is None
+                             or batch.prefix_table.shape[0] * cache.page_size < batch.prefix_len):
+        raise ValueError("prefix_table: a page for every page_size positions of the prefix")
     L, ref = B.load_library(), batch._with(tokens, cache)
     nbytes = L.loopspec_prefix_attention_workspace_bytes(cache._ref, ref, heads)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)

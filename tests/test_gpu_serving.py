@@ -266,6 +266,28 @@ def test_append_pages_outside_the_cache_are_left_out():
     assert changed == [[c.tables[2][0], 9]] and not q.isnan().any()
 
 
+def test_empty_batches_and_short_prefix_tables():
+    """No tokens, or no sequences: nothing happens.  A prefix table shorter than the prefix is refused."""
+    from paper_2609_17184_amd import serving
+    c = Case(4, 2, 64, 16, "f16", [1, 1], [40, 17], 50, seed=1)
+    before = c.kd.clone()
+    none = torch.empty((0, 4, 64), dtype=c.dtype, device=DEV)
+    kv = torch.empty((0, 2, 64), dtype=c.dtype, device=DEV)
+    assert serving.rope_append(none, kv, kv, c.cache, c.batch).shape == (0, 4, 64)
+    out, lse = serving.prefix_attention(none, c.cache, c.batch, return_lse=True)
+    assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    empty = torch.empty(0, dtype=torch.int32, device=DEV)
+    nobody = serving.Batch(empty, torch.empty((0, 4), dtype=torch.int32, device=DEV), None, 50, c.batch.prefix_table)
+    kept = torch.full(c.q.shape, 3.0, dtype=c.dtype, device=DEV)
+    serving.rope_append(c.q.to(DEV), c.kn.to(DEV), c.vn.to(DEV), c.cache, nobody, out=kept)
+    serving.prefix_attention(c.q.to(DEV), c.cache, nobody, out=kept)
+    assert (kept == 3).all() and torch.equal(c.kd.nan_to_num(7), before.nan_to_num(7))
+    assert [len(x) for x in serving.sample(torch.empty((0, 100), device=DEV), torch.empty(0, dtype=torch.float64, device=DEV))] == [0] * 3
+    for table in (None, c.batch.prefix_table[:3]):
+        with pytest.raises(ValueError):
+            serving.prefix_attention(c.q.to(DEV), c.cache, serving.Batch(c.batch.seq_len, c.batch.table, None, 50, table))
+
+
 def test_attention_large_offsets():
     """Pages behind 2^31 elements of the cache."""
     from paper_2609_17184_amd import serving

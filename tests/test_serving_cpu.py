@@ -84,6 +84,13 @@ def test_bad_attention(bad):
     assert _attn_rc(_cache(), _batch(), _attn(**bad)) == B.EINVAL
 
 
+def test_attention_grids():
+    """More rows than the grids hold."""
+    big = _batch(n_tokens=(1 << 23) + 1, n_seqs=1 << 23)
+    assert _attn_rc(_cache(), big, _attn(), nbytes=1 << 62) == B.EINVAL
+    assert B.load_library().loopspec_prefix_attention_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(big), 4) == 0
+
+
 def test_attention_workspace():
     L = B.load_library()
     need = L.loopspec_prefix_attention_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(_batch()), 4)
@@ -95,7 +102,13 @@ def test_attention_workspace():
 
 
 def test_nothing_to_do():
-    """No sequences or no tokens: no launch (none would succeed here)."""
+    """No sequences or no tokens: no launch (none would succeed here), and addresses do not matter, as empty tensors
+    have none."""
+    none = dict(q=None, k=None, v=None, q_out=None)
+    assert _rope_rc(_cache(), _batch(n_tokens=0), _rope(**none)) == B.OK
+    assert _attn_rc(_cache(), _batch(n_tokens=0), _attn(q=None, out=None), ws=None, nbytes=0) == B.OK
+    cfg = B.SampleCfg(100, B.F32, 1.0, 0, 1.0, 0.0)
+    assert B.load_library().loopspec_sample(ctypes.byref(cfg), 0, None, 100, None, None, None, None, None, 0, None) == B.OK
     for kw in (dict(n_seqs=0), dict(n_tokens=0)):
         assert _rope_rc(_cache(), _batch(**kw), _rope()) == B.OK
         assert _attn_rc(_cache(), _batch(**kw), _attn(), ws=None, nbytes=0) == B.OK
