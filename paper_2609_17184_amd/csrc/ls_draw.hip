@@ -221,21 +221,65 @@ __device__ __forceinline__ u64 binned(double y, int b) {
 // its mass in 2^-44
 __device__ __forceinline__ double bin_mass(u64 x, int b) { return (double)(x & (kOne - 1)) * __hiloint2double((1029 - b / 2) << 20, 0); }
 
+// Exchanges within a full wave by VALU moves (DPP, and swaps of rows and halves):
+// a permutation through LDS takes some 50 ns, and a sort of 1024 has 90 of them
+// (with those, a row with filters took 3.7 us longer).
+template <typename T, typename F>
+__device__ __forceinline__ T by_words(T v, F move) {
+    static_assert(sizeof(T) == 4 || sizeof(T) == 8, "one or two words");
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, (uint32_t)move(__builtin_bit_cast(uint32_t, v)));
+    } else {
+        const u64 b = __builtin_bit_cast(u64, v);
+        return __builtin_bit_cast(T, (u64)move((uint32_t)(b >> 32)) << 32 | move((uint32_t)b));
+    }
+}
+// what CTRL brings, zero where it brings nothing or the row is not in ROWS
+template <int CTRL, int ROWS = 15>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 15, false);
+}
+// the value of lane ^ J
+template <int J, typename T>
+__device__ __forceinline__ T from_xor(T v) {
+    return by_words(v, [](uint32_t x) -> uint32_t {
+        if constexpr (J == 1) return dpp<0xB1>(x);                  // quad_perm [1,0,3,2]
+        if constexpr (J == 2) return dpp<0x4E>(x);                  // quad_perm [2,3,0,1]
+        if constexpr (J == 4) return dpp<0x1B>(dpp<0x141>(x));      // row_half_mirror, quad_perm [3,2,1,0]
+        if constexpr (J == 8) return dpp<0x128>(x);                 // row_ror:8
+        if constexpr (J == 16) {
+            const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+            return threadIdx.x & 16 ? p[0] : p[1];
+        }
+        if constexpr (J == 32) {
+            const auto p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+            return threadIdx.x & 32 ? p[0] : p[1];
+        }
+    });
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T v, F f) {
+    v = f(v, from_xor<1>(v)), v = f(v, from_xor<2>(v)), v = f(v, from_xor<4>(v));
+    v = f(v, from_xor<8>(v)), v = f(v, from_xor<16>(v));
+    return f(v, from_xor<32>(v));
+}
 template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-    return v;
+__device__ __forceinline__ T wave_sum(T v) { return wave_all(v, [](T a, T b) { return a + b; }); }
+__device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ double wave_max(double v) { return wave_all(v, [](double a, double b) { return fmax(a, b); }); }
+// sum of the lanes up to the lane's own
+template <typename T>
+__device__ __forceinline__ T wave_upto(T v) {
+    v += by_words(v, dpp<0x111>), v += by_words(v, dpp<0x112>);     // row_shr:1, 2, 4, 8
+    v += by_words(v, dpp<0x114>), v += by_words(v, dpp<0x118>);
+    v += by_words(v, dpp<0x142, 0xA>);                              // row_bcast:15, then row_bcast:31
+    return v + by_words(v, dpp<0x143, 0xC>);
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) v = fmax(v, __shfl_xor(v, o));
-    return v;
+// the value of one lane, the same for the wave
+template <typename T>
+__device__ __forceinline__ T from_lane(T v, int l) {
+    l = __builtin_amdgcn_readfirstlane(l);
+    return by_words(v, [l](uint32_t x) -> uint32_t { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); });
 }
 // 2^n for an integral n <= 0, 0 below -300
 __device__ __forceinline__ double power2(double n) { return n < -300.0 ? 0.0 : ldexp(1.0, (int)n); }
@@ -384,29 +428,23 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
         const double all = wave_sum(lane < a.S ? r.mine.mass * he[lane] : 0.0), most = wave_sum(m0 + m1);
         const unsigned finite = wave_sum(r.mine.finite), counted = wave_sum(c0 + c1);
         if (lane == 63) m1 = fmax(all - most, 0.0), c1 = finite - counted;
-        double sm = m0 + m1;
-        unsigned sc = c0 + c1;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const double x = __shfl_up(sm, o);
-            const unsigned y = __shfl_up(sc, o);
-            if (lane >= o) sm += x, sc += y;
-        }
+        const double sm = wave_upto(m0 + m1);
+        const unsigned sc = wave_upto(c0 + c1);
         const unsigned long long used = __ballot(c0 + c1 > 0);
-        const int last_lane = 63 - __clzll(used), last = 2 * last_lane + (__shfl(c1, last_lane) > 0);
+        const int last_lane = 63 - __clzll(used), last = 2 * last_lane + (from_lane(c1, last_lane) > 0);
         // first bin that meets a condition on (mass through, count through), the last occupied one when none does
         auto first = [&](auto meets) {
             const bool low = meets(sm - m1, sc - c1), high = meets(sm, sc);
             const unsigned long long hit = __ballot(high);
             if (!hit) return last;
             const int l = __ffsll(hit) - 1;
-            return min(2 * l + (__shfl((int)low, l) ? 0 : 1), last);
+            return min(2 * l + (from_lane((int)low, l) ? 0 : 1), last);
         };
         int lo = kCoarse, hi = -1;
         double share = all;                           // bounds of the mass that top-k keeps, as far as known
         if (set.by_k) {
             hi = lo = first([&](double, unsigned c) { return c >= (unsigned)set.top_k; });
-            const double above = __shfl(sm - m0 - m1, hi / 2) + (hi & 1 ? __shfl(m0, hi / 2) : 0.0);
+            const double above = from_lane(sm - m0 - m1, hi / 2) + (hi & 1 ? from_lane(m0, hi / 2) : 0.0);
             share = above;
         }
         if (set.by_p) {
@@ -429,8 +467,8 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
                 lo = b;
             }
         }
-        const double am = __shfl(sm - m0 - m1, lo / 2) + (lo & 1 ? __shfl(m0, lo / 2) : 0.0);
-        const unsigned ac = __shfl(sc - c0 - c1, lo / 2) + (lo & 1 ? __shfl(c0, lo / 2) : 0u);
+        const double am = from_lane(sm - m0 - m1, lo / 2) + (lo & 1 ? from_lane(m0, lo / 2) : 0.0);
+        const unsigned ac = from_lane(sc - c0 - c1, lo / 2) + (lo & 1 ? from_lane(c0, lo / 2) : 0u);
         if (lane == 0) {
             range[0] = lo, range[1] = hi;
             if (s == 0) a.plan[row] = RowPlan{rank, ac, am, all, r.ref};
@@ -561,19 +599,8 @@ __device__ unsigned pick_bin(DrawLds& l, unsigned need, double share, double* go
     unsigned c[2] = {0, 0};
     if (MASS) m[0] = l.mass[b0], m[1] = l.mass[b0 + 1];
     if (COUNT) c[0] = l.count[b0], c[1] = l.count[b0 + 1];
-    u64 sm = m[0] + m[1];
-    unsigned sc = c[0] + c[1];
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        if (MASS) {
-            const u64 v = __shfl_up(sm, o);
-            if (lane >= o) sm += v;
-        }
-        if (COUNT) {
-            const unsigned k = __shfl_up(sc, o);
-            if (lane >= o) sc += k;
-        }
-    }
+    u64 sm = MASS ? wave_upto(m[0] + m[1]) : 0;
+    unsigned sc = COUNT ? wave_upto(c[0] + c[1]) : 0u;
     if (lane == 63) l.wm[wv] = sm, l.wc[wv] = sc;
     __syncthreads();
     sm += above_m - m[0] - m[1];
@@ -744,30 +771,29 @@ __device__ Cut sorted_cut(const Search<DT>& r, const Setting& set, double all, u
         const Entry x = r.list[tid];
         key = (u64)~order_key(x.v) << 32 | (unsigned)x.id;
     }
-    for (int k = 2; k / 2 < r.n; k *= 2)
-        for (int j = k / 2; j; j /= 2) {
-            u64 o;
-            if (j < 64) {
-                o = __shfl_xor(key, j);
-            } else {
-                __syncthreads();
-                l.mass[tid] = key;
-                __syncthreads();
-                o = l.mass[tid ^ j];
-            }
+    for (int k = 2; k / 2 < r.n; k *= 2) {
+        auto step = [&](int j, u64 o) {
             if ((o < key) == (((tid & j) == 0) == ((tid & k) == 0))) key = o;
+        };
+        for (int j = k / 2; j >= 64; j /= 2) {
+            __syncthreads();
+            l.mass[tid] = key;
+            __syncthreads();
+            step(j, l.mass[tid ^ j]);
         }
+        if (k >= 64) step(32, from_xor<32>(key));
+        if (k >= 32) step(16, from_xor<16>(key));
+        if (k >= 16) step(8, from_xor<8>(key));
+        if (k >= 8) step(4, from_xor<4>(key));
+        if (k >= 4) step(2, from_xor<2>(key));
+        step(1, from_xor<1>(key));
+    }
     const uint32_t h = ~(uint32_t)(key >> 32);
     const bool in = tid < r.n;
     e->v = in ? __uint_as_float(h & 0x80000000u ? h & 0x7FFFFFFFu : ~h) : -INFINITY;
     e->id = (int)(unsigned)key;
     *m = in ? mass44(r.y(e->v)) : 0;
-    u64 upto = *m;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const u64 x = __shfl_up(upto, o);
-        if (lane >= o) upto += x;
-    }
+    u64 upto = wave_upto(*m);
     __syncthreads();
     if (lane == 63) l.wm[wv] = upto;
     if (tid == 0) l.above_mass = 0;
@@ -794,13 +820,16 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     __shared__ DrawLds l;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const Setting set(a, row);
-    const Whole w(a, row);
     const size_t row0 = (size_t)row * a.S;
+    // (asked for together; what a row without filters, or a bad one, finds there is not used)
+    RowPlan plan = a.plan[row];
+    const unsigned listed = set.filters() ? a.listed[row] : 0u;
+    const double shard_above = tid < a.S ? a.above[row0 + tid] : 0.0;
+    const Whole w(a, row);
     if (!set.ok || w.bad || !(w.top > -INFINITY) || set.T == 0.f) {
         const bool greedy = set.ok && !w.bad && w.top > -INFINITY;
         int best = w.mine.top == w.top ? w.mine.arg : 0x7FFFFFFF;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) best = min(best, __shfl_xor(best, o));
+        best = wave_all(best, [](int a, int b) { return min(a, b); });
         if (tid == 0) {
             a.token[row] = greedy ? best : -1;
             if (a.prob) a.prob[row] = greedy ? 1.f : 0.f;
@@ -810,7 +839,6 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     }
     const double top = set.octaves(w.top);
     const bool filters = set.filters();
-    const unsigned listed = filters ? a.listed[row] : 0u;
     const bool fits = listed <= (unsigned)kListMax;
     Search<DT> r{a, row * a.stride, fits ? a.list + (size_t)row * kListMax : nullptr, fits ? (int)listed : a.V, w.top, set.scale, l};
     if (tid < kShardsMax) l.shard[tid] = 0;
@@ -819,7 +847,6 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     Cut cut;
     unsigned above_c = 0;
     if (filters) {
-        RowPlan plan = a.plan[row];
         // masses in units of 2^-44 of the row's largest weight
         const double unit = weight(plan.ref - top);
         u64 above_m = (u64)rint(plan.above_m * unit);
@@ -858,7 +885,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid < a.S) {
         double m = 0.0;
         if (w.mine.top > -INFINITY && (!filters || fits))
-            m = (filters ? a.above[row0 + tid] : w.mine.mass) * weight(w.mine.e - top);
+            m = (filters ? shard_above : w.mine.mass) * weight(w.mine.e - top);
         l.ws[tid] = m + (double)l.shard[tid];
     }
     const unsigned finite = wave_sum(w.mine.finite);
@@ -868,16 +895,10 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     // the shard that holds the token, found by every wave (sums may round up to the goal: then the last one
     // with any mass)
     const double here = lane < a.S ? l.ws[lane] : 0.0;
-    double through = here;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const double x = __shfl_up(through, o);
-        if (lane >= o) through += x;
-    }
-    const double all = __shfl(through, 63), goal = a.u[row] * all;
+    const double through = wave_upto(here), all = from_lane(through, 63), goal = a.u[row] * all;
     const u64 past = __ballot(here > 0.0 && through > goal), some = __ballot(here > 0.0);
     const int run = past ? __ffsll(past) - 1 : 63 - __clzll(some);
-    const double rest = goal - __shfl(through - here, run);
+    const double rest = goal - from_lane(through - here, run);
     // its ids in order, four a thread
     double own[4], sum = 0.0;
     const int id0 = run * kShard + 4 * tid;
@@ -888,12 +909,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
         own[k] = cut.keeps(v, id0 + k) && x >= (double)set.min_p ? x * 17592186044416.0 : 0.0;
         sum += own[k];
     }
-    double upto = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const double v = __shfl_up(upto, o);
-        if (lane >= o) upto += v;
-    }
+    double upto = wave_upto(sum);
     if (lane == 63) l.wd[wv] = upto;
     __syncthreads();
     for (int i = 0; i < wv; ++i) upto += l.wd[i];
