@@ -23,6 +23,9 @@ BATCHES = [
     (3, 3, 16, 16, "bf16", [1, 2], [5, 65], 33),
     (32, 8, 64, 16, "f16", [40, 3], [40, 200], 0),      # more rows of a sequence than a block holds
     (2, 1, 128, 1008, "f16", [1, 1], [1500, 20], 2000),  # pages that divide nothing
+    # more sequences than a wave looks at together, with a few tokens or many rows each
+    (2, 1, 32, 16, "f16", [i % 3 for i in range(600)], [i * 7 % 50 + 2 for i in range(600)], 33),
+    (32, 1, 16, 16, "bf16", [2] * 300, [i * 11 % 60 + 2 for i in range(300)], 20),
 ]
 
 
@@ -219,6 +222,15 @@ def test_attention_row_counts(tokens, D):
         c = Case(8, 2, D, 16, "f16" if tokens % 2 else "bf16", new, lens, 333, seed=tokens)
         out, lse = serving.prefix_attention(c.q.to(DEV), c.cache, c.batch, return_lse=True)
         check_attention(c, D ** -0.5, out, lse, out.cpu())
+
+
+@pytest.mark.parametrize("width,new", [(None, [1, 3]), (20000, [1, 3]), (20000, [1, 40])])
+def test_attention_long_sequences(width, new):
+    """Own positions in many chunks, in tables with room for more: chunks of every size, a short one behind them."""
+    from paper_2609_17184_amd import serving
+    c = Case(4, 2, 64, 64, "bf16", new, [9000, 20011], 500, seed=13, width=width)
+    out, lse = serving.prefix_attention(c.q.to(DEV), c.cache, c.batch, return_lse=True)
+    check_attention(c, 0.125, out, lse, out.cpu())
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
