@@ -524,6 +524,9 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
     r.start();
     const bool idle = row0 >= t.rows;
     const int lo = idle ? 0 : t.limit(row0, a.per), hi = idle ? 0 : t.limit(min(row0 + NR * 16, t.rows) - 1, a.per);
+    // some position that the workgroup brings is hidden from some of the wave's rows; from all of them where they
+    // are one token's (lo == hi) and another wave's token is later
+    const bool hidden = lo != hi || hi < t.p1;
     put(p, id, l[0]);
     id = nx;
     if (p + kStage < t.p1) bring(p + kStage, id);
@@ -591,7 +594,7 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const AttnArgs& a
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 u32x4 v = st.v[e][h][lane];
-                if (lo != hi) {
+                if (hidden) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &f);
                 }
