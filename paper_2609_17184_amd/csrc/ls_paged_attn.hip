@@ -246,12 +246,15 @@ struct Rows {
             if (p + 16 + 4 * gq + i >= lim) s[1][i] = -INFINITY;
         }
     }
-    // a new reference: the largest score so far gets the weight 2^kLift
-    __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
+    // A new reference for the lane's row if some weight of its is high: the largest score so far gets the weight
+    // 2^kLift.  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.
+    __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], float part, const AttnArgs& a) {
+        part = fmaxf(part, __shfl_xor(part, 16));
+        part = fmaxf(part, __shfl_xor(part, 32));
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float now = fmaxf(ref[rt], fmaf(mx, a.c, -kLift)), al = __builtin_amdgcn_exp2f(ref[rt] - now);
+        const float now = part > kHigh ? fmaxf(ref[rt], fmaf(mx, a.c, -kLift)) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
         ref[rt] = now;
         sum[rt] *= al;
 #pragma unroll
@@ -277,7 +280,7 @@ struct Rows {
         Weights w;
         w.take(s, ref[rt], a);
         if (__any(w.part > kHigh)) {
-            raise(rt, s, a);
+            raise(rt, s, w.part, a);
             w.take(s, ref[rt], a);
         }
         sum[rt] += w.part;
@@ -296,7 +299,7 @@ struct Rows {
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt)
                 if (__any(w[rt].part > kHigh)) {
-                    raise(rt, s[rt], a);
+                    raise(rt, s[rt], w[rt].part, a);
                     w[rt].take(s[rt], ref[rt], a);
                 }
 #pragma unroll
