@@ -130,9 +130,10 @@ struct Setting {
     // its place on the grid of half octaves
     __device__ __forceinline__ double grid(float v) const { return floor(2.0 * octaves(v)); }
 };
+// the bin of a place: 0 also for one above the largest logit's, where a threshold's slack may reach
 __device__ __forceinline__ int coarse(double grid_top, double grid) {
     const double d = grid_top - grid;
-    return d < (double)(kCoarse - 1) ? (int)d : kCoarse - 1;
+    return d < (double)(kCoarse - 1) ? max((int)d, 0) : kCoarse - 1;
 }
 
 __device__ __forceinline__ float half_bits(int dt, uint32_t b) {
