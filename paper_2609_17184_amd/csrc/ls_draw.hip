@@ -21,8 +21,11 @@
 // more are a tenth of a large batch's time) and sums have to be the same whatever
 // the order of adding: what atomics add are integers, in units of 2^-38 of a power
 // of two at a bin's upper end, or 2^-44 of the row's largest weight, and sums of
-// doubles run in an order that depends on the vocabulary alone.  Bins lie on a
-// grid of z log2(e) / T that all shards share.
+// doubles run in an order that depends on the vocabulary alone.  Weights are taken
+// from differences to the shard's or the row's largest logit, which itself weighs
+// exactly 1, so equal logits weigh the same and a u or top-p on the border between
+// them falls on the right side of it.  Bins lie on a grid of z log2(e) / T that all
+// shards share.
 //
 // The last kept rank: up to 1024 listed logits are sorted, one a thread (48 rows
 // of mixed settings: 32 us, through the histogram below 35).  More
@@ -62,8 +65,8 @@ constexpr int kDMaxVocab = 1 << 18, kShardsMax = kDMaxVocab / kShard;
 static_assert(kShardsMax == 64, "a shard per lane");
 
 struct Head {                                         // of a shard
-    double e, grid;                                   // masses are in 2^(e - 44); the largest logit's place on the grid
-    double mass;
+    double grid;                                      // the largest logit's place on the grid
+    double mass;                                      // in 2^-44 of the largest logit's weight
     float top;
     int arg, bad;                                     // lowest id of the largest logit; NaN or +infinity met
     unsigned finite;
@@ -75,8 +78,7 @@ struct Entry {
 struct RowPlan {                                      // what the listing found, for the pick
     int rank;                                         // the last kept rank lies in the list
     unsigned above_c;                                 // ranks above the listed bins
-    double above_m, all;                              // mass above them and in the whole row, in 2^ref
-    double ref;
+    double above_m, all;                              // mass above them and in the whole row, in 2^-44 of the largest weight
 };
 
 struct DrawArgs {
@@ -94,7 +96,7 @@ struct DrawArgs {
     // workspace
     Head* head;                                       // [rows][S]
     u64* bins;                                        // [rows][S][kCoarse]
-    double* above;                                    // [rows][S]: the shard's mass above the listed bins, in 2^(e - 44)
+    double* above;                                    // [rows][S]: the shard's mass above the listed bins, in the head's unit
     RowPlan* plan;                                    // [rows]
     Entry* list;                                      // [rows][kListMax]
     unsigned* listed;                                 // [rows]
@@ -120,8 +122,8 @@ struct Setting {
         by_m = draws && min_p > 0.f;
     }
     __device__ __forceinline__ bool filters() const { return by_k || by_p || by_m; }
-    // the logit in octaves, rounded: not contracted with what is subtracted from it, which at tiny T is the
-    // same product of the largest logit
+    // the logit in octaves, rounded: not contracted with what is added to it, so that a threshold lies on the grid
+    // where the largest logit does
     __device__ __forceinline__ double octaves(float v) const {
         double t = (double)v * scale;
         asm("" : "+v"(t));
@@ -129,6 +131,9 @@ struct Setting {
     }
     // its place on the grid of half octaves
     __device__ __forceinline__ double grid(float v) const { return floor(2.0 * octaves(v)); }
+    // Octaves between a logit and a larger one.  The difference is taken first: it is exact wherever weights matter,
+    // while octaves of logits far from zero are rounded, and equal logits weigh exactly 1.
+    __device__ __forceinline__ double below(float top, float v) const { return ((double)v - (double)top) * scale; }
 };
 // the bin of a place: 0 also for one above the largest logit's, where a threshold's slack may reach
 __device__ __forceinline__ int coarse(double grid_top, double grid) {
@@ -221,15 +226,17 @@ __device__ __forceinline__ u64 mass44(double y) {
     return (u64)__double_as_longlong(weight(y, 44) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
-// A bin: how many logits (from bit 51) and their mass in units of 2^-38 of
-// 2^-(b / 2), which no weight of bin b exceeds: each is off by 2^-37 of itself at
-// most, however far down, and 4096 of them stay below bit 51.
+// A bin: how many logits (from bit 51) and their mass in units of 2^-38 of the
+// power of two 2^-bin_octaves(b), which no weight of bin b exceeds beside the
+// largest one anywhere in bin 0: each is off by 2^-37 of itself at most, however
+// far down, and 4096 of them stay below bit 51.
 constexpr u64 kOne = 1ull << 51;
+__device__ __forceinline__ int bin_octaves(int b) { return (max(b, 1) - 1) >> 1; }
 __device__ __forceinline__ u64 binned(double y, int b) {
-    return kOne + ((u64)__double_as_longlong(weight(y, 38 + b / 2) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull);
+    return kOne + ((u64)__double_as_longlong(weight(y, 38 + bin_octaves(b)) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull);
 }
 // its mass in 2^-44
-__device__ __forceinline__ double bin_mass(u64 x, int b) { return (double)(x & (kOne - 1)) * __hiloint2double((1029 - b / 2) << 20, 0); }
+__device__ __forceinline__ double bin_mass(u64 x, int b) { return (double)(x & (kOne - 1)) * __hiloint2double((1029 - bin_octaves(b)) << 20, 0); }
 
 // Exchanges within a full wave by VALU moves (DPP, and swaps of rows and halves):
 // a permutation through LDS takes some 50 ns, and a sort of 1024 has 90 of them
@@ -291,8 +298,6 @@ __device__ __forceinline__ T from_lane(T v, int l) {
     l = __builtin_amdgcn_readfirstlane(l);
     return by_words(v, [l](uint32_t x) -> uint32_t { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); });
 }
-// 2^n for an integral n <= 0, 0 below -300
-__device__ __forceinline__ double power2(double n) { return n < -300.0 ? 0.0 : ldexp(1.0, (int)n); }
 
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
@@ -323,7 +328,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     __syncthreads();
     if (wrong) bad = 1;
     top = fmaxf(fmaxf(wf[0], wf[1]), fmaxf(wf[2], wf[3]));
-    const double tt = set.octaves(top), e = top > -INFINITY ? floor(tt) + 1.0 : 0.0, grid = set.grid(top);
+    const double grid = set.grid(top);
     if (set.T > 0.f && top > -INFINITY) {
         double sum = 0.0;
         if (set.filters()) {
@@ -334,7 +339,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     b[k] = coarse(grid, set.grid(v[k0 + k]));
-                    m[k] = binned(set.octaves(v[k0 + k]) - e, b[k]);
+                    m[k] = binned(set.below(top, v[k0 + k]), b[k]);
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -346,7 +351,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
             // (-infinity weighs 2^-200)
             double part[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-            for (int k = 0; k < kShardEach; ++k) part[k & 3] += weight(set.octaves(v[k]) - e, 44);
+            for (int k = 0; k < kShardEach; ++k) part[k & 3] += weight(set.below(top, v[k]), 44);
             sum = (part[0] + part[1]) + (part[2] + part[3]);
         }
         sum = wave_sum(sum);
@@ -365,7 +370,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
     const size_t at = (size_t)row * a.S + s;
     if (set.filters() && tid < kCoarse) a.bins[at * kCoarse + tid] = bins[tid];
     if (tid == 0) {
-        a.head[at] = Head{e, grid, (wm[0] + wm[1]) + (wm[2] + wm[3]), top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
+        a.head[at] = Head{grid, (wm[0] + wm[1]) + (wm[2] + wm[3]), top, arg, bad, wc[0] + wc[1] + wc[2] + wc[3]};
         if (s == 0) a.listed[row] = 0;
     }
 }
@@ -373,24 +378,23 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_shard(DrawArgs a) {
 // what a row's shards have in common; every wave works it out from the heads
 struct Whole {
     float top;
-    double grid, ref;                                 // of the row's largest logit; the largest e
+    double grid;                                      // of the row's largest logit
     bool bad;
     Head mine;                                        // lane s: shard s's (nothing in it behind the last one)
     __device__ __forceinline__ Whole(const DrawArgs& a, int row) {
         const int lane = threadIdx.x & 63;
-        mine = Head{-1e300, -INFINITY, 0.0, -INFINITY, 0x7FFFFFFF, 0, 0};
+        mine = Head{-INFINITY, 0.0, -INFINITY, 0x7FFFFFFF, 0, 0};
         if (lane < a.S) mine = a.head[(size_t)row * a.S + lane];
-        if (!(mine.top > -INFINITY)) mine.e = -1e300, mine.grid = -INFINITY;
+        if (!(mine.top > -INFINITY)) mine.grid = -INFINITY;
         top = wave_max(mine.top);
         grid = wave_max(mine.grid);
-        ref = wave_max(mine.e);
         bad = __any(mine.bad);
     }
 };
 
 template <int DT>
 __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
-    __shared__ double he[kShardsMax], part_m[2][kCoarse];   // a shard's unit over the row's; halves of the row's bins
+    __shared__ double he[kShardsMax], part_m[2][kCoarse];   // a shard's largest weight over the row's; halves of the row's bins
     __shared__ float shifted[kShard + 4];
     __shared__ int ho[kShardsMax];
     __shared__ unsigned part_c[2][kCoarse];
@@ -405,7 +409,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
     const size_t row0 = (size_t)row * a.S;
     if (tid < a.S) {
         // (a shard without a finite logit has empty bins, wherever they go)
-        he[tid] = power2(r.mine.e - r.ref);
+        he[tid] = weight(set.below(r.top, r.mine.top));
         ho[tid] = r.mine.grid > -INFINITY ? coarse(r.grid, r.mine.grid) : 0;
     }
     if (tid == 0) n = 0;
@@ -481,7 +485,7 @@ __global__ void __launch_bounds__(kShardThreads) k_draw_list(DrawArgs a) {
         const unsigned ac = from_lane(sc - c0 - c1, lo / 2) + (lo & 1 ? from_lane(c0, lo / 2) : 0u);
         if (lane == 0) {
             range[0] = lo, range[1] = hi;
-            if (s == 0) a.plan[row] = RowPlan{rank, ac, am, all, r.ref};
+            if (s == 0) a.plan[row] = RowPlan{rank, ac, am, all};
         }
     }
     __syncthreads();
@@ -847,7 +851,6 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
         }
         return;
     }
-    const double top = set.octaves(w.top);
     const bool filters = set.filters();
     const bool fits = listed <= (unsigned)kListMax;
     Search<DT> r{a, row * a.stride, fits ? a.list + (size_t)row * kListMax : nullptr, fits ? (int)listed : a.V, w.top, set.scale, l};
@@ -857,9 +860,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     Cut cut;
     unsigned above_c = 0;
     if (filters) {
-        // masses in units of 2^-44 of the row's largest weight
-        const double unit = weight(plan.ref - top);
-        u64 above_m = (u64)rint(plan.above_m * unit);
+        u64 above_m = (u64)rint(plan.above_m);        // masses in units of 2^-44 of the row's largest weight
         above_c = plan.above_c;
         if (!fits) above_m = 0, above_c = 0, plan.rank = set.by_k || set.by_p;
         auto count = [&](int id, float v, u64 m) -> unsigned {
@@ -872,7 +873,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
             Entry e{-INFINITY, 0};
             u64 m = 0;
             if (plan.rank) {
-                cut = sorted_cut(r, set, plan.all * unit, above_m, above_c, &e, &m);
+                cut = sorted_cut(r, set, plan.all, above_m, above_c, &e, &m);
             } else if (tid < r.n) {
                 e = r.list[tid];
                 m = mass44(r.y(e.v));
@@ -883,7 +884,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
             if (plan.rank && set.by_p) {
                 // (without top-k the row's mass is known; the list alone holds what top-k kept)
                 const bool whole = fits && !set.by_k;
-                cut = last_kept<false>(r, cut, 0u, whole ? 0.0 : (double)set.top_p, whole ? (double)set.top_p * (plan.all * unit) : 0.0, above_m, above_c);
+                cut = last_kept<false>(r, cut, 0u, whole ? 0.0 : (double)set.top_p, whole ? (double)set.top_p * plan.all : 0.0, above_m, above_c);
             }
             r.each([&](int id, float v) { n += count(id, v, mass44(r.y(v))); });
         }
@@ -895,7 +896,7 @@ __global__ void __launch_bounds__(kDThreads) k_draw_pick(DrawArgs a) {
     if (tid < a.S) {
         double m = 0.0;
         if (w.mine.top > -INFINITY && (!filters || fits))
-            m = (filters ? shard_above : w.mine.mass) * weight(w.mine.e - top);
+            m = (filters ? shard_above : w.mine.mass) * weight(r.y(w.mine.top));
         l.ws[tid] = m + (double)l.shard[tid];
     }
     const unsigned finite = wave_sum(w.mine.finite);
