@@ -555,7 +555,7 @@ uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* c
  * hold.  A visible position whose page lies outside the table or the cache
  * makes the rows that see it NaN; no memory outside the cache is read.
  * Products are of the cache's type with fp32 sums; the weights exp(s - m) are
- * rounded to that type.  A row's result does not depend on the other
+ * rounded to that type.  Values up to 2^127 give finite outputs.  A row's result does not depend on the other
  * sequences' contents.  workspace: 16-byte aligned, its contents on entry do
  * not matter.  Errors: EINVAL (arguments, workspace too small; checked before
  * any launch; tokens x heads up to 2^25), EHIP. */

@@ -23,8 +23,10 @@
 // Softmax: a weight is 2^(c s - m) with a reference m that gives the largest
 // score of its time 2^7 and is raised only when a weight could reach 2^15,
 // which after the first tiles is rare.  So the largest weight stays inside fp16's
-// range and the small ones of a long prefix keep 2^31 of room below it.  Sums
-// are fp32; weights are rounded to the cache's type for the second product.
+// range and the small ones of a long prefix keep 2^31 of room below it.  In bf16
+// these are 2^-36 and 2^-28: the output is divided by the sum of the weights last,
+// and so no finite values of 2^28 positions leave fp32 on the way.  Sums are fp32;
+// weights are rounded to the cache's type for the second product.
 //
 // Measured, both launches (us): three sequences of 40 positions and a prefix of
 // 500, 4 heads of 64: 10, two launches and their chains of loads.  32 sequences,
@@ -51,8 +53,11 @@ constexpr int kAStep = 4 * kATile;            // positions per workgroup and ste
 constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
 constexpr int kGroupsMax = 1 << 23;            // workgroups of the prefix, for the same reason
 constexpr float kNone = -3e38f;               // the reference before the first score
-constexpr float kLift = 7.0f;                 // log2 of the weight of the score that set the reference
-constexpr float kHigh = 32768.0f;             // a lane's sum of 8 weights up to which none leaves fp16
+constexpr float kRoom = 8.0f;                  // octaves that a weight may rise above the one that set the reference
+// log2 of the highest weight: a lane's sum of 8 weights up to which none leaves fp16; in bf16, whose exponents are
+// fp32's, what keeps the sums over 2^28 positions of any finite values inside fp32
+template <bool BF>
+constexpr float kTop = BF ? -28.0f : 15.0f;
 
 struct AttnArgs {
     const uint16_t* q;
@@ -226,6 +231,7 @@ __device__ __forceinline__ size_t part_slot(const AttnArgs& a, const AttnTask& t
 template <bool BF, int D, int NR>
 struct Rows {
     static constexpr int E = D / 16, NS = (D + 31) / 32;
+    static constexpr float high = BF ? 0x1p-28f : 0x1p15f;          // 2^kTop
     f32x4 o[NR][E];
     float ref[NR], sum[NR];                   // weights are 2^(c * score - ref)
 
@@ -247,21 +253,21 @@ struct Rows {
         }
     }
     // A new reference for the lane's row if some weight of its is high: the largest score so far gets the weight
-    // 2^kLift.  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.
+    // 2^(kTop - kRoom).  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.
     __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], float part, const AttnArgs& a) {
         part = fmaxf(part, __shfl_xor(part, 16));
         part = fmaxf(part, __shfl_xor(part, 32));
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float now = part > kHigh ? fmaxf(ref[rt], fmaf(mx, a.c, -kLift)) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
+        const float now = part > high ? fmaxf(ref[rt], fmaf(mx, a.c, kRoom - kTop<BF>)) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
         ref[rt] = now;
         sum[rt] *= al;
 #pragma unroll
         for (int e = 0; e < E; ++e) o[rt][e] *= al;
     }
     // The weights of 32 positions as an operand, and their sum.  No maximum is taken: a lane's sum of 8
-    // tells when some weight may leave fp16's range, and then, which is rare after the first tiles, the
+    // tells when some weight may leave its range, and then, which is rare after the first tiles, the
     // reference is raised and the weights are taken again.
     struct Weights {
         float x[2][4], part;
@@ -279,7 +285,7 @@ struct Rows {
     __device__ __forceinline__ u32x4 weights(int rt, const f32x4 (&s)[2], const AttnArgs& a) {
         Weights w;
         w.take(s, ref[rt], a);
-        if (__any(w.part > kHigh)) {
+        if (__any(w.part > high)) {
             raise(rt, s, w.part, a);
             w.take(s, ref[rt], a);
         }
@@ -289,16 +295,16 @@ struct Rows {
     // the same for all row tiles with one branch, which leaves the products' code whole
     __device__ __forceinline__ void weights(const f32x4 (&s)[NR][2], u32x4 (&p)[NR], const AttnArgs& a) {
         Weights w[NR];
-        bool high = false;
+        bool any = false;
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
             w[rt].take(s[rt], ref[rt], a);
-            high |= w[rt].part > kHigh;
+            any |= w[rt].part > high;
         }
-        if (__builtin_expect(__any(high), 0))
+        if (__builtin_expect(__any(any), 0))
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt)
-                if (__any(w[rt].part > kHigh)) {
+                if (__any(w[rt].part > high)) {
                     raise(rt, s[rt], w[rt].part, a);
                     w[rt].take(s[rt], ref[rt], a);
                 }
