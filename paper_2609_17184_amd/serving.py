@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 from typing import Optional
 
 from . import binding as B
@@ -36,6 +37,13 @@ def _dtype(t) -> int:
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
+
+
+def _size(n: int, what: str) -> int:
+    """A size for a 32-bit field, which would keep the low bits of a larger one."""
+    if not 0 <= n < 1 << 31:
+        raise ValueError(f"{what}: {n} is not in [0, 2^31)")
+    return n
 
 
 def _ints(t, shape, device, what: str):
@@ -72,7 +80,7 @@ class PagedCache:
         _need(k.is_cuda and k.device == v.device, "keys and values: on one GPU")
         _need(k.stride(3) == 1 and v.stride(3) == 1, "keys and values: elements of a head next to each other")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = (_size(n, "keys and values") for n in k.shape)
         self._c = B.PagedCacheC(_dtype(k), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, k.data_ptr(),
                                 v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
         self._ref = ctypes.byref(self._c)
@@ -88,10 +96,10 @@ class Batch:
         n, dev = seq_len.shape[0], seq_len.device
         _need(seq_len.is_cuda, "seq_len: on the GPU")
         self.seq_len, self.table, self.q_start, self.prefix_table = seq_len, table, q_start, prefix_table
-        self.n_seqs, self.prefix_len, self.device = n, int(prefix_len), dev
+        self.n_seqs, self.prefix_len, self.device = _size(n, "seq_len"), _size(int(prefix_len), "prefix_len"), dev
         self._c = B.PagedBatchC(n, 0, None if q_start is None else _ints(q_start, (n + 1,), dev, "q_start"),
                                 _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table"),
-                                table.stride(0), table.shape[1], self.prefix_len,
+                                table.stride(0), _size(table.shape[1], "table"), self.prefix_len,
                                 None if prefix_table is None else _ints(prefix_table, (None,), dev, "prefix_table"))
 
     def _with(self, tokens: int, cache: PagedCache):
@@ -119,8 +127,8 @@ def _heads(q, cache: PagedCache):
     if q.dim() != 3:
         raise ValueError("q: [tokens, heads, head_dim]")
     tokens, heads, _ = q.shape
-    _rows(q, heads, cache, tokens, "q")
-    return tokens, heads
+    _rows(q, heads, cache, _size(tokens, "q"), "q")
+    return tokens, _size(heads, "q")
 
 
 def _like(q):
@@ -197,7 +205,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     import torch
     _need(logits.dim() == 2 and logits.is_cuda and _dtype(logits) >= 0, "logits: [rows, vocab] float32, bfloat16 or "
           "float16 on a GPU")
-    rows, vocab = logits.shape
+    rows, vocab = (_size(n, "logits") for n in logits.shape)
     dev = logits.device
     _need(vocab == 1 or logits.stride(1) == 1, "logits: a row's elements next to each other")
     _need(u.dtype == torch.float64 and u.shape == (rows,) and u.is_contiguous() and u.device == dev,
@@ -211,7 +219,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
             values.append(0)
             arrays.append(x.data_ptr())
         else:
-            values.append(x)
+            # (more ranks than there are keep all; the field has 32 bits)
+            values.append(min(max(operator.index(x), 0), vocab) if kind is torch.int32 else x)
             arrays.append(None)
     cfg = B.SampleCfg(vocab, _dtype(logits), *values, *arrays)
     token = torch.empty((rows,), dtype=torch.int32, device=dev)
