@@ -39,3 +39,22 @@ def test_last_token_of_many_heads(heads, D, tokens, length, prefix):
     if at == 0:                               # the last token begins a page of its own
         c.batch.table[0, (length - 1) // 32] = c.n_pages
         assert _same(c, q, out, lse, see)[tokens - 1].isnan().all()
+
+
+@pytest.mark.parametrize("H,G,D,page,new,lens,prefix,first", [
+    (8, 2, 64, 16, [6, 2], [45, 2], 40, 42), (4, 2, 128, 32, [70, 40], [200, 40], 100, 150), (16, 1, 32, 48, [5, 1], [700, 9], 0, 698),
+    (6, 6, 96, 16, [40, 30], [1100, 30], 7, 1075)])
+def test_last_tokens_of_few_heads(H, G, D, page, new, lens, prefix, first):
+    """The first sequence's keys and values from position `first` on: bit for bit nothing for the tokens before it and
+    the other sequence's."""
+    from paper_2609_17184_amd import serving
+    c = Case(H, G, D, page, "f16" if D < 96 else "bf16", new, lens, prefix, seed=9)
+    q = c.q.to(DEV)
+    out, lse = serving.prefix_attention(q, c.cache, c.batch, return_lse=True)
+    see = list(range(new[0] - (lens[0] - first))) + list(range(new[0], sum(new)))
+    assert 0 < len(see) < sum(new)
+    for bad in (float("nan"), float("inf"), float("-inf"), 60000.0):
+        for t in (c.kd, c.vd):
+            for place in range(first, lens[0]):
+                t[c.tables[0][place // page], :, place % page] = bad
+        _same(c, q, out, lse, see)
