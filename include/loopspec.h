@@ -542,7 +542,9 @@ typedef struct {
 } loopspec_attention_args;
 
 /* Bytes of device workspace loopspec_prefix_attention needs (0 for arguments
- * it refuses): a row's partial result per chunk of positions. */
+ * it refuses): a row's partial result per chunk of positions.  Own chunks are of
+ * 128 to 4096 positions and counted by table_width, whatever the lengths are, so
+ * prompts in tables much wider than needed ask for gigabytes. */
 uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* cache, const loopspec_paged_batch* batch,
                                                    int32_t n_heads);
 
@@ -555,7 +557,8 @@ uint64_t loopspec_prefix_attention_workspace_bytes(const loopspec_paged_cache* c
  * hold.  A visible position whose page lies outside the table or the cache
  * makes the rows that see it NaN; no memory outside the cache is read.
  * Products are of the cache's type with fp32 sums; the weights exp(s - m) are
- * rounded to that type.  Values up to 2^127 give finite outputs.  A row's result does not depend on the other
+ * rounded to that type (in fp16 those below 2^-32 of a row's largest vanish
+ * beside their share of the sum).  Values up to 2^127 give finite outputs.  A row's result does not depend on the other
  * sequences' contents.  workspace: 16-byte aligned, its contents on entry do
  * not matter.  Errors: EINVAL (arguments, workspace too small; checked before
  * any launch; tokens x heads up to 2^25), EHIP. */

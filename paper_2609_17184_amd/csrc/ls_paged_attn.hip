@@ -12,7 +12,7 @@
 // Up to 32 rows: a wave holds a tile of 32 positions of K and V in registers and
 // runs all row tiles over it; the four waves take every fourth tile and meet at
 // the end of the chunk.  Scores are formed transposed, S^T = K Q^T (K rows straight from
-// memory as the MFMA's A operand, Q in LDS in operand order): a lane ends with
+// memory as the MFMA's A operand, Q in registers as the other): a lane ends with
 // 8 positions of one query, which after exp are its B operand of
 // O^T += V^T P^T when the k index runs over the positions in that order.  V^T's
 // operand needs 8 positions of one column per lane: a lane loads D/16
@@ -25,8 +25,10 @@
 // which after the first tiles is rare.  So the largest weight stays inside fp16's
 // range and the small ones of a long prefix keep 2^31 of room below it.  In bf16
 // these are 2^-36 and 2^-28: the output is divided by the sum of the weights last,
-// and so no finite values of 2^28 positions leave fp32 on the way.  Sums are fp32;
-// weights are rounded to the cache's type for the second product.
+// and so no finite values of 2^28 positions leave fp32 on the way.  Sums are fp32.
+// Weights are rounded to the cache's type for the second product, whose operands
+// have 16 bits (with a high and a low part of each they would keep twice the bits
+// for twice the products).
 //
 // Measured, both launches (us): three sequences of 40 positions and a prefix of
 // 500, 4 heads of 64: 10, two launches and their chains of loads.  32 sequences,
@@ -34,7 +36,7 @@
 // bound by the loads of the ragged own positions and 6 us of the join.  48 x 5
 // rows, prefix 4007, 300 own, 55 heads of 96 (bf16, 272 MB): 81, 3.4 TB/s, the own
 // positions alone 51 + 8.  192 x 4 rows, prefix 32768, 8 heads of 128 (bf16, 103
-// GFLOP): 154, 671 TFLOP/s; the matrix cores are busy a third of the time, without
+// GFLOP): 151, 684 TFLOP/s; the matrix cores are busy a third of the time, without
 // a stage's loads (and their way to LDS) it would take 34 less, without the
 // exponentials 8, and the join takes 11.
 #include <algorithm>
@@ -908,6 +910,8 @@ int attn_plan(const PagedCache& c, const PagedBatch& b, int H, AttnPlan* pl) {
     // 32 rows a wave halve what passes through LDS, 16 spread better: 96 rows 43.7 and 38.9, 240 rows
     // 58.6 and 58.0, 768 rows of 8 heads over 32768 positions 151 and 181
     pl->nr = pl->wide ? (pl->wide_own || rows > 256 ? 2 : 1) : b.prefix > 0 && rows > 16 ? 2 : 1;
+    // slots: two workgroups a CU, also for heads up to 96, of which three fit (chunks for 768: 91 us instead of 83
+    // for 240 rows over 4007 positions of 55 heads of 96)
     const int block = pl->nr * (pl->wide ? 64 : 16), slots = 512;
     pl->rb = (int)((rows + block - 1) / block);
     pl->rows = (int)((rows + pl->rb * 16 - 1) / (pl->rb * 16) * 16);

@@ -13,8 +13,8 @@ DEV = "cuda:0"
 PATHS = {
     "16 rows a wave": (64, 16, [1] * 9, [30 + i for i in range(9)], 8192),
     "32 rows a wave": (64, 16, [1] * 25, [30 + i for i in range(25)], 8192),
-    "block of 128 rows": (64, 16, [1] * 60, [30 + i for i in range(60)], 8192),
-    "block of 256 rows": (64, 16, [1] * 270, [2 + i % 30 for i in range(270)], 8192),
+    "blocks of 64 rows": (64, 16, [1] * 60, [30 + i for i in range(60)], 8192),
+    "blocks of 128 rows": (64, 16, [1] * 270, [2 + i % 30 for i in range(270)], 8192),
     "own positions": (4, 64, [6, 3], [120, 100], 0),
     "own positions, blocks": (8, 64, [60, 40], [900, 700], 20),
 }
