@@ -566,6 +566,97 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
                               const loopspec_attention_args* args, void* workspace_dev, uint64_t workspace_bytes,
                               void* stream);
 
+/* Scales of a cache held in 8 bits.  Such a cache is a loopspec_paged_cache whose
+ * k_dev and v_dev hold e4m3 codes (one byte an element; the strides count bytes
+ * and are multiples of 16) and whose dtype is that of the queries and outputs.
+ * Every 16 positions of a page, head by head, have a scale 2^(b - 127), b the byte
+ * at k_dev + p * k_page + g * k_head + i for positions 16 i .. 16 i + 15 of head
+ * g of page p (values alike); an element stands for code * scale.  b = 255 makes
+ * its positions NaN. */
+typedef struct {
+    void *k_dev, *v_dev;
+    int64_t k_page, k_head, v_page, v_head;
+} loopspec_page_scales;
+
+/* loopspec_rope_append to a cache held in 8 bits: the same queries; keys (after
+ * norm and rotation, in fp32) and values become codes.  A block of 16 positions
+ * takes the smallest scale 2^e, e >= -64, that holds its new elements' largest
+ * magnitude within 448; where it keeps positions from before the step, whose scale
+ * is larger, that one, and where theirs is smaller, their codes are rounded
+ * again.  Codes are rounded to nearest even; NaN and infinities become NaN and do
+ * not count for the scale.  What lies behind a sequence's last position in its
+ * block has no meaning afterwards.  Sequences must not share the block that they
+ * append to. */
+int loopspec_rope_append_quantized(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
+                                   const loopspec_paged_batch* batch, const loopspec_rope_args* args, void* stream);
+
+/* Attention of the step's queries under a window, over 16-bit pages (scales NULL)
+ * or 8-bit ones.  Positions are counted through the prefix: token t of sequence b
+ * at own place s stands at p = prefix_len + s and sees the positions j <= p with
+ * p - j < window or j < sinks; window 0: all j <= p.  A token before its
+ * sequence's first position, and any row that sees nothing, gives zeros and an
+ * lse of -infinity; padding rows stay as they are.  Pages that hold no visible
+ * position may be missing from the tables.  What a row does not see has no
+ * influence on it, whatever it holds.  A visible position whose page lies outside
+ * the table or the cache makes the rows that see it NaN; no memory outside the
+ * cache is read.  Products are of the queries' type with fp32 sums; the weights are
+ * rounded to that type (in fp16 those below 2^-32 of a row's largest vanish beside
+ * their share of the sum; over 8-bit pages in fp16 a weight counts times its
+ * value's scale for that).  A row's result does not depend on the other
+ * sequences' contents.  window, sinks: >= 0.  workspace: 16-byte aligned, its
+ * contents on entry do not matter.  Errors: EINVAL (arguments, workspace too
+ * small; checked before any launch; tokens x heads up to 2^25), EHIP. */
+int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
+                              const loopspec_paged_batch* batch, const loopspec_attention_args* args, int32_t window,
+                              int32_t sinks, void* workspace_dev, uint64_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace loopspec_window_attention needs; 0 for arguments it
+ * refuses, and where every row is finished by one workgroup. */
+uint64_t loopspec_window_attention_workspace_bytes(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
+                                                   const loopspec_paged_batch* batch, int32_t n_heads, int32_t window,
+                                                   int32_t sinks);
+
+/* A batch whose rows continue rows of another one. */
+typedef struct {
+    int32_t n_seqs, n_children;     /* up to 65535 each; n_children * table_width < 2^31 */
+    int32_t page_size, n_pages;     /* of all the caches */
+    const int32_t* seq_len_dev;     /* [n_seqs] own positions; < 0: a row without a sequence, whose pages are not looked at */
+    const int32_t* table_dev;       /* [n_seqs][table_stride] pages that a row holds; anything outside the cache: none */
+    int64_t table_stride;
+    int32_t table_width;            /* table_width * page_size <= 2^28 */
+    const int32_t* parent_dev;      /* [n_children] row that a child continues; outside 0 .. n_seqs - 1: none */
+    const int32_t* refs_dev;        /* [n_pages] how many entries of the tables (and others of the caller) name a page; 0: free */
+    int32_t prefix_len, window, sinks;  /* as in loopspec_window_attention; window 0: all pages stay */
+    int32_t room;                   /* positions behind a child's that it is to hold pages for, up to table_width * page_size */
+    int32_t* seq_len_out_dev;       /* [n_children] */
+    int32_t* table_out_dev;         /* [n_children][out_stride], table_width of each written; apart from table_dev */
+    int64_t out_stride;
+    int32_t* refs_out_dev;          /* [n_pages]; may be refs_dev */
+    int32_t* short_dev;             /* [1] pages that were not to be had */
+} loopspec_fork_args;
+
+/* Fork, keep and end sequences of a paged cache in one step.  A child has its
+ * parent's positions.  The first child of a row takes its pages over; every other
+ * one shares the full pages and has a page of its own for what the last one holds
+ * (n positions, n = length mod page_size), to which keys and values (and scales)
+ * of these positions are copied in each of the n_caches caches.  Pages that hold
+ * no position that the sequence's next one sees (window, sinks) are let go, and so
+ * are those of rows without a child.  Then a child gets pages until it holds
+ * those of `room` positions more.  refs_out counts the new table's entries in the
+ * old one's place; new pages are those whose count has become 0, the lowest
+ * first, in the order of children and positions.  Where none is left, or the
+ * table has no place, short counts and the entry is -1, as are all entries
+ * without a page.  Children without a parent have length -1.  The last
+ * page of a row must not be held by another.  scales: [n_caches] or NULL (16-bit
+ * pages); a NULL k_dev marks a 16-bit cache.  Errors: EINVAL (arguments, checked
+ * before any launch), EHIP. */
+int loopspec_fork_pages(const loopspec_fork_args* args, const loopspec_paged_cache* caches,
+                        const loopspec_page_scales* scales, int32_t n_caches, void* workspace_dev,
+                        uint64_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace loopspec_fork_pages needs (0 for sizes it refuses). */
+uint64_t loopspec_fork_pages_workspace_bytes(int32_t n_children, int32_t n_pages);
+
 typedef struct {
     int32_t vocab;                  /* V, 1 .. 262144 */
     int32_t dtype;                  /* of the logits: LOOPSPEC_F32, LOOPSPEC_BF16 or LOOPSPEC_F16 */

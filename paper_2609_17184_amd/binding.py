@@ -76,6 +76,20 @@ class PagedBatchC(ctypes.Structure):
                 ("table_width", ctypes.c_int32), ("prefix_len", ctypes.c_int32), ("prefix_table", ctypes.c_void_p)]
 
 
+class PageScalesC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [
+        (n, ctypes.c_int64) for n in ("k_page", "k_head", "v_page", "v_head")]
+
+
+class ForkArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_children", "page_size", "n_pages")] + [
+        ("seq_len", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("table_width", ctypes.c_int32), ("parent", ctypes.c_void_p), ("refs", ctypes.c_void_p)] + [
+        (n, ctypes.c_int32) for n in ("prefix_len", "window", "sinks", "room")] + [
+        ("seq_len_out", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+        ("refs_out", ctypes.c_void_p), ("short", ctypes.c_void_p)]
+
+
 class RopeArgs(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("eps", ctypes.c_float)] + [
         (n, ctypes.c_void_p) for n in ("q", "k", "v")] + [
@@ -167,6 +181,16 @@ def load_library() -> ctypes.CDLL:
                                                                         ctypes.c_int32]),
         "loopspec_prefix_attention": (ctypes.c_int, [P(PagedCacheC), P(PagedBatchC), P(AttentionArgs),
                                                      ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
+        "loopspec_rope_append_quantized": (ctypes.c_int, [P(PagedCacheC), P(PageScalesC), P(PagedBatchC), P(RopeArgs),
+                                                          ctypes.c_void_p]),
+        "loopspec_window_attention_workspace_bytes": (ctypes.c_uint64, [P(PagedCacheC), P(PageScalesC), P(PagedBatchC),
+                                                                        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+        "loopspec_window_attention": (ctypes.c_int, [P(PagedCacheC), P(PageScalesC), P(PagedBatchC), P(AttentionArgs),
+                                                     ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_uint64,
+                                                     ctypes.c_void_p]),
+        "loopspec_fork_pages_workspace_bytes": (ctypes.c_uint64, [ctypes.c_int32, ctypes.c_int32]),
+        "loopspec_fork_pages": (ctypes.c_int, [P(ForkArgs), P(PagedCacheC), P(PageScalesC), ctypes.c_int32,
+                                               ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
         "loopspec_sample_workspace_bytes": (ctypes.c_uint64, [ctypes.c_int32, ctypes.c_int32]),
         "loopspec_sample": (ctypes.c_int, [P(SampleCfg), ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,

@@ -26,8 +26,6 @@
 
 namespace ls {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 struct RopeArgs {
     const uint16_t *q, *k, *v;
     uint16_t* out;
@@ -37,28 +35,6 @@ struct RopeArgs {
     int H, rot;
     float eps;
 };
-
-template <bool BF>
-__device__ __forceinline__ void unpack8(const u32x4& u, float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w = u[i];
-        f[2 * i] = BF ? __uint_as_float(w << 16) : h2f((uint16_t)w);
-        f[2 * i + 1] = BF ? __uint_as_float(w & 0xFFFF0000u) : h2f((uint16_t)(w >> 16));
-    }
-}
-template <bool BF>
-__device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
-    u32x4 u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (BF)
-            u[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f[2 * i], (__bf16)f[2 * i + 1]});
-        else
-            u[i] = pack_h2(f[2 * i], f[2 * i + 1]);
-    }
-    return u;
-}
 
 constexpr int kRopeThreads = 256, kRopeTokens = 4;
 
@@ -184,12 +160,40 @@ int paged_args(const loopspec_paged_cache* cache, const loopspec_paged_batch* ba
     return LOOPSPEC_OK;
 }
 
-namespace {
+// an 8-bit cache's own conditions, beside paged_args'
+int scale_args(const loopspec_paged_cache* cache, const loopspec_page_scales* scales, PageScales* s) {
+    if (!cache || !scales) return LOOPSPEC_EINVAL;
+    for (int64_t st : {cache->k_page, cache->k_head, cache->k_pos, cache->v_page, cache->v_head, cache->v_pos})
+        if (st % 16) return LOOPSPEC_EINVAL;
+    const int units = cache->page_size / kPageUnit;
+    if (!scales->k_dev || !scales->v_dev) return LOOPSPEC_EINVAL;
+    for (int64_t st : {scales->k_head, scales->v_head})
+        if (st < 0 || (cache->n_kv_heads > 1 && st < units)) return LOOPSPEC_EINVAL;
+    for (int64_t st : {scales->k_page, scales->v_page})
+        if (st < 0 || (cache->n_pages > 1 && st < units)) return LOOPSPEC_EINVAL;
+    *s = PageScales{(uint8_t*)scales->k_dev, (uint8_t*)scales->v_dev, scales->k_page, scales->k_head, scales->v_page, scales->v_head};
+    return LOOPSPEC_OK;
+}
 
 // rows of 16-byte chunks: element strides and the address keep that alignment
 bool rows_ok(const void* p, int64_t token, int64_t head) {
     return p && !((uintptr_t)p & 15) && token >= 0 && head >= 0 && token % 8 == 0 && head % 8 == 0;
 }
+
+int rope_args(const PagedCache& c, const PagedBatch& b, const loopspec_rope_args* args) {
+    if (args->n_heads < 1 || args->n_heads > (1 << 16) || args->n_heads % c.G) return LOOPSPEC_EINVAL;
+    if (args->rot_dim < 0 || args->rot_dim > c.D || args->rot_dim % 16 || (args->rot_dim && !args->freq_dev))
+        return LOOPSPEC_EINVAL;
+    if (!(args->eps >= 0.f)) return LOOPSPEC_EINVAL;
+    if (!b.B || !b.T) return LOOPSPEC_OK;     // (empty tensors have no address)
+    if (!rows_ok(args->q_dev, args->q_token, args->q_head) || !rows_ok(args->k_dev, args->k_token, args->k_head) ||
+        !rows_ok(args->v_dev, args->v_token, args->v_head) || !rows_ok(args->q_out_dev, args->out_token, args->out_head))
+        return LOOPSPEC_EINVAL;
+    if ((args->n_heads > 1 && args->out_head < c.D) || (b.T > 1 && args->out_token < c.D)) return LOOPSPEC_EINVAL;
+    return LOOPSPEC_OK;
+}
+
+namespace {
 
 template <bool BF>
 const void* rope_kernel(int L) {
@@ -210,17 +214,9 @@ extern "C" int loopspec_rope_append(const loopspec_paged_cache* cache, const loo
     PagedCache c;
     PagedBatch b;
     if (!args) return LOOPSPEC_EINVAL;
-    const int rc = paged_args(cache, batch, &c, &b);
-    if (rc) return rc;
-    if (args->n_heads < 1 || args->n_heads > (1 << 16) || args->n_heads % c.G) return LOOPSPEC_EINVAL;
-    if (args->rot_dim < 0 || args->rot_dim > c.D || args->rot_dim % 16 || (args->rot_dim && !args->freq_dev))
-        return LOOPSPEC_EINVAL;
-    if (!(args->eps >= 0.f)) return LOOPSPEC_EINVAL;
+    int rc = paged_args(cache, batch, &c, &b);
+    if (rc || (rc = rope_args(c, b, args))) return rc;
     if (!b.B || !b.T) return LOOPSPEC_OK;     // (empty tensors have no address)
-    if (!rows_ok(args->q_dev, args->q_token, args->q_head) || !rows_ok(args->k_dev, args->k_token, args->k_head) ||
-        !rows_ok(args->v_dev, args->v_token, args->v_head) || !rows_ok(args->q_out_dev, args->out_token, args->out_head))
-        return LOOPSPEC_EINVAL;
-    if ((args->n_heads > 1 && args->out_head < c.D) || (b.T > 1 && args->out_token < c.D)) return LOOPSPEC_EINVAL;
     RopeArgs a{(const uint16_t*)args->q_dev, (const uint16_t*)args->k_dev, (const uint16_t*)args->v_dev,
                (uint16_t*)args->q_out_dev, args->q_token, args->q_head, args->k_token, args->k_head, args->v_token,
                args->v_head, args->out_token, args->out_head, args->freq_dev, args->q_norm_dev, args->k_norm_dev,

@@ -45,9 +45,6 @@
 
 namespace ls {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAThreads = 256;
 constexpr int kATile = 32;                    // positions per wave and step
@@ -82,31 +79,6 @@ struct AttnArgs {
 __host__ __device__ __forceinline__ int own_chunks(int len, int shift) {
     const int c = (len + (1 << shift) / 2 - 1) >> shift;
     return len <= 0 ? 0 : c > 1 ? c : 1;
-}
-
-template <bool BF>
-__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
-    if constexpr (BF)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-template <bool BF>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    if (BF) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    return pack_h2(a, b);
-}
-template <bool BF>
-__device__ __forceinline__ bool finite16(uint32_t w) {
-    constexpr uint32_t e = BF ? 0x7F80u : 0x7C00u;
-    return (w & e) != e;
-}
-// the halves of a word that are finite; *all becomes false when one is not
-template <bool BF>
-__device__ __forceinline__ uint32_t sane(uint32_t w, bool* all) {
-    const uint32_t k = (finite16<BF>(w) ? 0xFFFFu : 0u) | (finite16<BF>(w >> 16) ? 0xFFFF0000u : 0u);
-    *all = *all && k == ~0u;
-    return w & k;
 }
 
 // D/16 consecutive 16-bit columns of one position: `off` bytes behind a

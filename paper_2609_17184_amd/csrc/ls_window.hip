@@ -1,0 +1,817 @@
+// Attention over a paged cache of 16-bit or 8-bit pages under a window of the
+// latest positions and a few first ones.
+//
+//   o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   s_j = scale * q . k_j,   j <= p and (p - j < window or j < sinks)
+//
+// A task is a block of rows (tokens x query heads of a key/value head) of one
+// sequence.  What its rows see are two runs of blocks of 16 positions, the first
+// ones and the latest; the task's list of blocks is the two put together, cut
+// into chunks where there are too few tasks to fill the card.
+//
+// The products are those of the prefix's attention: S^T = K Q^T with K straight
+// from memory as the matrix instruction's first operand, so that a lane holds 4
+// positions of each of two blocks for one row; exp of them is the operand of
+// O^T += V^T P^T.
+//
+// 8-bit pages: codes have 4 significant bits and are exact in fp16 and bf16, so
+// they are widened (one instruction for two) and multiplied as they are.  A key
+// block's scale joins the factor of its scores.  A value block's scale 2^e goes
+// into the widening in bf16, whose range holds the result; in fp16 it goes into
+// the weights, 2^(c s + e - m), and out of their sum again, so that m bounds the
+// product and neither factor leaves fp16.
+//
+// Softmax: a weight is 2^(c s - m) with a reference m that gives the largest
+// score of its time 2^7 and is raised only when a weight could reach 2^15; in
+// bf16 these are 2^-36 and 2^-28, and the division by the sum comes last, so that
+// no finite values leave fp32.  Sums are fp32, weights are rounded to the
+// queries' type for the second product.
+#include <algorithm>
+
+#include "ls_paged.h"
+
+namespace ls {
+
+namespace {
+
+constexpr int kT = 256;
+constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
+constexpr int kAll = 1 << 30;                 // a window that holds every position
+constexpr float kNone = -3e38f;               // the reference before the first score
+constexpr float kRoom = 8.0f;                  // octaves that a weight may rise above the one that set the reference
+template <bool BF>
+constexpr float kTop = BF ? -28.0f : 15.0f;    // log2 of the highest weight
+
+struct WinArgs {
+    const uint16_t* q;
+    int64_t qt, qh;
+    uint16_t* out;
+    int64_t ot, oh;
+    float* lse;
+    float* part;                              // [rows][NO][D], rows = tokens x heads
+    float* ml;                                // [rows][NO][2]: reference (base 2), sum
+    float c;                                  // scale * log2(e)
+    int H, per;                               // query heads; per key/value head
+    int W, S;                                 // window (kAll: none), sinks
+    int RT;                                   // rows of a block
+    int NO, CT;                               // chunks at most, tiles of 32 positions per chunk
+};
+
+// ---- 8-bit operands
+template <bool BF, int HALF>
+__device__ __forceinline__ uint32_t widen2(uint32_t w, float scale) {
+    if constexpr (BF)
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HALF != 0));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HALF != 0));
+}
+template <bool BF>
+__device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
+    return u32x4{widen2<BF, 0>(a, 1.f), widen2<BF, 1>(a, 1.f), widen2<BF, 0>(b, 1.f), widen2<BF, 1>(b, 1.f)};
+}
+// the exponent of a value block's scale, as far as it matters (below 2^-64 e4m3 values vanish in every output)
+__device__ __forceinline__ int value_exp(uint32_t b) { return max((int)b - 127, -64); }
+
+// Columns of the output that lane m of 16 and index e stand for: what a lane loads of a position's values.
+template <bool Q8, int E>
+__device__ __forceinline__ constexpr int column_of(int m, int e) {
+    return Q8 && E == 6 ? (e < 4 ? 4 * m + e : 64 + 2 * m + e - 4) : E * m + e;
+}
+
+// A lane's part of the keys of 16 positions.
+template <bool BF, bool Q8, int D>
+struct Keys;
+template <bool BF, int D>
+struct Keys<BF, false, D> {
+    static constexpr int NS = (D + 31) / 32;
+    u32x4 w[NS];
+    __device__ __forceinline__ void load(const char* b, uint32_t row, int gq) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            w[s] = u32x4{0, 0, 0, 0};
+            if (D % 32 == 0 || gq < 2) w[s] = *(const u32x4*)(b + 64 * s + (2 * row + 16 * gq));
+        }
+    }
+    __device__ __forceinline__ u32x4 get(int s) const { return w[s]; }
+    // element of the head that lane gq has first in step s
+    static __device__ __forceinline__ constexpr int first(int s, int gq) { return 32 * s + 8 * gq; }
+};
+// 16 bytes hold two steps' elements: the contraction's order is free, and the queries follow it
+template <bool BF, int D>
+struct Keys<BF, true, D> {
+    static constexpr int NS = (D + 31) / 32;
+    uint32_t w[2 * NS];
+    __device__ __forceinline__ void load(const char* b, uint32_t row, int gq) {
+#pragma unroll
+        for (int m = 0; m < D / 64; ++m) {
+            const u32x4 u = *(const u32x4*)(b + 64 * m + (row + 16 * gq));
+            w[4 * m] = u[0], w[4 * m + 1] = u[1], w[4 * m + 2] = u[2], w[4 * m + 3] = u[3];
+        }
+        if constexpr (D % 64 != 0) {
+            u32x2 u = {0, 0};
+            if (D % 32 == 0 || gq < 2) u = *(const u32x2*)(b + D / 64 * 64 + (row + 8 * gq));
+            w[2 * NS - 2] = u[0], w[2 * NS - 1] = u[1];
+        }
+    }
+    __device__ __forceinline__ u32x4 get(int s) const { return widen8<BF>(w[2 * s], w[2 * s + 1]); }
+    static __device__ __forceinline__ constexpr int first(int s, int gq) {
+        return s < D / 64 * 2 ? s / 2 * 64 + 16 * gq + 8 * (s & 1) : 32 * s + 8 * gq;
+    }
+};
+
+// A lane's D / 16 columns of one position's values, as loaded and as 16-bit words.
+template <bool BF, bool Q8, int E>
+struct Vals;
+template <bool BF, int E>
+struct Vals<BF, false, E> {
+    uint32_t w[(E + 1) / 2];
+    __device__ __forceinline__ void load(const char* p, uint32_t row, int n) {
+        const uint32_t off = 2 * row + 2 * E * n;
+        if constexpr (E == 8) {
+            const u32x4 u = *(const u32x4*)(p + off);
+            w[0] = u[0], w[1] = u[1], w[2] = u[2], w[3] = u[3];
+        } else if constexpr (E == 6) {
+            const uint32_t* q = (const uint32_t*)(p + off);         // 12 bytes, 4-byte aligned
+            w[0] = q[0], w[1] = q[1], w[2] = q[2];
+        } else if constexpr (E == 4) {
+            const u32x2 u = *(const u32x2*)(p + off);
+            w[0] = u[0], w[1] = u[1];
+        } else if constexpr (E == 2) {
+            w[0] = *(const uint32_t*)(p + off);
+        } else {
+            w[0] = *(const uint16_t*)(p + off);
+        }
+    }
+    __device__ __forceinline__ void wide(uint32_t (&o)[(E + 1) / 2], float) const {
+#pragma unroll
+        for (int i = 0; i < (E + 1) / 2; ++i) o[i] = w[i];
+    }
+};
+template <bool BF, int E>
+struct Vals<BF, true, E> {
+    uint32_t w[(E + 3) / 4];
+    __device__ __forceinline__ void load(const char* p, uint32_t row, int n) {
+        p += row;
+        if constexpr (E == 8) {
+            const u32x2 u = *(const u32x2*)(p + 8 * n);
+            w[0] = u[0], w[1] = u[1];
+        } else if constexpr (E == 6) {
+            w[0] = *(const uint32_t*)(p + 4 * n);
+            w[1] = *(const uint16_t*)(p + 64 + 2 * n);
+        } else if constexpr (E == 4) {
+            w[0] = *(const uint32_t*)(p + 4 * n);
+        } else if constexpr (E == 2) {
+            w[0] = *(const uint16_t*)(p + 2 * n);
+        } else {
+            w[0] = *(const uint8_t*)(p + n);
+        }
+    }
+    __device__ __forceinline__ void wide(uint32_t (&o)[(E + 1) / 2], float scale) const {
+#pragma unroll
+        for (int i = 0; i < (E + 1) / 2; ++i) o[i] = i & 1 ? widen2<BF, 1>(w[i / 2], scale) : widen2<BF, 0>(w[i / 2], scale);
+    }
+};
+
+// ---- what there is to do
+
+// A sequence as the device finds it: its tokens in this step and the own position of the first of them.
+struct Seq {
+    int start, n, first;
+};
+__device__ __forceinline__ Seq seq_at(const PagedBatch& b, int s) {
+    const int len = b.seq_len[s];
+    int start = b.q_start ? b.q_start[s] : s;
+    const int64_t end = b.q_start ? b.q_start[s + 1] : s + 1;
+    start = min(max(start, 0), b.T);
+    const int n = (int)min((int64_t)max(end, (int64_t)start), (int64_t)b.T) - start;
+    const int64_t first = (int64_t)len - (end - start);
+    return Seq{start, len < 0 ? 0 : n, (int)min(max(first, (int64_t)-kAll), (int64_t)kAll)};
+}
+
+// The blocks of 16 positions that the rows at positions lo .. hi see, numbered through the prefix's blocks and the
+// sequence's own: the first `head` of them, then those from `from` on, n in all.
+struct Seen {
+    int head, from, n;
+};
+__device__ __forceinline__ int block_of(int j, int P, int PB) { return j < P ? j >> 4 : PB + ((j - P) >> 4); }
+__device__ __forceinline__ Seen seen(const PagedBatch& b, int64_t cap, int W, int S, int lo, int hi) {
+    const int P = b.prefix, PB = (P + 15) >> 4;
+    hi = (int)min((int64_t)hi, P + cap - 1);
+    lo = max(lo, P);
+    if (hi < lo && hi < P) return Seen{0, 0, 0};     // (behind the table's end lo may pass hi)
+    const int from = block_of(min(max(lo - W + 1, 0), hi), P, PB), to = block_of(hi, P, PB) + 1;
+    const int head = S > 0 ? min(block_of(min(S - 1, hi), P, PB) + 1, from) : 0;
+    return Seen{head, from, head + to - from};
+}
+__device__ __forceinline__ int chunks_of(int n, int CT) { return max(1, ((n + 1) / 2 + CT - 1) / CT); }
+
+struct Task {
+    const int32_t* table;
+    int b0, b1;                               // its part of the list of blocks (b1 is the list's end or even)
+    int g, tok0, r0, rows;                    // row r of the block: row r0 + r of the tokens from tok0 (r < rows)
+    int pos0;                                 // position of token tok0
+    int lo, hi;                               // of the first and last row (lo -1: some rows see nothing)
+    int low;                                  // positions above it (or below the sinks) are seen by some row
+    Seen s;
+    int split, splits;
+
+    __device__ __forceinline__ int token(int r, int per) const { return tok0 + (r0 + r) / per; }
+    __device__ __forceinline__ int position(int r, int per) const { return pos0 + (r0 + r) / per; }
+};
+
+// 16 positions of a task's list
+struct Blk {
+    int id, j0, nv;                           // page (-1: none of the cache's), first position, how many there are
+    unsigned off, unit;                       // position and block in the page
+};
+__device__ __forceinline__ Blk look(const PagedCache& c, const PagedBatch& b, const Task& t, int i) {
+    if (i >= t.b1) return Blk{0, kAll, 0, 0, 0};                    // hidden: any page will do
+    const int P = b.prefix, PB = (P + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
+    const bool pre = vb < PB;
+    const unsigned o = pre ? vb : vb - PB, at = unit_div(o, c.magic), u = o - at * c.unit;
+    Blk r{-1, (pre ? 0 : P) + 16 * (int)o, pre ? min(16, P - 16 * (int)o) : 16, u * kPageUnit, u};
+    if (pre || at < (unsigned)b.width) {
+        r.id = ld_uniform((pre ? b.prefix_table : t.table) + at);
+        if ((unsigned)r.id >= (unsigned)c.n_pages) r.id = -1;
+    }
+    return r;
+}
+__device__ __forceinline__ bool whole(const Blk& x, const Task& t, const WinArgs& a) {
+    return x.nv == 16 && x.j0 + 15 <= t.lo && (x.j0 > t.hi - a.W || x.j0 + 15 < a.S);
+}
+
+// The tasks, numbered sequence by sequence: (row block from the last on, chunk, key/value head).  How many there are
+// only the device knows; whoever asks for rising numbers walks the sequences once.
+struct Tasks {
+    int base = 0;                             // the sequences before it hold `done` tasks
+    int64_t done = 0;
+
+    __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, int64_t task, Task& t) {
+        const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
+        const int lane = threadIdx.x & 63, PB = (b.prefix + 15) >> 4;
+        for (; base < b.B; base += 64) {
+            Seq q{0, 0, 0};
+            if (base + lane < b.B) q = seq_at(b, base + lane);
+            const int nb = (int)(((int64_t)q.n * a.per + a.RT - 1) / a.RT);
+            // chunks of its blocks of rows at most
+            int most = PB + (int)((min(max((int64_t)q.first + q.n, (int64_t)0), cap) + 15) >> 4);
+            if (a.W < kAll) most = min(most, (int)(((int64_t)a.W + a.RT / a.per + 2 + 15) / 16 + 3 + ((int64_t)a.S + 15) / 16));
+            const int nc = chunks_of(most, a.CT);
+            const int64_t mine = (int64_t)nb * nc * c.G;
+            int64_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const int64_t v = __shfl_up(upto, o);
+                if (lane >= o) upto += v;
+            }
+            const unsigned long long over = __ballot(done + upto > task);
+            if (!over) {
+                done += (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32) |
+                                  (unsigned)__builtin_amdgcn_readlane((int)upto, 63));
+                continue;
+            }
+            const int hit = __ffsll(over) - 1, sq = base + hit;
+            const int64_t at64 = task - (done + upto - mine);
+            const unsigned rest_lo = (unsigned)__builtin_amdgcn_readlane((int)at64, hit), rest_hi = (unsigned)__builtin_amdgcn_readlane((int)(at64 >> 32), hit);
+            const uint64_t rest = (uint64_t)rest_hi << 32 | rest_lo;
+            const int n = __builtin_amdgcn_readlane(q.n, hit), first = __builtin_amdgcn_readlane(q.first, hit);
+            const int ncs = __builtin_amdgcn_readlane(nc, hit), blocks = __builtin_amdgcn_readlane(nb, hit);
+            t.g = (int)(rest % (unsigned)c.G);
+            const uint64_t rc = rest / (unsigned)c.G;
+            const int ch = (int)(rc % (unsigned)ncs), rb = blocks - 1 - (int)(rc / (unsigned)ncs);
+            t.table = b.table + sq * b.table_stride;
+            t.tok0 = __builtin_amdgcn_readlane(q.start, hit);
+            t.pos0 = b.prefix + first;
+            t.r0 = rb * a.RT;
+            t.rows = (int)min((int64_t)a.RT, (int64_t)n * a.per - t.r0);
+            t.lo = t.position(0, a.per);
+            t.hi = t.position(t.rows - 1, a.per);
+            t.s = seen(b, cap, a.W, a.S, t.lo, t.hi);
+            t.splits = chunks_of(t.s.n, a.CT);
+            t.split = ch;
+            const int tiles = (t.s.n + 1) / 2, each = (tiles + t.splits - 1) / t.splits;
+            t.b0 = 2 * ch * each;
+            t.b1 = min(t.s.n, t.b0 + 2 * each);
+            t.low = max(t.lo, b.prefix) - a.W;
+            if (t.lo < b.prefix) t.lo = -1;
+            return true;
+        }
+        return false;
+    }
+};
+
+// ---- a wave's rows
+
+// NR tiles of 16 rows: output (transposed, lane = row), reference of the exponent and the lane's share of the sum.
+template <bool BF, bool Q8, int D, int NR>
+struct Rows {
+    static constexpr int E = D / 16;
+    static constexpr float high = BF ? 0x1p-28f : 0x1p15f;          // 2^kTop
+    static constexpr bool JOINT = Q8 && !BF;  // the weights hold the values' scale
+    f32x4 o[NR][E];
+    float ref[NR], sum[NR];                   // weights are 2^(c * score (+ e) - ref)
+    int hi[NR];                               // the lane's rows' positions; -1: they see nothing
+
+    __device__ __forceinline__ void start(const Task& t, int P, int per, int row0) {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            const int i = row0 + rt * 16 + (threadIdx.x & 15), p = t.position(i, per);
+            hi[rt] = i < t.rows && p >= P ? p : -1;
+            ref[rt] = kNone, sum[rt] = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    static __device__ __forceinline__ bool sees(int j, int hi, const WinArgs& a) { return j <= hi && (j > hi - a.W || j < a.S); }
+    // the scores of what the lane's row does not see
+    __device__ __forceinline__ void hide(int rt, const Blk (&x)[2], f32x4 (&s)[2], const WinArgs& a) const {
+        const int gq = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (4 * gq + i >= x[h].nv || !sees(x[h].j0 + 4 * gq + i, hi[rt], a)) s[h][i] = -INFINITY;
+    }
+    struct Weights {
+        float x[2][4], part, sum;
+        __device__ __forceinline__ void take(const f32x4 (&s)[2], float ref, const float (&ck)[2], const float (&ev)[2]) {
+            float p[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float z = JOINT ? ev[h] - ref : -ref;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], ck[h], z));
+                p[h] = (x[h][0] + x[h][1]) + (x[h][2] + x[h][3]);
+            }
+            part = p[0] + p[1];
+            sum = JOINT ? fmaf(p[0], __builtin_amdgcn_exp2f(-ev[0]), p[1] * __builtin_amdgcn_exp2f(-ev[1])) : part;
+        }
+        __device__ __forceinline__ u32x4 packed() const {
+            return u32x4{pack2<BF>(x[0][0], x[0][1]), pack2<BF>(x[0][2], x[0][3]), pack2<BF>(x[1][0], x[1][1]), pack2<BF>(x[1][2], x[1][3])};
+        }
+    };
+    // A new reference for the lane's row if some weight of its is high: the largest score so far gets the weight
+    // 2^(kTop - kRoom).  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.
+    __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], float part, const float (&ck)[2], const float (&ev)[2]) {
+        part = fmaxf(part, __shfl_xor(part, 16));
+        part = fmaxf(part, __shfl_xor(part, 32));
+        float mx = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            mx = fmaxf(mx, fmaf(fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])), ck[h], JOINT ? ev[h] : 0.f));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float now = part > high ? fmaxf(ref[rt], mx + (kRoom - kTop<BF>)) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
+        ref[rt] = now;
+        sum[rt] *= al;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[rt][e] *= al;
+    }
+    // The weights of 32 positions as operands, and their sums.  No maximum is taken: a lane's sum of 8 tells when some
+    // weight may leave its range, and then, which is rare after the first tiles, the reference is raised.
+    __device__ __forceinline__ void weights(const f32x4 (&s)[NR][2], u32x4 (&p)[NR], const float (&ck)[2], const float (&ev)[2]) {
+        Weights w[NR];
+        bool any = false;
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            w[rt].take(s[rt], ref[rt], ck, ev);
+            any |= w[rt].part > high;
+        }
+        if (__builtin_expect(__any(any), 0))
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt)
+                if (__any(w[rt].part > high)) {
+                    raise(rt, s[rt], w[rt].part, ck, ev);
+                    w[rt].take(s[rt], ref[rt], ck, ev);
+                }
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) sum[rt] += w[rt].sum, p[rt] = w[rt].packed();
+    }
+    // What values that are not finite contribute to the rows that see them: the products' operand has zeros in their
+    // places, since a zero weight would not keep them out of the other rows.
+    __device__ __forceinline__ void add_odd(const PagedCache& c, const Task& t, const Blk (&x)[2], const float (&vs)[2], const WinArgs& a) {
+        const int gq = (threadIdx.x & 63) >> 4;
+        for (int i = 0; i < 32; ++i) {
+            const Blk& y = x[i >> 4];
+            if ((i & 15) >= y.nv || y.id < 0) continue;
+            const int j = y.j0 + (i & 15);
+            const int64_t at = y.id * c.vp + t.g * c.vh + (int64_t)(y.off + (i & 15)) * c.vs;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int col = column_of<Q8, E>(4 * gq + k, e);
+                    float v;
+                    bool odd;
+                    if (Q8) {
+                        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)c.v)[at + col], 0) * (BF ? vs[i >> 4] : 1.f);
+                        odd = !(fabsf(v) < INFINITY) || (BF && !finite16<true>(pack2<true>(v, v)));
+                    } else {
+                        const uint16_t w = c.v[at + col];
+                        odd = !finite16<BF>(w);
+                        v = BF ? __uint_as_float((uint32_t)w << 16) : h2f(w);
+                    }
+                    if (!odd) continue;
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt)
+                        if (sees(j, hi[rt], a)) o[rt][e][k] += v;
+                }
+        }
+    }
+    __device__ __forceinline__ void finish(int64_t end) {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+            sum[rt] += __shfl_xor(sum[rt], 16);
+            sum[rt] += __shfl_xor(sum[rt], 32);
+            if (hi[rt] >= end) sum[rt] = NAN;                       // it sees positions that the table does not hold
+        }
+    }
+};
+
+// The keys and values of two blocks in a wave's registers.
+template <bool BF, bool Q8, int D>
+struct Tile {
+    static constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
+    Keys<BF, Q8, D> k[2];
+    Vals<BF, Q8, E> v[8];
+    uint32_t ks[2], vs[2];                    // scale bytes
+
+    __device__ __forceinline__ void load_k(const PagedCache& c, const PageScales& sc, int g, const Blk (&x)[2]) {
+        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t page = max(x[h].id, 0);
+            const int64_t at = page * c.kp + g * c.kh + (int64_t)x[h].off * c.ks;
+            k[h].load((const char*)c.k + (Q8 ? at : 2 * at), n * (uint32_t)c.ks, gq);
+            if (Q8) ks[h] = sc.k[page * sc.kp + g * sc.kh + x[h].unit];
+        }
+    }
+    __device__ __forceinline__ void load_v(const PagedCache& c, const PageScales& sc, int g, const Blk (&x)[2]) {
+        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t page = max(x[h].id, 0);
+            const int64_t at = page * c.vp + g * c.vh + (int64_t)x[h].off * c.vs;
+            const char* b = (const char*)c.v + (Q8 ? at : 2 * at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * h + i].load(b + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * gq * (uint32_t)c.vs, n);
+            if (Q8) vs[h] = sc.v[page * sc.vp + g * sc.vh + x[h].unit];
+        }
+    }
+};
+
+template <bool BF, bool Q8, int D, int NR>
+__device__ __forceinline__ void load_q(const WinArgs& a, const Task& t, int row0, u32x4 (&q)[NR][(D + 31) / 32]) {
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        const int i = row0 + rt * 16 + n, tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+#pragma unroll
+        for (int s = 0; s < (D + 31) / 32; ++s) {
+            const int d = Keys<BF, Q8, D>::first(s, gq);
+            q[rt][s] = u32x4{0, 0, 0, 0};
+            if (i < t.rows && d < D) q[rt][s] = *(const u32x4*)(a.q + (int64_t)tok * a.qt + h * a.qh + d);
+        }
+    }
+}
+
+// Few rows (16 or 32): the wave takes the tiles b, b + step, ... of the task; the next tile's keys and values come into
+// the registers of this one's as soon as a product has read them.
+template <bool BF, bool Q8, int D, int NR>
+__device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a,
+                                     const Task& t, int at, int step, Rows<BF, Q8, D, NR>& r) {
+    constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
+    const int gq = (threadIdx.x & 63) >> 4;
+    r.start(t, b.prefix, a.per, 0);
+    if (at >= t.b1) return;
+    Tile<BF, Q8, D> x;
+    Blk cur[2] = {look(c, b, t, at), look(c, b, t, at + 1)};
+    x.load_k(c, sc, t.g, cur);
+    x.load_v(c, sc, t.g, cur);
+    Blk nxt[2] = {look(c, b, t, at + step), look(c, b, t, at + step + 1)};
+    u32x4 q[NR][NS];
+    load_q<BF, Q8, D, NR>(a, t, 0, q);
+    const bool several = t.position(0, a.per) != t.hi;
+    for (; at < t.b1; at += step) {
+        const Blk after[2] = {look(c, b, t, at + 2 * step), look(c, b, t, at + 2 * step + 1)};
+        float ck[2] = {a.c, a.c}, ev[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
+        bool bad[2] = {cur[0].id < 0, cur[1].id < 0};
+        if (Q8)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bad[h] |= x.ks[h] == 255 || x.vs[h] == 255;
+                ck[h] = ldexpf(a.c, x.ks[h] == 255 ? 0 : (int)x.ks[h] - 127);
+                ev[h] = x.vs[h] == 255 ? 0.f : (float)value_exp(x.vs[h]);
+                vs[h] = BF ? ldexpf(1.f, (int)ev[h]) : 1.f;
+            }
+        f32x4 s[NR][2];
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 f = x.k[h].get(k);
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) s[rt][h] = mfma16<BF>(f, q[rt][k], s[rt][h]);
+            }
+        if (at + step < t.b1) x.load_k(c, sc, t.g, nxt);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (bad[h])
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) s[rt][h] = f32x4{NAN, NAN, NAN, NAN};
+        const bool part = !whole(cur[0], t, a) || !whole(cur[1], t, a);
+        if (part)
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) r.hide(rt, cur, s[rt], a);
+        u32x4 w[NR];
+        r.weights(s, w, ck, ev);
+        uint32_t v[8][EW];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.v[i].wide(v[i], vs[i >> 2]);
+        if (at + step < t.b1) x.load_v(c, sc, t.g, nxt);
+        bool fine = true;
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = 4 * gq + (i & 3), j = cur[i >> 2].j0 + k;
+                // values that no row sees do not reach the product, whatever they hold
+                const bool some = k < cur[i >> 2].nv && j <= t.hi && (j > t.low || j < a.S) && !bad[i >> 2];
+#pragma unroll
+                for (int m = 0; m < EW; ++m) {
+                    if (!some) v[i][m] = 0;
+                    if (several) v[i][m] = sane<BF>(v[i][m], &fine);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            u32x4 f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], sel);
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(f, w[rt], r.o[rt][e]);
+        }
+        if (part && __any(!fine)) r.add_odd(c, t, cur, vs, a);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) cur[h] = nxt[h], nxt[h] = after[h];
+    }
+}
+
+// the output of one row, columns D / 16 at a time in the lanes' order
+template <bool BF, bool Q8, int E>
+__device__ __forceinline__ void put_out(uint16_t* o, int m, const float (&v)[E]) {
+    if constexpr (E == 1) {
+        o[m] = (uint16_t)pack2<BF>(v[0], 0.f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) *(uint32_t*)(o + column_of<Q8, E>(m, e)) = pack2<BF>(v[e], v[e + 1]);
+    }
+}
+
+template <int D, int NR>
+struct MeetLds {
+    float o[4][16][D + 4];
+    float ml[4][NR * 16][2];
+};
+
+// the four waves' results of a workgroup's task, summed and stored
+template <bool BF, bool Q8, int D, int NR>
+__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t end, Rows<BF, Q8, D, NR>& r, MeetLds<D, NR>& l) {
+    constexpr int E = D / 16;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, n = lane & 15, gq = lane >> 4;
+    r.finish(end);
+    __syncthreads();                          // an earlier task's LDS is read out
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt)
+        if (gq == 0) l.ml[w][rt * 16 + n][0] = r.ref[rt], l.ml[w][rt * 16 + n][1] = r.sum[rt];
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        if (rt * 16 >= t.rows) break;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, l.ml[i][rt * 16 + n][0]);
+        const float f = __builtin_amdgcn_exp2f(r.ref[rt] - top);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) l.o[w][n][column_of<Q8, E>(4 * gq + i, e)] = r.o[rt][e][i] * f;
+        __syncthreads();
+        for (int i = tid; i < 16 * (D / 4); i += kT) {
+            const int rr = i / (D / 4), d = i % (D / 4) * 4, row = rt * 16 + rr;
+            if (row >= t.rows) continue;
+            f32x4 v = *(const f32x4*)&l.o[0][rr][d];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) v += *(const f32x4*)&l.o[k][rr][d];
+            float tp = -INFINITY, sm = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sm += l.ml[k][row][1] * __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp);
+            const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
+            const size_t at = (size_t)tok * a.H + h;
+            if (t.splits > 1) {
+                const size_t slot = at * a.NO + t.split;
+                *(f32x4*)(a.part + slot * D + d) = v;
+                if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
+            } else {
+                const float inv = sm == 0.f ? 0.f : 1.0f / sm;
+                const u32x2 o = {pack2<BF>(v[0] * inv, v[1] * inv), pack2<BF>(v[2] * inv, v[3] * inv)};
+                *(u32x2*)(a.out + (int64_t)tok * a.ot + h * a.oh + d) = o;
+                if (a.lse && d == 0) a.lse[at] = sm == 0.f ? -INFINITY : tp * 0.69314718055994531f + logf(sm);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// One workgroup per task: 16 * NR rows, the four waves on every fourth tile.
+template <bool BF, bool Q8, int D, int NR>
+__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
+    __shared__ MeetLds<D, NR> l;
+    const int64_t end = b.prefix + (int64_t)b.width * c.unit * kPageUnit;
+    Tasks all;
+    for (int64_t task = blockIdx.x;; task += gridDim.x) {
+        Task t;
+        if (!all.find(c, b, a, task, t)) return;
+        if (t.split >= t.splits) continue;    // fewer chunks than the sequence's longest block of rows
+        Rows<BF, Q8, D, NR> r;
+        walk<BF, Q8, D, NR>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
+        meet<BF, Q8, D, NR>(a, t, end, r, l);
+    }
+}
+
+// A wave per row (token, head) joins its chunks: their references and sums in the lanes, a group of lanes (four
+// columns a lane) one chunk each.
+template <bool BF>
+__global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, WinArgs a) {
+    const int lane = threadIdx.x & 63, D = c.D, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= b.T * a.H) return;
+    const int t = row / a.H, h = row % a.H;
+    int64_t place = -1;
+    const int sq = paged_place(b, t, &place);
+    if (sq < 0) return;
+    const Seq q = seq_at(b, sq);
+    if (t - q.start >= q.n) return;           // padding: its output stays as it is
+    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
+    const int64_t rb = ((int64_t)(t - q.start) * a.per + h % a.per) / a.RT;
+    const int lo = (int)(rb * a.RT / a.per), hi = (int)min((rb * a.RT + a.RT - 1) / a.per, (int64_t)q.n - 1);
+    const int n = chunks_of(seen(b, cap, a.W, a.S, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
+    if (n == 1) return;                       // finished where it was computed
+    const float* ml = a.ml + (size_t)row * a.NO * 2;
+    const float* part = a.part + (size_t)row * a.NO * D;
+    const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float top = kNone, sum = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        float2 v = {kNone, 0.f};
+        if (i0 + lane < n) v = *(const float2*)(ml + 2 * (i0 + lane));
+        float tp = fmaxf(top, v.x);
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) tp = fmaxf(tp, __shfl_xor(tp, o));
+        const float old = __builtin_amdgcn_exp2f(top - tp), f = __builtin_amdgcn_exp2f(v.x - tp);
+        float s = v.y * f;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) s += __shfl_xor(s, o);
+        sum = fmaf(sum, old, s);
+        acc *= old;
+        top = tp;
+        const int m = min(64, n - i0);
+        for (int k0 = 0; k0 < m; k0 += 4 * groups) {
+            f32x4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + j * groups + g;
+                x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (k < m && d < D) x[j] = *(const f32x4*)(part + (size_t)(i0 + k) * D + d);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float fk = __shfl(f, min(k0 + j * groups + g, 63));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[j][e], fk, acc[e]);
+            }
+        }
+    }
+    for (int o = gl; o < 64; o *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    if (g == 0 && d < D) {
+        const u32x2 r = {pack2<BF>(acc[0] * inv, acc[1] * inv), pack2<BF>(acc[2] * inv, acc[3] * inv)};
+        *(u32x2*)(a.out + (int64_t)t * a.ot + h * a.oh + d) = r;
+    }
+    if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
+}
+
+struct Plan {
+    int nr, RT, NO, CT;
+    int64_t tasks;
+};
+
+int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan* p) {
+    const int per = H / c.G;
+    const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
+    if (rows * c.G > kRowsMax) return LOOPSPEC_EINVAL;
+    p->nr = each > 16 ? 2 : 1;
+    p->RT = 16 * p->nr;
+    // blocks of 16 positions that a block of rows may see
+    int64_t most = (b.prefix + 15) / 16 + (int64_t)b.width * c.unit;
+    if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
+    const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
+    const int64_t blocks = std::min(rows, (rows + p->RT - 1) / p->RT + b.B) * c.G;
+    // about 1024 tasks where the tables are full, of at least two tiles a wave
+    p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(8, tiles * blocks / 1024));
+    p->NO = (int)((tiles + p->CT - 1) / p->CT);
+    p->tasks = blocks * p->NO;
+    return LOOPSPEC_OK;
+}
+
+uint64_t bytes_of(const PagedCache& c, const PagedBatch& b, int H, const Plan& p) {
+    return p.NO > 1 ? (uint64_t)b.T * H * p.NO * (c.D + 2) * 4 : 0;
+}
+
+int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales, const loopspec_paged_batch* batch, int n_heads,
+          int window, int sinks, PagedCache* c, PageScales* s, PagedBatch* b, Plan* p) {
+    int rc = paged_args(cache, batch, c, b);
+    if (rc) return rc;
+    *s = PageScales{};
+    if (scales && (rc = scale_args(cache, scales, s))) return rc;
+    if (n_heads < 1 || n_heads > (1 << 16) || n_heads % c->G) return LOOPSPEC_EINVAL;
+    if (window < 0 || sinks < 0) return LOOPSPEC_EINVAL;
+    if (b->prefix > 0 && !b->prefix_table) return LOOPSPEC_EINVAL;
+    if (!b->B || !b->T) return LOOPSPEC_OK;
+    return plan_of(*c, *b, n_heads, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p);
+}
+
+template <bool BF, bool Q8, int D>
+const void* kernel_of(const Plan& p) {
+    return p.nr == 1 ? (const void*)k_window<BF, Q8, D, 1> : (const void*)k_window<BF, Q8, D, 2>;
+}
+template <bool BF, bool Q8>
+const void* kernel_of(int D, const Plan& p) {
+    switch (D) {
+        case 16: return kernel_of<BF, Q8, 16>(p);
+        case 32: return kernel_of<BF, Q8, 32>(p);
+        case 64: return kernel_of<BF, Q8, 64>(p);
+        case 96: return kernel_of<BF, Q8, 96>(p);
+        default: return kernel_of<BF, Q8, 128>(p);
+    }
+}
+
+}  // namespace
+}  // namespace ls
+
+extern "C" {
+
+uint64_t loopspec_window_attention_workspace_bytes(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
+                                                   const loopspec_paged_batch* batch, int32_t n_heads, int32_t window,
+                                                   int32_t sinks) {
+    ls::PagedCache c;
+    ls::PageScales s;
+    ls::PagedBatch b;
+    ls::Plan p{};
+    if (ls::check(cache, scales, batch, n_heads, window, sinks, &c, &s, &b, &p)) return 0;
+    if (!b.B || !b.T) return 0;
+    return ls::bytes_of(c, b, n_heads, p);
+}
+
+int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
+                              const loopspec_paged_batch* batch, const loopspec_attention_args* args, int32_t window,
+                              int32_t sinks, void* workspace_dev, uint64_t workspace_bytes, void* stream) {
+    using namespace ls;
+    PagedCache c;
+    PageScales s;
+    PagedBatch b;
+    Plan p{};
+    if (!args) return LOOPSPEC_EINVAL;
+    const int rc = check(cache, scales, batch, args->n_heads, window, sinks, &c, &s, &b, &p);
+    if (rc) return rc;
+    const float cs = args->scale * 1.44269504088896341f;
+    if (!(args->scale > 0.f) || !(cs < 3e38f)) return LOOPSPEC_EINVAL;
+    if (!b.B || !b.T) return LOOPSPEC_OK;     // (empty tensors have no address)
+    if (!rows_ok(args->q_dev, args->q_token, args->q_head) || !rows_ok(args->out_dev, args->out_token, args->out_head)) return LOOPSPEC_EINVAL;
+    if ((args->n_heads > 1 && args->out_head < c.D) || (b.T > 1 && args->out_token < c.D)) return LOOPSPEC_EINVAL;
+    const uint64_t need = bytes_of(c, b, args->n_heads, p);
+    if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
+    const uint64_t rows = (uint64_t)b.T * args->n_heads;
+    WinArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
+              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.NO * c.D, cs, args->n_heads,
+              args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT};
+    hipStream_t st = (hipStream_t)stream;
+    const bool bf = cache->dtype == LOOPSPEC_BF16, q8 = scales != nullptr;
+    void* kargs[] = {&c, &s, &b, &a};
+    const void* f = bf ? q8 ? kernel_of<true, true>(c.D, p) : kernel_of<true, false>(c.D, p)
+                       : q8 ? kernel_of<false, true>(c.D, p) : kernel_of<false, false>(c.D, p);
+    if (hipLaunchKernel(f, dim3((unsigned)std::min<int64_t>(p.tasks, 16384)), dim3(kT), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    if (p.NO > 1) {
+        void* jargs[] = {&c, &b, &a};
+        const void* j = bf ? (const void*)k_window_join<true> : (const void*)k_window_join<false>;
+        if (hipLaunchKernel(j, dim3((unsigned)((rows + 3) / 4)), dim3(kT), jargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    }
+    return LOOPSPEC_OK;
+}
+
+}  // extern "C"

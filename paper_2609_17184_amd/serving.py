@@ -46,6 +46,12 @@ def _size(n: int, what: str) -> int:
     return n
 
 
+def _whole(n, what: str) -> int:
+    n = operator.index(n)
+    _need(n >= 0, f"{what}: not below zero")
+    return n
+
+
 def _ints(t, shape, device, what: str):
     import torch
     _need(t.dtype == torch.int32 and t.device == device and t.dim() == len(shape) and t.stride(-1) == 1
@@ -85,6 +91,43 @@ class PagedCache:
                                 v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
         self._ref = ctypes.byref(self._c)
 
+    _scales_ref = None
+
+    def _for(self, dtype):
+        return self._ref
+
+
+class QuantizedCache:
+    """Pages of keys and values in 8 bits: float8_e4m3fn codes k, v [n_pages, n_kv_heads, page_size, head_dim] and
+    float8_e8m0fnu scales k_scale, v_scale [n_pages, n_kv_heads, page_size / 16], one for 16 positions of a head; an
+    element stands for code * scale.  The last strides are 1, the codes' others multiples of 16.  Sizes as in PagedCache;
+    queries are float16 or bfloat16.  Scales of pages that hold nothing yet do not matter."""
+
+    dtype = None                              # (the queries' decides)
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        _need(k.dim() == 4 and k.shape == v.shape, "keys and values: [n_pages, n_kv_heads, page_size, head_dim] alike")
+        _need(k.dtype == v.dtype == torch.float8_e4m3fn, "keys and values: float8_e4m3fn")
+        _need(k_scale.dtype == v_scale.dtype == torch.float8_e8m0fnu, "scales: float8_e8m0fnu")
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = (_size(n, "keys and values") for n in k.shape)
+        blocks = (self.n_pages, self.n_kv_heads, self.page_size // 16)
+        _need(k_scale.shape == v_scale.shape == blocks, "scales: [n_pages, n_kv_heads, page_size / 16]")
+        _need(k.is_cuda and k.device == v.device == k_scale.device == v_scale.device, "keys, values and scales: on one GPU")
+        _need(k.stride(3) == 1 and v.stride(3) == 1, "keys and values: elements of a head next to each other")
+        _need(blocks[2] < 2 or k_scale.stride(2) == v_scale.stride(2) == 1, "scales: those of a page next to each other")
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self._scales = B.PageScalesC(k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride()[:2], *v_scale.stride()[:2])
+        self._scales_ref = ctypes.byref(self._scales)
+        self._by_type = {t: B.PagedCacheC(d, *k.shape[:1], self.page_size, self.n_kv_heads, self.head_dim, k.data_ptr(),
+                                          v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
+                         for t, d in ((torch.float16, B.F16), (torch.bfloat16, B.BF16))}
+
+    def _for(self, dtype):
+        if dtype not in self._by_type:
+            raise ValueError("queries of an 8-bit cache: float16 or bfloat16")
+        return ctypes.byref(self._by_type[dtype])
+
 
 class Batch:
     """The sequences of a step.  seq_len [n]: own positions of each, with this step's tokens; table [n, pages]: their
@@ -116,18 +159,18 @@ def rope_frequencies(rot_dim: int, base: float = 1e4, device="cuda:0"):
     return base ** (-torch.arange(rot_dim // 2, dtype=torch.float64, device=device) * 2 / rot_dim)
 
 
-def _rows(t, heads: int, cache: PagedCache, tokens: int, what: str):
-    if not (t.shape == (tokens, heads, cache.head_dim) and t.dtype is cache.dtype and t.device == cache.device
+def _rows(t, heads: int, cache, tokens: int, what: str, dtype):
+    if not (t.shape == (tokens, heads, cache.head_dim) and t.dtype is dtype and t.device == cache.device
             and t.stride(2) == 1):
         raise ValueError(f"{what}: [tokens, heads, head_dim] of the cache's type and device, elements adjacent")
 
 
-def _heads(q, cache: PagedCache):
+def _heads(q, cache):
     """(tokens, heads) of the queries."""
     if q.dim() != 3:
         raise ValueError("q: [tokens, heads, head_dim]")
     tokens, heads, _ = q.shape
-    _rows(q, heads, cache, _size(tokens, "q"), "q")
+    _rows(q, heads, cache, _size(tokens, "q"), "q", cache.dtype or q.dtype)
     return tokens, _size(heads, "q")
 
 
@@ -136,21 +179,22 @@ def _like(q):
     return torch.empty_like(q, memory_format=torch.contiguous_format)
 
 
-def rope_append(q, k, v, cache: PagedCache, batch: Batch, freq=None, q_norm=None, k_norm=None, eps: float = 1e-6,
-                out=None):
+def rope_append(q, k, v, cache, batch: Batch, freq=None, q_norm=None, k_norm=None, eps: float = 1e-6, out=None):
     """Normalise (optional gains q_norm, k_norm: float32 [head_dim]) and rotate the queries and keys of a step's
     tokens, and append keys and values to their sequences' pages.  q [tokens, n_heads, head_dim], k and v [tokens,
     n_kv_heads, head_dim] (views of a fused projection are fine); freq float64 [rot_dim / 2] radians per position
     (None: no rotation), the first rot_dim elements of a head being rotated in halves.  Returns the queries: `out`
-    (which may be q) or a new tensor, whose padding rows are then undefined."""
+    (which may be q) or a new tensor, whose padding rows are then undefined.  Into a QuantizedCache keys and values go
+    as codes: a block of 16 positions has the power of two that holds its largest magnitude within 448, and keeps the
+    one of positions it holds already where that is larger."""
     import torch
     tokens, heads = _heads(q, cache)
-    _rows(k, cache.n_kv_heads, cache, tokens, "k")
-    _rows(v, cache.n_kv_heads, cache, tokens, "v")
+    _rows(k, cache.n_kv_heads, cache, tokens, "k", q.dtype)
+    _rows(v, cache.n_kv_heads, cache, tokens, "v", q.dtype)
     if out is None:
         out = _like(q)
     else:
-        _rows(out, heads, cache, tokens, "out")
+        _rows(out, heads, cache, tokens, "out", q.dtype)
     rot = 0
     if freq is not None:
         _need(freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous() and freq.device == cache.device,
@@ -164,9 +208,19 @@ def rope_append(q, k, v, cache: PagedCache, batch: Batch, freq=None, q_norm=None
                    k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
                    None if freq is None else freq.data_ptr(), None if q_norm is None else q_norm.data_ptr(),
                    None if k_norm is None else k_norm.data_ptr())
-    _check(_launch(cache.device, B.load_library().loopspec_rope_append, cache._ref, batch._with(tokens, cache),
-                   ctypes.byref(a)), "loopspec_rope_append")
+    L, ref, more = B.load_library(), batch._with(tokens, cache), ctypes.byref(a)
+    if cache._scales_ref is None:
+        _check(_launch(cache.device, L.loopspec_rope_append, cache._ref, ref, more), "loopspec_rope_append")
+    else:
+        _check(_launch(cache.device, L.loopspec_rope_append_quantized, cache._for(q.dtype), cache._scales_ref, ref, more),
+               "loopspec_rope_append_quantized")
     return out
+
+
+def _prefix_held(cache, batch: Batch):
+    if batch.prefix_len and (batch.prefix_table is None
+                             or batch.prefix_table.shape[0] * cache.page_size < batch.prefix_len):
+        raise ValueError("prefix_table: a page for every page_size positions of the prefix")
 
 
 def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] = None, out=None,
@@ -176,15 +230,14 @@ def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] 
     tensor whose padding rows are undefined), with return_lse also the log of each row's sum of exp(score) (float32
     [tokens, n_heads])."""
     import torch
+    _need(isinstance(cache, PagedCache), "prefix_attention: 16-bit pages (window_attention takes both)")
     tokens, heads = _heads(q, cache)
     if out is None:
         out = _like(q)
     else:
-        _rows(out, heads, cache, tokens, "out")
+        _rows(out, heads, cache, tokens, "out", q.dtype)
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
-    if batch.prefix_len and (batch.prefix_table is None
-                             or batch.prefix_table.shape[0] * cache.page_size < batch.prefix_len):
-        raise ValueError("prefix_table: a page for every page_size positions of the prefix")
+    _prefix_held(cache, batch)
     L, ref = B.load_library(), batch._with(tokens, cache)
     nbytes = L.loopspec_prefix_attention_workspace_bytes(cache._ref, ref, heads)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
@@ -194,6 +247,64 @@ def prefix_attention(q, cache: PagedCache, batch: Batch, scale: Optional[float] 
     _check(_launch(cache.device, L.loopspec_prefix_attention, cache._ref, ref, ctypes.byref(a), ws.data_ptr(), nbytes),
            "loopspec_prefix_attention")
     return (out, lse) if return_lse else out
+
+
+def window_attention(q, cache, batch: Batch, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out=None,
+                     return_lse: bool = False):
+    """Attention of a step's queries [tokens, n_heads, head_dim] over 16-bit or 8-bit pages.  The token at position p
+    (counted through the prefix) sees the positions j <= p with p - j < window or j < sinks; window 0: all of them.
+    Arguments and results as in prefix_attention; a token before its sequence's first position gives zeros."""
+    import torch
+    tokens, heads = _heads(q, cache)
+    if out is None:
+        out = _like(q)
+    else:
+        _rows(out, heads, cache, tokens, "out", q.dtype)
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    _prefix_held(cache, batch)
+    # (a window or sinks beyond all positions are those of all positions)
+    window, sinks = (min(_whole(n, what), 1 << 30) for n, what in ((window, "window"), (sinks, "sinks")))
+    L, ref, c = B.load_library(), batch._with(tokens, cache), cache._for(q.dtype)
+    nbytes = L.loopspec_window_attention_workspace_bytes(c, cache._scales_ref, ref, heads, window, sinks)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+    a = B.AttentionArgs(heads, 1.0 / math.sqrt(cache.head_dim) if scale is None else scale, q.data_ptr(), q.stride(0),
+                        q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
+                        None if lse is None else lse.data_ptr())
+    _check(_launch(cache.device, L.loopspec_window_attention, c, cache._scales_ref, ref, ctypes.byref(a), window, sinks,
+                   None if ws is None else ws.data_ptr(), nbytes), "loopspec_window_attention")
+    return (out, lse) if return_lse else out
+
+
+def fork_pages(seq_len, table, parent, refs, caches, prefix_len: int = 0, window: int = 0, sinks: int = 0, room: int = 0):
+    """A batch whose row i continues row parent[i] (int32 [children]; outside the rows: none) of the batch seq_len
+    [rows], table [rows, pages] over the caches of all layers (PagedCache or QuantizedCache, of equal n_pages and
+    page_size).  refs [n_pages]: how many entries name a page (a prefix's pages have theirs from the caller).  A row's
+    first child takes its pages over, others share the full ones and get a copy of what the last one holds; pages without
+    a child, or that the next position does not see (window, sinks), are let go; every child then holds pages for
+    `room` more positions.  table's entries without a page lie outside the cache (-1), also those behind a row's last
+    page.  Returns (seq_len, table, refs, short), new int32 tensors: short [1] counts the pages that were not to be had,
+    whose entries are -1."""
+    import torch
+    caches = list(caches)
+    _need(bool(caches), "caches: one or more")
+    dev, n_pages, page_size = caches[0].device, caches[0].n_pages, caches[0].page_size
+    _need(all(c.device == dev and c.n_pages == n_pages and c.page_size == page_size for c in caches),
+          "caches: on one device, of equal n_pages and page_size")
+    n, m = _size(seq_len.shape[0], "seq_len"), _size(parent.shape[0], "parent")
+    made = [torch.empty(shape, dtype=torch.int32, device=dev) for shape in ((m,), (m, table.shape[-1]), (n_pages,), (1,))]
+    a = B.ForkArgs(n, m, page_size, n_pages, _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table"),
+                   table.stride(0), _size(table.shape[1], "table"), _ints(parent, (m,), dev, "parent"),
+                   _ints(refs, (n_pages,), dev, "refs"), *(min(_whole(x, what), 1 << 30) for x, what in
+                                                           ((prefix_len, "prefix_len"), (window, "window"), (sinks, "sinks"), (room, "room"))),
+                   made[0].data_ptr(), made[1].data_ptr(), made[1].stride(0), made[2].data_ptr(), made[3].data_ptr())
+    L = B.load_library()
+    cs = (B.PagedCacheC * len(caches))(*(c._for(torch.float16)._obj for c in caches))
+    sc = (B.PageScalesC * len(caches))(*(B.PageScalesC() if c._scales_ref is None else c._scales for c in caches))
+    nbytes = L.loopspec_fork_pages_workspace_bytes(m, n_pages)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _check(_launch(dev, L.loopspec_fork_pages, ctypes.byref(a), cs, sc, len(caches), ws.data_ptr(), nbytes),
+           "loopspec_fork_pages")
+    return tuple(made)
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
