@@ -35,7 +35,9 @@ namespace {
 
 constexpr int kT = 256;
 constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
+constexpr int kGroupsMax = 1 << 23;            // workgroups of the prefix, for the same reason
 constexpr int kAll = 1 << 30;                 // a window that holds every position
+constexpr int kNowhere = INT32_MIN;
 constexpr float kNone = -3e38f;               // the reference before the first score
 constexpr float kRoom = 8.0f;                  // octaves that a weight may rise above the one that set the reference
 template <bool BF>
@@ -47,13 +49,15 @@ struct WinArgs {
     uint16_t* out;
     int64_t ot, oh;
     float* lse;
-    float* part;                              // [rows][NO][D], rows = tokens x heads
-    float* ml;                                // [rows][NO][2]: reference (base 2), sum
+    float* part;                              // [rows][NP + NO][D], rows = tokens x heads
+    float* ml;                                // [rows][NP + NO][2]: reference (base 2), sum
     float c;                                  // scale * log2(e)
     int H, per;                               // query heads; per key/value head
     int W, S;                                 // window (kAll: none), sinks
     int RT;                                   // rows of a block
     int NO, CT;                               // chunks at most, tiles of 32 positions per chunk
+    int NP, CP;                               // the prefix for the rows of all sequences at once: chunks (0: it is not), tiles per chunk
+    int rb, rows, ptasks;                     // blocks of these rows, rows of a block, workgroups
 };
 
 // ---- 8-bit operands
@@ -193,13 +197,15 @@ struct Seen {
     int head, from, n;
 };
 __device__ __forceinline__ int block_of(int j, int P, int PB) { return j < P ? j >> 4 : PB + ((j - P) >> 4); }
-__device__ __forceinline__ Seen seen(const PagedBatch& b, int64_t cap, int W, int S, int lo, int hi) {
+__device__ __forceinline__ Seen seen(const PagedBatch& b, const WinArgs& a, int64_t cap, int lo, int hi) {
     const int P = b.prefix, PB = (P + 15) >> 4;
     hi = (int)min((int64_t)hi, P + cap - 1);
     lo = max(lo, P);
-    if (hi < lo && hi < P) return Seen{0, 0, 0};     // (behind the table's end lo may pass hi)
-    const int from = block_of(min(max(lo - W + 1, 0), hi), P, PB), to = block_of(hi, P, PB) + 1;
-    const int head = S > 0 ? min(block_of(min(S - 1, hi), P, PB) + 1, from) : 0;
+    if (hi < P) return Seen{0, 0, 0};         // (behind the table's end lo may pass hi)
+    const int to = block_of(hi, P, PB) + 1;
+    if (a.NP) return Seen{0, PB, to - PB};
+    const int from = block_of(min(max(lo - a.W + 1, 0), hi), P, PB);
+    const int head = a.S > 0 ? min(block_of(min(a.S - 1, hi), P, PB) + 1, from) : 0;
     return Seen{head, from, head + to - from};
 }
 __device__ __forceinline__ int chunks_of(int n, int CT) { return max(1, ((n + 1) / 2 + CT - 1) / CT); }
@@ -208,35 +214,47 @@ struct Task {
     const int32_t* table;
     int b0, b1;                               // its part of the list of blocks (b1 is the list's end or even)
     int g, tok0, r0, rows;                    // row r of the block: row r0 + r of the tokens from tok0 (r < rows)
-    int pos0;                                 // position of token tok0
+    int pos0;                                 // position of token tok0; kNowhere: all rows stand at hi
     int lo, hi;                               // of the first and last row (lo -1: some rows see nothing)
     int low;                                  // positions above it (or below the sinks) are seen by some row
     Seen s;
-    int split, splits;
+    int split, splits;                        // where the partial results go; 1: the results are whole
 
     __device__ __forceinline__ int token(int r, int per) const { return tok0 + (r0 + r) / per; }
-    __device__ __forceinline__ int position(int r, int per) const { return pos0 + (r0 + r) / per; }
+    __device__ __forceinline__ int position(int r, int per) const { return pos0 == kNowhere ? hi : pos0 + (r0 + r) / per; }
 };
 
-// 16 positions of a task's list
+// 16 positions of a task's list: the first one and how many there are (0: behind the list's end)
 struct Blk {
-    int id, j0, nv;                           // page (-1: none of the cache's), first position, how many there are
-    unsigned off, unit;                       // position and block in the page
+    int j0, nv;
 };
-__device__ __forceinline__ Blk look(const PagedCache& c, const PagedBatch& b, const Task& t, int i) {
-    if (i >= t.b1) return Blk{0, kAll, 0, 0, 0};                    // hidden: any page will do
+__device__ __forceinline__ Blk look(const PagedBatch& b, const Task& t, int i) {
+    if (i >= t.b1) return Blk{kAll, 0};
     const int P = b.prefix, PB = (P + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
+    return vb < PB ? Blk{16 * vb, min(16, P - 16 * vb)} : Blk{P + 16 * (vb - PB), 16};
+}
+// where they are: page (-1: none of the cache's; any page will do behind the list's end) and block of the page
+struct Place {
+    int id, unit;
+};
+__device__ __forceinline__ Place place(const PagedCache& c, const PagedBatch& b, const Task& t, int i) {
+    if (i >= t.b1) return Place{0, 0};
+    const int PB = (b.prefix + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
     const bool pre = vb < PB;
-    const unsigned o = pre ? vb : vb - PB, at = unit_div(o, c.magic), u = o - at * c.unit;
-    Blk r{-1, (pre ? 0 : P) + 16 * (int)o, pre ? min(16, P - 16 * (int)o) : 16, u * kPageUnit, u};
+    const unsigned o = pre ? vb : vb - PB, at = unit_div(o, c.magic);
+    Place r{-1, (int)(o - at * c.unit)};
     if (pre || at < (unsigned)b.width) {
         r.id = ld_uniform((pre ? b.prefix_table : t.table) + at);
         if ((unsigned)r.id >= (unsigned)c.n_pages) r.id = -1;
     }
     return r;
 }
-__device__ __forceinline__ bool whole(const Blk& x, const Task& t, const WinArgs& a) {
-    return x.nv == 16 && x.j0 + 15 <= t.lo && (x.j0 > t.hi - a.W || x.j0 + 15 < a.S);
+// all rows from position lo to hi see all of it; none of them sees any of it
+__device__ __forceinline__ bool whole(const Blk& x, int lo, int hi, const WinArgs& a) {
+    return x.nv == 16 && x.j0 + 15 <= lo && (x.j0 > hi - a.W || x.j0 + 15 < a.S);
+}
+__device__ __forceinline__ bool hidden(const Blk& x, int lo, int hi, const WinArgs& a) {
+    return x.nv == 0 || x.j0 > hi || (x.j0 + 15 <= lo - a.W && x.j0 >= a.S);
 }
 
 // The tasks, numbered sequence by sequence: (row block from the last on, chunk, key/value head).  How many there are
@@ -253,7 +271,7 @@ struct Tasks {
             if (base + lane < b.B) q = seq_at(b, base + lane);
             const int nb = (int)(((int64_t)q.n * a.per + a.RT - 1) / a.RT);
             // chunks of its blocks of rows at most
-            int most = PB + (int)((min(max((int64_t)q.first + q.n, (int64_t)0), cap) + 15) >> 4);
+            int most = (a.NP ? 0 : PB) + (int)((min(max((int64_t)q.first + q.n, (int64_t)0), cap) + 15) >> 4);
             if (a.W < kAll) most = min(most, (int)(((int64_t)a.W + a.RT / a.per + 2 + 15) / 16 + 3 + ((int64_t)a.S + 15) / 16));
             const int nc = chunks_of(most, a.CT);
             const int64_t mine = (int64_t)nb * nc * c.G;
@@ -285,10 +303,10 @@ struct Tasks {
             t.rows = (int)min((int64_t)a.RT, (int64_t)n * a.per - t.r0);
             t.lo = t.position(0, a.per);
             t.hi = t.position(t.rows - 1, a.per);
-            t.s = seen(b, cap, a.W, a.S, t.lo, t.hi);
-            t.splits = chunks_of(t.s.n, a.CT);
-            t.split = ch;
-            const int tiles = (t.s.n + 1) / 2, each = (tiles + t.splits - 1) / t.splits;
+            t.s = seen(b, a, cap, t.lo, t.hi);
+            const int n_chunks = chunks_of(t.s.n, a.CT), tiles = (t.s.n + 1) / 2, each = (tiles + n_chunks - 1) / n_chunks;
+            t.splits = a.NP + n_chunks;
+            t.split = a.NP + ch;
             t.b0 = 2 * ch * each;
             t.b1 = min(t.s.n, t.b0 + 2 * each);
             t.low = max(t.lo, b.prefix) - a.W;
@@ -298,6 +316,26 @@ struct Tasks {
         return false;
     }
 };
+
+// the prefix's tasks: the blocks of rows of one chunk follow each other on one XCD (workgroups go round the 8 XCDs)
+__device__ __forceinline__ bool prefix_task(const PagedCache& c, const PagedBatch& b, const WinArgs& a, Task& t) {
+    const int j = blockIdx.x / 8, pair = j / a.rb * 8 + blockIdx.x % 8, rb = j % a.rb, PB = (b.prefix + 15) >> 4;
+    if (pair >= c.G * a.NP) return false;
+    t.table = nullptr;
+    t.g = pair % c.G;
+    t.split = pair / c.G;
+    t.splits = a.NP + 1;
+    t.s = Seen{0, 0, PB};
+    t.b0 = 2 * t.split * a.CP;
+    t.b1 = min(PB, t.b0 + 2 * a.CP);
+    t.tok0 = 0;
+    t.r0 = rb * a.rows;
+    t.rows = min(a.rows, b.T * a.per - t.r0);
+    t.pos0 = kNowhere;
+    t.lo = t.hi = b.prefix - 1;
+    t.low = t.lo - a.W;
+    return true;
+}
 
 // ---- a wave's rows
 
@@ -315,7 +353,7 @@ struct Rows {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
             const int i = row0 + rt * 16 + (threadIdx.x & 15), p = t.position(i, per);
-            hi[rt] = i < t.rows && p >= P ? p : -1;
+            hi[rt] = i < t.rows && (p >= P || t.pos0 == kNowhere) ? p : -1;
             ref[rt] = kNone, sum[rt] = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -388,13 +426,15 @@ struct Rows {
     }
     // What values that are not finite contribute to the rows that see them: the products' operand has zeros in their
     // places, since a zero weight would not keep them out of the other rows.
-    __device__ __forceinline__ void add_odd(const PagedCache& c, const Task& t, const Blk (&x)[2], const float (&vs)[2], const WinArgs& a) {
+    __device__ __forceinline__ void add_odd(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a, const Task& t, int at) {
         const int gq = (threadIdx.x & 63) >> 4;
         for (int i = 0; i < 32; ++i) {
-            const Blk& y = x[i >> 4];
-            if ((i & 15) >= y.nv || y.id < 0) continue;
+            const Blk y = look(b, t, at + (i >> 4));
+            const Place w = place(c, b, t, at + (i >> 4));
+            if ((i & 15) >= y.nv || w.id < 0) continue;
             const int j = y.j0 + (i & 15);
-            const int64_t at = y.id * c.vp + t.g * c.vh + (int64_t)(y.off + (i & 15)) * c.vs;
+            const int64_t from = w.id * c.vp + t.g * c.vh + (int64_t)(16 * w.unit + (i & 15)) * c.vs;
+            const float scale = Q8 && BF ? ldexpf(1.f, value_exp(sc.v[w.id * sc.vp + t.g * sc.vh + w.unit])) : 1.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -403,12 +443,12 @@ struct Rows {
                     float v;
                     bool odd;
                     if (Q8) {
-                        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)c.v)[at + col], 0) * (BF ? vs[i >> 4] : 1.f);
+                        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)c.v)[from + col], 0) * scale;
                         odd = !(fabsf(v) < INFINITY) || (BF && !finite16<true>(pack2<true>(v, v)));
                     } else {
-                        const uint16_t w = c.v[at + col];
-                        odd = !finite16<BF>(w);
-                        v = BF ? __uint_as_float((uint32_t)w << 16) : h2f(w);
+                        const uint16_t u = c.v[from + col];
+                        odd = !finite16<BF>(u);
+                        v = BF ? __uint_as_float((uint32_t)u << 16) : h2f(u);
                     }
                     if (!odd) continue;
 #pragma unroll
@@ -427,37 +467,35 @@ struct Rows {
     }
 };
 
-// The keys and values of two blocks in a wave's registers.
+// The keys and the values of 16 positions in a wave's registers, and their scale bytes.
 template <bool BF, bool Q8, int D>
-struct Tile {
-    static constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
-    Keys<BF, Q8, D> k[2];
-    Vals<BF, Q8, E> v[8];
-    uint32_t ks[2], vs[2];                    // scale bytes
-
-    __device__ __forceinline__ void load_k(const PagedCache& c, const PageScales& sc, int g, const Blk (&x)[2]) {
-        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+__device__ __forceinline__ void load_k(Keys<BF, Q8, D>& k, uint32_t& scale, const PagedCache& c, const PageScales& sc, int g, const Place& x) {
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+    const int64_t page = max(x.id, 0), at = page * c.kp + g * c.kh + (int64_t)(16 * x.unit) * c.ks;
+    k.load((const char*)c.k + (Q8 ? at : 2 * at), n * (uint32_t)c.ks, gq);
+    if (Q8) scale = sc.k[page * sc.kp + g * sc.kh + x.unit];
+}
+template <bool BF, bool Q8, int D>
+__device__ __forceinline__ void load_v(Vals<BF, Q8, D / 16> (&v)[4], uint32_t& scale, const PagedCache& c, const PageScales& sc, int g, const Place& x) {
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+    const int64_t page = max(x.id, 0), at = page * c.vp + g * c.vh + (int64_t)(16 * x.unit) * c.vs;
+    const char* const b = (const char*)c.v + (Q8 ? at : 2 * at);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t page = max(x[h].id, 0);
-            const int64_t at = page * c.kp + g * c.kh + (int64_t)x[h].off * c.ks;
-            k[h].load((const char*)c.k + (Q8 ? at : 2 * at), n * (uint32_t)c.ks, gq);
-            if (Q8) ks[h] = sc.k[page * sc.kp + g * sc.kh + x[h].unit];
-        }
+    for (int i = 0; i < 4; ++i) v[i].load(b + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * gq * (uint32_t)c.vs, n);
+    if (Q8) scale = sc.v[page * sc.vp + g * sc.vh + x.unit];
+}
+// What a block's scale bytes say: the scores' factor, the values' exponent, and whether it is NaN (or its page is
+// missing).  16-bit pages: the factor alone.
+template <bool Q8>
+__device__ __forceinline__ bool scales_of(const WinArgs& a, int id, uint32_t kb, uint32_t vb, float* ck, float* ev) {
+    if (!Q8) {
+        *ck = a.c, *ev = 0.f;
+        return id < 0;
     }
-    __device__ __forceinline__ void load_v(const PagedCache& c, const PageScales& sc, int g, const Blk (&x)[2]) {
-        const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t page = max(x[h].id, 0);
-            const int64_t at = page * c.vp + g * c.vh + (int64_t)x[h].off * c.vs;
-            const char* b = (const char*)c.v + (Q8 ? at : 2 * at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * h + i].load(b + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * gq * (uint32_t)c.vs, n);
-            if (Q8) vs[h] = sc.v[page * sc.vp + g * sc.vh + x[h].unit];
-        }
-    }
-};
+    *ck = ldexpf(a.c, (int)kb - 127);
+    *ev = (float)value_exp(vb);
+    return id < 0 || kb == 255 || vb == 255;
+}
 
 template <bool BF, bool Q8, int D, int NR>
 __device__ __forceinline__ void load_q(const WinArgs& a, const Task& t, int row0, u32x4 (&q)[NR][(D + 31) / 32]) {
@@ -474,7 +512,7 @@ __device__ __forceinline__ void load_q(const WinArgs& a, const Task& t, int row0
     }
 }
 
-// Few rows (16 or 32): the wave takes the tiles b, b + step, ... of the task; the next tile's keys and values come into
+// Few rows (16 or 32): the wave takes the tiles at, at + step, ... of the task; the next tile's keys and values come into
 // the registers of this one's as soon as a product has read them.
 template <bool BF, bool Q8, int D, int NR>
 __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a,
@@ -483,26 +521,29 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
     const int gq = (threadIdx.x & 63) >> 4;
     r.start(t, b.prefix, a.per, 0);
     if (at >= t.b1) return;
-    Tile<BF, Q8, D> x;
-    Blk cur[2] = {look(c, b, t, at), look(c, b, t, at + 1)};
-    x.load_k(c, sc, t.g, cur);
-    x.load_v(c, sc, t.g, cur);
-    Blk nxt[2] = {look(c, b, t, at + step), look(c, b, t, at + step + 1)};
+    Keys<BF, Q8, D> xk[2];
+    Vals<BF, Q8, E> xv[2][4];
+    uint32_t kb[2], vb[2];
+    Place cur[2], nxt[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        cur[h] = place(c, b, t, at + h);
+        load_k<BF, Q8, D>(xk[h], kb[h], c, sc, t.g, cur[h]);
+        load_v<BF, Q8, D>(xv[h], vb[h], c, sc, t.g, cur[h]);
+        nxt[h] = place(c, b, t, at + step + h);
+    }
     u32x4 q[NR][NS];
     load_q<BF, Q8, D, NR>(a, t, 0, q);
     const bool several = t.position(0, a.per) != t.hi;
     for (; at < t.b1; at += step) {
-        const Blk after[2] = {look(c, b, t, at + 2 * step), look(c, b, t, at + 2 * step + 1)};
-        float ck[2] = {a.c, a.c}, ev[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
-        bool bad[2] = {cur[0].id < 0, cur[1].id < 0};
-        if (Q8)
+        Place after[2];
+        float ck[2], ev[2];
+        bool bad[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bad[h] |= x.ks[h] == 255 || x.vs[h] == 255;
-                ck[h] = ldexpf(a.c, x.ks[h] == 255 ? 0 : (int)x.ks[h] - 127);
-                ev[h] = x.vs[h] == 255 ? 0.f : (float)value_exp(x.vs[h]);
-                vs[h] = BF ? ldexpf(1.f, (int)ev[h]) : 1.f;
-            }
+        for (int h = 0; h < 2; ++h) {
+            after[h] = place(c, b, t, at + 2 * step + h);
+            bad[h] = scales_of<Q8>(a, cur[h].id, kb[h], vb[h], &ck[h], &ev[h]);
+        }
         f32x4 s[NR][2];
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -510,33 +551,39 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         for (int k = 0; k < NS; ++k)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const u32x4 f = x.k[h].get(k);
+                const u32x4 f = xk[h].get(k);
 #pragma unroll
                 for (int rt = 0; rt < NR; ++rt) s[rt][h] = mfma16<BF>(f, q[rt][k], s[rt][h]);
             }
-        if (at + step < t.b1) x.load_k(c, sc, t.g, nxt);
+        const bool more = at + step < t.b1;
+        if (more)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (bad[h])
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) s[rt][h] = f32x4{NAN, NAN, NAN, NAN};
-        const bool part = !whole(cur[0], t, a) || !whole(cur[1], t, a);
+            for (int h = 0; h < 2; ++h) load_k<BF, Q8, D>(xk[h], kb[h], c, sc, t.g, nxt[h]);
+        const Blk x[2] = {look(b, t, at), look(b, t, at + 1)};
+        const bool part = bad[0] | bad[1] | !whole(x[0], t.lo, t.hi, a) | !whole(x[1], t.lo, t.hi, a);
         if (part)
 #pragma unroll
-            for (int rt = 0; rt < NR; ++rt) r.hide(rt, cur, s[rt], a);
+            for (int rt = 0; rt < NR; ++rt) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (bad[h]) s[rt][h] = f32x4{NAN, NAN, NAN, NAN};
+                r.hide(rt, x, s[rt], a);
+            }
         u32x4 w[NR];
         r.weights(s, w, ck, ev);
         uint32_t v[8][EW];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x.v[i].wide(v[i], vs[i >> 2]);
-        if (at + step < t.b1) x.load_v(c, sc, t.g, nxt);
+        for (int i = 0; i < 8; ++i) xv[i >> 2][i & 3].wide(v[i], Q8 && BF ? ldexpf(1.f, (int)ev[i >> 2]) : 1.f);
+        if (more)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) load_v<BF, Q8, D>(xv[h], vb[h], c, sc, t.g, nxt[h]);
         bool fine = true;
         if (part) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int k = 4 * gq + (i & 3), j = cur[i >> 2].j0 + k;
+                const int k = 4 * gq + (i & 3), j = x[i >> 2].j0 + k;
                 // values that no row sees do not reach the product, whatever they hold
-                const bool some = k < cur[i >> 2].nv && j <= t.hi && (j > t.low || j < a.S) && !bad[i >> 2];
+                const bool some = k < x[i >> 2].nv && j <= t.hi && (j > t.low || j < a.S) && !bad[i >> 2];
 #pragma unroll
                 for (int m = 0; m < EW; ++m) {
                     if (!some) v[i][m] = 0;
@@ -553,9 +600,130 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(f, w[rt], r.o[rt][e]);
         }
-        if (part && __any(!fine)) r.add_odd(c, t, cur, vs, a);
+        if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at);
 #pragma unroll
         for (int h = 0; h < 2; ++h) cur[h] = nxt[h], nxt[h] = after[h];
+    }
+}
+
+// Many rows: the four waves share the positions and each has its own 16 * NR rows, Q in registers.  A stage of 64
+// positions comes to LDS in operand order and in 16 bits (a wave brings 16 of them, in registers while the stage before is
+// worked on) and every wave reads all of it.
+constexpr int kBlocks = 4;                    // of 16 positions in a stage, one for each wave
+
+template <int D>
+struct StageLds {
+    static constexpr int E = D / 16, NS = (D + 31) / 32;
+    u32x4 k[kBlocks][NS][64];
+    u32x4 v[E][kBlocks / 2][64];              // a column of each lane's, 32 positions each
+    float ck[kBlocks], ev[kBlocks];           // 8-bit pages: the scores' factors and the values' exponents
+};
+
+template <bool BF, bool Q8, int D, int NR>
+__device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a,
+                                          const Task& t, StageLds<D> (&l)[2], Rows<BF, Q8, D, NR>& r) {
+    constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
+    const int lane = threadIdx.x & 63, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row0 = w * NR * 16;             // the wave's rows of the block
+    r.start(t, b.prefix, a.per, row0);
+    if (t.b0 >= t.b1) return;
+    Keys<BF, Q8, D> xk;
+    Vals<BF, Q8, E> xv[4];
+    uint32_t kb, vb;
+    auto bring = [&](const Place& x) {
+        load_k<BF, Q8, D>(xk, kb, c, sc, t.g, x);
+        load_v<BF, Q8, D>(xv, vb, c, sc, t.g, x);
+    };
+    auto put = [&](int at, const Place& x, StageLds<D>& s) {
+        float ck, ev;
+        const bool bad = scales_of<Q8>(a, x.id, kb, vb, &ck, &ev);
+        const Blk y = look(b, t, at);
+        const float scale = Q8 && BF ? ldexpf(1.f, (int)ev) : 1.f;
+        uint32_t v[4][EW];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xv[i].wide(v[i], scale);
+        if (bad || !whole(y, t.lo, t.hi, a)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = 4 * gq + i, j = y.j0 + k;
+                const bool some = k < y.nv && j <= t.hi && (j > t.low || j < a.S) && !bad;
+                if (!some)
+#pragma unroll
+                    for (int m = 0; m < EW; ++m) v[i][m] = 0;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            u32x4 f = xk.get(k);
+            if (bad) f = u32x4{~0u, ~0u, ~0u, ~0u};                 // its scores are NaN
+            s.k[w][k][lane] = f;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel),
+                                                          __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel)};
+        }
+        if (Q8 && lane == 0) s.ck[w] = bad ? 1.f : ck, s.ev[w] = bad ? 0.f : ev;
+    };
+    int at = t.b0;
+    Place p0 = place(c, b, t, at + w), p1;
+    bring(p0);
+    u32x4 q[NR][NS];
+    load_q<BF, Q8, D, NR>(a, t, row0, q);
+    const int last = min(row0 + 16 * NR, t.rows) - 1;
+    const bool idle = last < row0;
+    // positions of the wave's first and last row
+    const int hi = idle ? -1 : t.position(last, a.per), first = idle ? -1 : t.position(row0, a.per);
+    const int lo = first < b.prefix && t.pos0 != kNowhere ? -1 : first;
+    put(at + w, p0, l[0]);
+    p1 = place(c, b, t, at + kBlocks + w);
+    bring(p1);
+    for (int turn = 0;; ++turn, at += kBlocks) {
+        __syncthreads();                      // the stage is there, and nobody reads the one before
+        const StageLds<D>& st = l[turn & 1];
+        if (at + kBlocks < t.b1) {
+            put(at + kBlocks + w, p1, l[(turn + 1) & 1]);
+            p1 = place(c, b, t, at + 2 * kBlocks + w);
+            if (at + 2 * kBlocks < t.b1) bring(p1);
+        }
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const Blk x[2] = {look(b, t, at + 2 * h), look(b, t, at + 2 * h + 1)};
+            if (hidden(x[0], lo, hi, a) && hidden(x[1], lo, hi, a)) continue;
+            const bool part = !whole(x[0], lo, hi, a) | !whole(x[1], lo, hi, a);
+            f32x4 s[NR][2];
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 f = st.k[2 * h + i][k][lane];
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt) s[rt][i] = mfma16<BF>(f, q[rt][k], s[rt][i]);
+                }
+            float ck[2] = {a.c, a.c}, ev[2] = {0.f, 0.f};
+            if (Q8) ck[0] = st.ck[2 * h], ck[1] = st.ck[2 * h + 1], ev[0] = st.ev[2 * h], ev[1] = st.ev[2 * h + 1];
+            if (part)
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) r.hide(rt, x, s[rt], a);
+            u32x4 wt[NR];
+            r.weights(s, wt, ck, ev);
+            bool fine = true;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                u32x4 v = st.v[e][h][lane];
+                if (part) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &fine);
+                }
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
+            }
+            if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at + 2 * h);
+        }
+        if (at + kBlocks >= t.b1) break;
     }
 }
 
@@ -567,6 +735,41 @@ __device__ __forceinline__ void put_out(uint16_t* o, int m, const float (&v)[E])
     } else {
 #pragma unroll
         for (int e = 0; e < E; e += 2) *(uint32_t*)(o + column_of<Q8, E>(m, e)) = pack2<BF>(v[e], v[e + 1]);
+    }
+}
+
+// a wave's rows without the workgroup's other waves: partial results, or whole ones
+template <bool BF, bool Q8, int D, int NR>
+__device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t end, Rows<BF, Q8, D, NR>& r, int row0) {
+    constexpr int E = D / 16;
+    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+    r.finish(end);
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+        const int i = row0 + rt * 16 + n;
+        if (i >= t.rows) continue;
+        const int tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+        const size_t at = (size_t)tok * a.H + h;
+        if (t.splits > 1) {
+            const size_t slot = at * (a.NP + a.NO) + t.split;
+            float* const p = a.part + slot * D;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[column_of<Q8, E>(4 * gq + k, e)] = r.o[rt][e][k];
+            if (gq == 0) a.ml[slot * 2] = r.ref[rt], a.ml[slot * 2 + 1] = r.sum[rt];
+        } else {
+            const float inv = r.sum[rt] == 0.f ? 0.f : 1.0f / r.sum[rt];
+            uint16_t* const o = a.out + (int64_t)tok * a.ot + h * a.oh;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float v[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = r.o[rt][e][k] * inv;
+                put_out<BF, Q8, E>(o, 4 * gq + k, v);
+            }
+            if (a.lse && gq == 0) a.lse[at] = r.sum[rt] == 0.f ? -INFINITY : r.ref[rt] * 0.69314718055994531f + logf(r.sum[rt]);
+        }
     }
 }
 
@@ -613,7 +816,7 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t en
             const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
             const size_t at = (size_t)tok * a.H + h;
             if (t.splits > 1) {
-                const size_t slot = at * a.NO + t.split;
+                const size_t slot = at * (a.NP + a.NO) + t.split;
                 *(f32x4*)(a.part + slot * D + d) = v;
                 if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
             } else {
@@ -627,19 +830,48 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t en
     }
 }
 
-// One workgroup per task: 16 * NR rows, the four waves on every fourth tile.
-template <bool BF, bool Q8, int D, int NR>
+// One workgroup per task.  WIDE: blocks of 64 * NR rows, the four waves on different rows; else of 16 * NR rows, the four
+// waves on every fourth tile.  Workgroups below ptasks take the prefix for the rows of all sequences at once, the
+// others the sequences' tasks, in blocks of 16 rows where these are not WIDE_OWN.
+template <bool BF, bool Q8, int D, int NR, bool WIDE, bool WIDE_OWN>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
-    __shared__ MeetLds<D, NR> l;
+    constexpr int NO = WIDE && !WIDE_OWN ? 1 : NR;
+    union Lds {
+        StageLds<WIDE ? D : 16> st[2];
+        MeetLds<WIDE && WIDE_OWN ? 16 : D, WIDE ? 1 : NR> m;
+    };
+    __shared__ Lds l;
     const int64_t end = b.prefix + (int64_t)b.width * c.unit * kPageUnit;
+    const bool prefix = (int)blockIdx.x < a.ptasks;
+    if (prefix && WIDE != WIDE_OWN) {
+        if constexpr (WIDE && !WIDE_OWN) {
+            Task t;
+            if (!prefix_task(c, b, a, t)) return;
+            Rows<BF, Q8, D, NR> r;
+            walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l.st, r);
+            store<BF, Q8, D, NR>(a, t, kAll, r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
+        }
+        return;
+    }
     Tasks all;
-    for (int64_t task = blockIdx.x;; task += gridDim.x) {
+    for (int64_t task = (int)blockIdx.x - a.ptasks;; task += gridDim.x - a.ptasks) {
         Task t;
-        if (!all.find(c, b, a, task, t)) return;
-        if (t.split >= t.splits) continue;    // fewer chunks than the sequence's longest block of rows
-        Rows<BF, Q8, D, NR> r;
-        walk<BF, Q8, D, NR>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
-        meet<BF, Q8, D, NR>(a, t, end, r, l);
+        if (prefix) {
+            if (!prefix_task(c, b, a, t)) return;
+        } else {
+            if (!all.find(c, b, a, task, t)) return;
+            if (t.split >= t.splits) continue;                      // fewer chunks than the sequence's longest block of rows
+        }
+        Rows<BF, Q8, D, NO> r;
+        if constexpr (WIDE_OWN) {
+            __syncthreads();                  // an earlier task's LDS is read out
+            walk_wide<BF, Q8, D, NO>(c, sc, b, a, t, l.st, r);
+            store<BF, Q8, D, NO>(a, t, end, r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NO * 16);
+        } else {
+            walk<BF, Q8, D, NO>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
+            meet<BF, Q8, D, NO>(a, t, prefix ? (int64_t)kAll : end, r, l.m);
+        }
+        if (prefix) return;
     }
 }
 
@@ -658,10 +890,11 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
     const int64_t rb = ((int64_t)(t - q.start) * a.per + h % a.per) / a.RT;
     const int lo = (int)(rb * a.RT / a.per), hi = (int)min((rb * a.RT + a.RT - 1) / a.per, (int64_t)q.n - 1);
-    const int n = chunks_of(seen(b, cap, a.W, a.S, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
+    int n = a.NP + chunks_of(seen(b, a, cap, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
     if (n == 1) return;                       // finished where it was computed
-    const float* ml = a.ml + (size_t)row * a.NO * 2;
-    const float* part = a.part + (size_t)row * a.NO * D;
+    if (place < 0) n = 0;                     // (the prefix was worked on for all rows)
+    const float* ml = a.ml + (size_t)row * (a.NP + a.NO) * 2;
+    const float* part = a.part + (size_t)row * (a.NP + a.NO) * D;
     const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float top = kNone, sum = 0.f;
@@ -707,30 +940,59 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
 }
 
 struct Plan {
-    int nr, RT, NO, CT;
+    int nr;                                   // tiles of 16 rows a wave has
+    bool wide, wide_own;
+    int RT, NO, CT, NP, CP, rb, rows, ptasks;
     int64_t tasks;
 };
 
+// Rows per block, chunks and workgroups from the sizes that the host knows.
 int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan* p) {
     const int per = H / c.G;
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > kRowsMax) return LOOPSPEC_EINVAL;
-    p->nr = each > 16 ? 2 : 1;
-    p->RT = 16 * p->nr;
+    p->wide_own = each > 32;
+    // rows of several sequences over the prefix at once, where none has enough of its own
+    const bool together = b.prefix > 0 && W == kAll && b.B > 1 && !p->wide_own;
+    p->wide = p->wide_own || (together && rows > 32);
+    p->nr = p->wide ? 2 : (together ? rows : each) > 16 ? 2 : 1;
+    p->RT = p->wide_own ? 64 * p->nr : p->wide ? 16 : 16 * p->nr;
+    const int slots = 512;                    // two workgroups a CU
+    p->NP = p->CP = p->rb = p->rows = p->ptasks = 0;
+    if (together) {
+        const int block = p->wide ? 64 * p->nr : 16 * p->nr;
+        p->rb = (int)((rows + block - 1) / block);
+        p->rows = (int)((rows + p->rb * 16 - 1) / (p->rb * 16) * 16);
+        // the number of chunks whose rounds of resident workgroups take the least time, a workgroup's start and end
+        // counted as two steps of 128 positions
+        const int64_t steps = (b.prefix + 127) / 128, heads = (int64_t)c.G * p->rb;
+        int64_t best = -1;
+        for (int64_t np = 1; np <= std::min<int64_t>(steps, 128); ++np) {
+            const int64_t len = (steps + np - 1) / np, n = (steps + len - 1) / len;
+            const int64_t cost = (heads * n + slots - 1) / slots * (len + 2);
+            if (best < 0 || cost < best) best = cost, p->NP = (int)n, p->CP = (int)(len * 4);
+        }
+        const int64_t pairs = ((int64_t)c.G * p->NP + 7) / 8 * 8;
+        if (pairs * p->rb > kGroupsMax) return LOOPSPEC_EINVAL;
+        p->ptasks = (int)(pairs * p->rb);
+    }
     // blocks of 16 positions that a block of rows may see
-    int64_t most = (b.prefix + 15) / 16 + (int64_t)b.width * c.unit;
+    int64_t most = (together ? 0 : (b.prefix + 15) / 16) + (int64_t)b.width * c.unit;
     if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
     const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
     const int64_t blocks = std::min(rows, (rows + p->RT - 1) / p->RT + b.B) * c.G;
-    // about 1024 tasks where the tables are full, of at least two tiles a wave
-    p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(8, tiles * blocks / 1024));
+    // about 1024 tasks where the tables are full, of at least two tiles a wave; prompts that fill the card are not cut
+    if (p->wide_own && blocks >= slots)
+        p->CT = (int)tiles;
+    else
+        p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(p->wide_own ? 16 : 8, (tiles * blocks / 1024 + 1) / 2 * 2));
     p->NO = (int)((tiles + p->CT - 1) / p->CT);
     p->tasks = blocks * p->NO;
     return LOOPSPEC_OK;
 }
 
 uint64_t bytes_of(const PagedCache& c, const PagedBatch& b, int H, const Plan& p) {
-    return p.NO > 1 ? (uint64_t)b.T * H * p.NO * (c.D + 2) * 4 : 0;
+    return p.NP + p.NO > 1 ? (uint64_t)b.T * H * (p.NP + p.NO) * (c.D + 2) * 4 : 0;
 }
 
 int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales, const loopspec_paged_batch* batch, int n_heads,
@@ -748,7 +1010,9 @@ int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
 
 template <bool BF, bool Q8, int D>
 const void* kernel_of(const Plan& p) {
-    return p.nr == 1 ? (const void*)k_window<BF, Q8, D, 1> : (const void*)k_window<BF, Q8, D, 2>;
+    if (p.wide_own) return (const void*)k_window<BF, Q8, D, 2, true, true>;
+    if (p.wide) return (const void*)k_window<BF, Q8, D, 2, true, false>;
+    return p.nr == 1 ? (const void*)k_window<BF, Q8, D, 1, false, false> : (const void*)k_window<BF, Q8, D, 2, false, false>;
 }
 template <bool BF, bool Q8>
 const void* kernel_of(int D, const Plan& p) {
@@ -798,15 +1062,16 @@ int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     WinArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
-              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.NO * c.D, cs, args->n_heads,
-              args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT};
+              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (p.NP + p.NO) * c.D, cs, args->n_heads,
+              args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT,
+              p.NP, p.CP, p.rb, p.rows, p.ptasks};
     hipStream_t st = (hipStream_t)stream;
     const bool bf = cache->dtype == LOOPSPEC_BF16, q8 = scales != nullptr;
     void* kargs[] = {&c, &s, &b, &a};
     const void* f = bf ? q8 ? kernel_of<true, true>(c.D, p) : kernel_of<true, false>(c.D, p)
                        : q8 ? kernel_of<false, true>(c.D, p) : kernel_of<false, false>(c.D, p);
-    if (hipLaunchKernel(f, dim3((unsigned)std::min<int64_t>(p.tasks, 16384)), dim3(kT), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
-    if (p.NO > 1) {
+    if (hipLaunchKernel(f, dim3((unsigned)(p.ptasks + std::min<int64_t>(p.tasks, 16384))), dim3(kT), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
+    if (p.NP + p.NO > 1) {
         void* jargs[] = {&c, &b, &a};
         const void* j = bf ? (const void*)k_window_join<true> : (const void*)k_window_join<false>;
         if (hipLaunchKernel(j, dim3((unsigned)((rows + 3) / 4)), dim3(kT), jargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
