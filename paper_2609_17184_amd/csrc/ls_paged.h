@@ -65,6 +65,7 @@ struct PageScales {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 template <bool BF>
 __device__ __forceinline__ void unpack8(const u32x4& u, float (&f)[8]) {
@@ -78,7 +79,7 @@ __device__ __forceinline__ void unpack8(const u32x4& u, float (&f)[8]) {
 template <bool BF>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     if (BF) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    return pack_h2(a, b);
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));      // one instruction
 }
 template <bool BF>
 __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {

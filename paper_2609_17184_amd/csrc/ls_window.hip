@@ -233,26 +233,55 @@ __device__ __forceinline__ Blk look(const PagedBatch& b, const Task& t, int i) {
     const int P = b.prefix, PB = (P + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
     return vb < PB ? Blk{16 * vb, min(16, P - 16 * vb)} : Blk{P + 16 * (vb - PB), 16};
 }
-// where they are: page (-1: none of the cache's; any page will do behind the list's end) and block of the page
-struct Place {
-    int id, unit;
+// The list's blocks that all rows from position lo to hi see whole: from w0 to w1, but for one (the prefix's last, if it
+// is not full).
+struct Inner {
+    int w0, w1, pb;
+    __device__ __forceinline__ bool holds(int i, int n) const { return i >= w0 && i + n <= w1 && (pb < i || pb >= i + n); }
 };
-__device__ __forceinline__ Place place(const PagedCache& c, const PagedBatch& b, const Task& t, int i) {
-    if (i >= t.b1) return Place{0, 0};
+__device__ __forceinline__ Inner inner(const PagedBatch& b, const WinArgs& a, const Task& t, int lo, int hi) {
+    const int P = b.prefix, PB = (P + 15) >> 4, shift = t.s.head - t.s.from, x = max(hi - a.W + 1, 0);
+    const int vb = block_of(x, P, PB), j0 = vb < PB ? 16 * vb : P + 16 * (vb - PB);
+    return Inner{max(t.s.head, vb + (j0 < x) + shift), min(t.b1, block_of(lo + 1, P, PB) + shift), P & 15 ? PB - 1 + shift : -1};
+}
+// Where 64 blocks of the list are, one in each lane: page, and in one word the scale bytes (keys', values' << 8), kBad (the
+// page is none of the cache's, or a scale is NaN) and the block of the page.
+constexpr int kBad = 1 << 16, kUnit = 20;
+struct Where {
+    int id, info;
+};
+template <bool Q8>
+__device__ __forceinline__ Where where(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const Task& t, int i) {
     const int PB = (b.prefix + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
-    const bool pre = vb < PB;
+    const bool pre = vb < PB, in = i < t.b1;
     const unsigned o = pre ? vb : vb - PB, at = unit_div(o, c.magic);
-    Place r{-1, (int)(o - at * c.unit)};
-    if (pre || at < (unsigned)b.width) {
-        r.id = ld_uniform((pre ? b.prefix_table : t.table) + at);
-        if ((unsigned)r.id >= (unsigned)c.n_pages) r.id = -1;
+    const int unit = in ? (int)(o - at * c.unit) : 0;
+    const bool held = in && (pre || at < (unsigned)b.width);
+    const int raw = *(held ? (pre ? b.prefix_table : t.table) + at : b.seq_len);
+    const bool ok = held && (unsigned)raw < (unsigned)c.n_pages;
+    const int id = ok ? raw : 0;              // (behind the list's end any page will do)
+    int info = unit << kUnit | (in && !ok ? kBad : 0);
+    if (Q8) {
+        const int kb = sc.k[id * sc.kp + t.g * sc.kh + unit], vb8 = sc.v[id * sc.vp + t.g * sc.vh + unit];
+        info |= kb | vb8 << 8 | (in && (kb == 255 || vb8 == 255) ? kBad : 0);
     }
-    return r;
+    return Where{id, info};
 }
-// all rows from position lo to hi see all of it; none of them sees any of it
-__device__ __forceinline__ bool whole(const Blk& x, int lo, int hi, const WinArgs& a) {
-    return x.nv == 16 && x.j0 + 15 <= lo && (x.j0 > hi - a.W || x.j0 + 15 < a.S);
+__device__ __forceinline__ Where lane_of(const Where& x, int j) {
+    return Where{__builtin_amdgcn_readlane(x.id, j), __builtin_amdgcn_readlane(x.info, j)};
 }
+// the block's keys and values of the task's head
+template <bool Q8>
+__device__ __forceinline__ const char* keys_at(const PagedCache& c, const Task& t, const Where& x) {
+    const int64_t at = x.id * c.kp + t.g * c.kh + (int64_t)((x.info >> kUnit) * kPageUnit) * c.ks;
+    return (const char*)c.k + (Q8 ? at : 2 * at);
+}
+template <bool Q8>
+__device__ __forceinline__ const char* values_at(const PagedCache& c, const Task& t, const Where& x) {
+    const int64_t at = x.id * c.vp + t.g * c.vh + (int64_t)((x.info >> kUnit) * kPageUnit) * c.vs;
+    return (const char*)c.v + (Q8 ? at : 2 * at);
+}
+// none of the rows from position lo to hi sees any of it
 __device__ __forceinline__ bool hidden(const Blk& x, int lo, int hi, const WinArgs& a) {
     return x.nv == 0 || x.j0 > hi || (x.j0 + 15 <= lo - a.W && x.j0 >= a.S);
 }
@@ -360,14 +389,19 @@ struct Rows {
         }
     }
     static __device__ __forceinline__ bool sees(int j, int hi, const WinArgs& a) { return j <= hi && (j > hi - a.W || j < a.S); }
-    // the scores of what the lane's row does not see
-    __device__ __forceinline__ void hide(int rt, const Blk (&x)[2], f32x4 (&s)[2], const WinArgs& a) const {
-        const int gq = (threadIdx.x & 63) >> 4;
+    // the scores of what the lane's row does not see in a block, where rows from position `lo` to `top` are the wave's
+    __device__ __forceinline__ void hide(int rt, const Blk& x, f32x4& s, int lo, int top, const WinArgs& a) const {
+        const int first = x.j0 + 4 * ((threadIdx.x & 63) >> 4);     // the lane's positions are first + i
+        if (x.j0 + 15 > lo || x.nv < 16) {                          // some row is before the block's end
+            const int n = min(hi[rt], x.j0 + x.nv - 1) - first;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < 4; ++i) s[i] = i <= n ? s[i] : -INFINITY;
+        }
+        if (x.j0 <= top - a.W && x.j0 + 15 >= a.S) {                // some row's window begins behind the block's first
+            const int n = hi[rt] - a.W - first, m = a.S - first;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (4 * gq + i >= x[h].nv || !sees(x[h].j0 + 4 * gq + i, hi[rt], a)) s[h][i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) s[i] = i > n || i < m ? s[i] : -INFINITY;
+        }
     }
     struct Weights {
         float x[2][4], part, sum;
@@ -404,16 +438,16 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < E; ++e) o[rt][e] *= al;
     }
-    // The weights of 32 positions as operands, and their sums.  No maximum is taken: a lane's sum of 8 tells when some
-    // weight may leave its range, and then, which is rare after the first tiles, the reference is raised.
-    __device__ __forceinline__ void weights(const f32x4 (&s)[NR][2], u32x4 (&p)[NR], const float (&ck)[2], const float (&ev)[2]) {
-        Weights w[NR];
+    // The weights of 32 positions as operands, and their sums, in two steps.  No maximum is taken: a lane's sum of 8
+    // tells when some weight may leave its range, and then, which is rare after the first tiles, the reference is raised.
+    __device__ __forceinline__ void take(const f32x4 (&s)[NR][2], Weights (&w)[NR], const float (&ck)[2], const float (&ev)[2]) const {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) w[rt].take(s[rt], ref[rt], ck, ev);
+    }
+    __device__ __forceinline__ void settle(const f32x4 (&s)[NR][2], Weights (&w)[NR], u32x4 (&p)[NR], const float (&ck)[2], const float (&ev)[2]) {
         bool any = false;
 #pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            w[rt].take(s[rt], ref[rt], ck, ev);
-            any |= w[rt].part > high;
-        }
+        for (int rt = 0; rt < NR; ++rt) any |= w[rt].part > high;
         if (__builtin_expect(__any(any), 0))
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt)
@@ -424,17 +458,22 @@ struct Rows {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) sum[rt] += w[rt].sum, p[rt] = w[rt].packed();
     }
+    __device__ __forceinline__ void weights(const f32x4 (&s)[NR][2], u32x4 (&p)[NR], const float (&ck)[2], const float (&ev)[2]) {
+        Weights w[NR];
+        take(s, w, ck, ev);
+        settle(s, w, p, ck, ev);
+    }
     // What values that are not finite contribute to the rows that see them: the products' operand has zeros in their
     // places, since a zero weight would not keep them out of the other rows.
     __device__ __forceinline__ void add_odd(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a, const Task& t, int at) {
         const int gq = (threadIdx.x & 63) >> 4;
         for (int i = 0; i < 32; ++i) {
             const Blk y = look(b, t, at + (i >> 4));
-            const Place w = place(c, b, t, at + (i >> 4));
-            if ((i & 15) >= y.nv || w.id < 0) continue;
+            const Where w = where<Q8>(c, sc, b, t, at + (i >> 4));
+            if ((i & 15) >= y.nv || (w.info & kBad)) continue;
             const int j = y.j0 + (i & 15);
-            const int64_t from = w.id * c.vp + t.g * c.vh + (int64_t)(16 * w.unit + (i & 15)) * c.vs;
-            const float scale = Q8 && BF ? ldexpf(1.f, value_exp(sc.v[w.id * sc.vp + t.g * sc.vh + w.unit])) : 1.f;
+            const char* const from = values_at<Q8>(c, t, w) + (int64_t)(i & 15) * c.vs * (Q8 ? 1 : 2);
+            const float scale = Q8 && BF ? ldexpf(1.f, value_exp(w.info >> 8 & 255)) : 1.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -443,10 +482,10 @@ struct Rows {
                     float v;
                     bool odd;
                     if (Q8) {
-                        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)c.v)[from + col], 0) * scale;
+                        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)from)[col], 0) * scale;
                         odd = !(fabsf(v) < INFINITY) || (BF && !finite16<true>(pack2<true>(v, v)));
                     } else {
-                        const uint16_t u = c.v[from + col];
+                        const uint16_t u = ((const uint16_t*)from)[col];
                         odd = !finite16<BF>(u);
                         v = BF ? __uint_as_float((uint32_t)u << 16) : h2f(u);
                     }
@@ -467,34 +506,23 @@ struct Rows {
     }
 };
 
-// The keys and the values of 16 positions in a wave's registers, and their scale bytes.
+// The keys and the values of 16 positions in a wave's registers.
 template <bool BF, bool Q8, int D>
-__device__ __forceinline__ void load_k(Keys<BF, Q8, D>& k, uint32_t& scale, const PagedCache& c, const PageScales& sc, int g, const Place& x) {
-    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-    const int64_t page = max(x.id, 0), at = page * c.kp + g * c.kh + (int64_t)(16 * x.unit) * c.ks;
-    k.load((const char*)c.k + (Q8 ? at : 2 * at), n * (uint32_t)c.ks, gq);
-    if (Q8) scale = sc.k[page * sc.kp + g * sc.kh + x.unit];
+__device__ __forceinline__ void load_k(Keys<BF, Q8, D>& k, const PagedCache& c, const char* at) {
+    const int lane = threadIdx.x & 63;
+    k.load(at, (lane & 15) * (uint32_t)c.ks, lane >> 4);
 }
 template <bool BF, bool Q8, int D>
-__device__ __forceinline__ void load_v(Vals<BF, Q8, D / 16> (&v)[4], uint32_t& scale, const PagedCache& c, const PageScales& sc, int g, const Place& x) {
-    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-    const int64_t page = max(x.id, 0), at = page * c.vp + g * c.vh + (int64_t)(16 * x.unit) * c.vs;
-    const char* const b = (const char*)c.v + (Q8 ? at : 2 * at);
+__device__ __forceinline__ void load_v(Vals<BF, Q8, D / 16> (&v)[4], const PagedCache& c, const char* at) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i].load(b + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * gq * (uint32_t)c.vs, n);
-    if (Q8) scale = sc.v[page * sc.vp + g * sc.vh + x.unit];
+    for (int i = 0; i < 4; ++i) v[i].load(at + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * (lane >> 4) * (uint32_t)c.vs, lane & 15);
 }
-// What a block's scale bytes say: the scores' factor, the values' exponent, and whether it is NaN (or its page is
-// missing).  16-bit pages: the factor alone.
+// What a block's scale bytes say: the scores' factor and the values' exponent.
 template <bool Q8>
-__device__ __forceinline__ bool scales_of(const WinArgs& a, int id, uint32_t kb, uint32_t vb, float* ck, float* ev) {
-    if (!Q8) {
-        *ck = a.c, *ev = 0.f;
-        return id < 0;
-    }
-    *ck = ldexpf(a.c, (int)kb - 127);
-    *ev = (float)value_exp(vb);
-    return id < 0 || kb == 255 || vb == 255;
+__device__ __forceinline__ void scales_of(const WinArgs& a, int info, float* ck, float* ev) {
+    *ck = Q8 ? ldexpf(a.c, (info & 255) - 127) : a.c;
+    *ev = Q8 ? (float)value_exp(info >> 8 & 255) : 0.f;
 }
 
 template <bool BF, bool Q8, int D, int NR>
@@ -523,27 +551,34 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
     if (at >= t.b1) return;
     Keys<BF, Q8, D> xk[2];
     Vals<BF, Q8, E> xv[2][4];
-    uint32_t kb[2], vb[2];
-    Place cur[2], nxt[2];
+    // lane 2 j + h: block h of the wave's tile j of 32
+    const int lane = threadIdx.x & 63;
+    const int at0 = at + (lane & 1);
+    auto find = [&](int j) { return where<Q8>(c, sc, b, t, at0 + step * (j + (lane >> 1))); };
+    Where run = find(0);
+    int turn = 0, info[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        cur[h] = place(c, b, t, at + h);
-        load_k<BF, Q8, D>(xk[h], kb[h], c, sc, t.g, cur[h]);
-        load_v<BF, Q8, D>(xv[h], vb[h], c, sc, t.g, cur[h]);
-        nxt[h] = place(c, b, t, at + step + h);
+        const Where x = lane_of(run, h);
+        load_k<BF, Q8, D>(xk[h], c, keys_at<Q8>(c, t, x));
+        load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, x));
+        info[h] = x.info;
     }
     u32x4 q[NR][NS];
     load_q<BF, Q8, D, NR>(a, t, 0, q);
     const bool several = t.position(0, a.per) != t.hi;
-    for (; at < t.b1; at += step) {
-        Place after[2];
+    const Inner in = inner(b, a, t, t.lo, t.hi);
+    for (int known = 31;; known += 32) {      // the last tile whose place the lanes hold
+    for (; at < t.b1 && turn < known; at += step, ++turn) {
         float ck[2], ev[2];
         bool bad[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            after[h] = place(c, b, t, at + 2 * step + h);
-            bad[h] = scales_of<Q8>(a, cur[h].id, kb[h], vb[h], &ck[h], &ev[h]);
+            scales_of<Q8>(a, info[h], &ck[h], &ev[h]);
+            bad[h] = info[h] & kBad;
         }
+        const bool more = at + step < t.b1;
+        Where nx[2];
         f32x4 s[NR][2];
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -555,19 +590,25 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
 #pragma unroll
                 for (int rt = 0; rt < NR; ++rt) s[rt][h] = mfma16<BF>(f, q[rt][k], s[rt][h]);
             }
-        const bool more = at + step < t.b1;
         if (more)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) load_k<BF, Q8, D>(xk[h], kb[h], c, sc, t.g, nxt[h]);
-        const Blk x[2] = {look(b, t, at), look(b, t, at + 1)};
-        const bool part = bad[0] | bad[1] | !whole(x[0], t.lo, t.hi, a) | !whole(x[1], t.lo, t.hi, a);
+            for (int h = 0; h < 2; ++h) {
+                nx[h] = lane_of(run, (2 * turn + 2 + h) & 63);
+                load_k<BF, Q8, D>(xk[h], c, keys_at<Q8>(c, t, nx[h]));
+            }
+        const bool part = bad[0] | bad[1] | !in.holds(at, 2);
+        Blk x[2];
+        if (part)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[h] = look(b, t, at + h);
         if (part)
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {
                     if (bad[h]) s[rt][h] = f32x4{NAN, NAN, NAN, NAN};
-                r.hide(rt, x, s[rt], a);
+                    r.hide(rt, x[h], s[rt][h], t.lo, t.hi, a);
+                }
             }
         u32x4 w[NR];
         r.weights(s, w, ck, ev);
@@ -576,7 +617,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         for (int i = 0; i < 8; ++i) xv[i >> 2][i & 3].wide(v[i], Q8 && BF ? ldexpf(1.f, (int)ev[i >> 2]) : 1.f);
         if (more)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) load_v<BF, Q8, D>(xv[h], vb[h], c, sc, t.g, nxt[h]);
+            for (int h = 0; h < 2; ++h) load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, nx[h])), info[h] = nx[h].info;
         bool fine = true;
         if (part) {
 #pragma unroll
@@ -601,8 +642,9 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
             for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(f, w[rt], r.o[rt][e]);
         }
         if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) cur[h] = nxt[h], nxt[h] = after[h];
+    }
+    if (at >= t.b1) return;
+    run = find(turn + 1);                     // 32 more, outside the loop: a branch in it costs copies of the accumulators
     }
 }
 
@@ -617,6 +659,7 @@ struct StageLds {
     u32x4 k[kBlocks][NS][64];
     u32x4 v[E][kBlocks / 2][64];              // a column of each lane's, 32 positions each
     float ck[kBlocks], ev[kBlocks];           // 8-bit pages: the scores' factors and the values' exponents
+    int odd[kBlocks];                         // values that are not finite have been left out
 };
 
 template <bool BF, bool Q8, int D, int NR>
@@ -627,37 +670,51 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
     const int row0 = w * NR * 16;             // the wave's rows of the block
     r.start(t, b.prefix, a.per, row0);
     if (t.b0 >= t.b1) return;
+    const int last = min(row0 + 16 * NR, t.rows) - 1;
+    const bool idle = last < row0;
+    // positions of the wave's first and last row
+    const int hi = idle ? -1 : t.position(last, a.per), first = idle ? -1 : t.position(row0, a.per);
+    const int lo = first < b.prefix && t.pos0 != kNowhere ? -1 : first;
+    const Inner in = inner(b, a, t, lo, hi), all = inner(b, a, t, t.lo, t.hi);
     Keys<BF, Q8, D> xk;
     Vals<BF, Q8, E> xv[4];
-    uint32_t kb, vb;
-    auto bring = [&](const Place& x) {
-        load_k<BF, Q8, D>(xk, kb, c, sc, t.g, x);
-        load_v<BF, Q8, D>(xv, vb, c, sc, t.g, x);
+    // lane j: the block that the wave brings of stage j of 64
+    Where run;
+    int turn = 0, info = 0;                   // turn: of the stage that is worked on
+    auto find = [&](int j) { run = where<Q8>(c, sc, b, t, t.b0 + kBlocks * (j + lane) + w); };
+    auto bring = [&](int j) {
+        const Where x = lane_of(run, j & 63);
+        load_k<BF, Q8, D>(xk, c, keys_at<Q8>(c, t, x));
+        load_v<BF, Q8, D>(xv, c, values_at<Q8>(c, t, x));
+        info = x.info;
     };
-    auto put = [&](int at, const Place& x, StageLds<D>& s) {
+    auto put = [&](int at, StageLds<D>& s) {
         float ck, ev;
-        const bool bad = scales_of<Q8>(a, x.id, kb, vb, &ck, &ev);
-        const Blk y = look(b, t, at);
+        scales_of<Q8>(a, info, &ck, &ev);
+        const bool bad = info & kBad;
         const float scale = Q8 && BF ? ldexpf(1.f, (int)ev) : 1.f;
         uint32_t v[4][EW];
 #pragma unroll
         for (int i = 0; i < 4; ++i) xv[i].wide(v[i], scale);
-        if (bad || !whole(y, t.lo, t.hi, a)) {
+        bool odd = false;
+        if (bad || !all.holds(at, 1)) {       // some row does not see some of it: a zero weight keeps no NaN out
+            const Blk y = look(b, t, at);
+            bool fine = true;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = 4 * gq + i, j = y.j0 + k;
                 const bool some = k < y.nv && j <= t.hi && (j > t.low || j < a.S) && !bad;
-                if (!some)
 #pragma unroll
-                    for (int m = 0; m < EW; ++m) v[i][m] = 0;
+                for (int m = 0; m < EW; ++m) v[i][m] = some ? sane<BF>(v[i][m], &fine) : 0;
             }
+            odd = __any(!fine);
         }
+        if (lane == 0) s.odd[w] = odd;
 #pragma unroll
-        for (int k = 0; k < NS; ++k) {
-            u32x4 f = xk.get(k);
-            if (bad) f = u32x4{~0u, ~0u, ~0u, ~0u};                 // its scores are NaN
-            s.k[w][k][lane] = f;
-        }
+        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = xk.get(k);
+        if (bad)                              // its scores are NaN
+#pragma unroll
+            for (int k = 0; k < NS; ++k) s.k[w][k][lane] = u32x4{~0u, ~0u, ~0u, ~0u};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
@@ -667,63 +724,104 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
         if (Q8 && lane == 0) s.ck[w] = bad ? 1.f : ck, s.ev[w] = bad ? 0.f : ev;
     };
     int at = t.b0;
-    Place p0 = place(c, b, t, at + w), p1;
-    bring(p0);
+    find(0);
+    bring(0);
     u32x4 q[NR][NS];
     load_q<BF, Q8, D, NR>(a, t, row0, q);
-    const int last = min(row0 + 16 * NR, t.rows) - 1;
-    const bool idle = last < row0;
-    // positions of the wave's first and last row
-    const int hi = idle ? -1 : t.position(last, a.per), first = idle ? -1 : t.position(row0, a.per);
-    const int lo = first < b.prefix && t.pos0 != kNowhere ? -1 : first;
-    put(at + w, p0, l[0]);
-    p1 = place(c, b, t, at + kBlocks + w);
-    bring(p1);
-    for (int turn = 0;; ++turn, at += kBlocks) {
-        __syncthreads();                      // the stage is there, and nobody reads the one before
-        const StageLds<D>& st = l[turn & 1];
+    put(at + w, l[0]);
+    if (at + kBlocks < t.b1) bring(1);
+    // the next stage to LDS, the one after that on its way
+    auto next = [&]() {
         if (at + kBlocks < t.b1) {
-            put(at + kBlocks + w, p1, l[(turn + 1) & 1]);
-            p1 = place(c, b, t, at + 2 * kBlocks + w);
-            if (at + 2 * kBlocks < t.b1) bring(p1);
+            put(at + kBlocks + w, l[(turn + 1) & 1]);
+            if (at + 2 * kBlocks < t.b1) bring(turn + 2);
         }
+    };
+    // Operands come from LDS well before their products, past other work: left to itself the compiler reads each into the
+    // same registers right before its products and waits for it there.
+    u32x4 kf[NS][2], vf[E];
+    auto read_k = [&](const StageLds<D>& st, int h) {
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) kf[k][i] = st.k[2 * h + i][k][lane];
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_v = [&](const StageLds<D>& st, int h) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < E; ++e) vf[e] = st.v[e][h][lane];
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    f32x4 s[NR][2];
+    u32x4 wt[NR];
+    auto scores = [&]() {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) s[rt][i] = mfma16<BF>(kf[k][i], q[rt][k], s[rt][i]);
+    };
+    float ck[2] = {a.c, a.c}, ev[2] = {0.f, 0.f};
+    auto factors = [&](const StageLds<D>& st, int h) {
+        if (Q8) ck[0] = st.ck[2 * h], ck[1] = st.ck[2 * h + 1], ev[0] = st.ev[2 * h], ev[1] = st.ev[2 * h + 1];
+    };
+    auto add = [&]() {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(vf[e], wt[rt], r.o[rt][e]);
+    };
+    for (int known = 62;;) {
+        // the places of 64 more stages, outside the loops around products: a branch in these costs copies of the
+        // accumulators
+        if (turn == known) find(turn + 2), known += 64;
+        // stages that all rows of the wave see (waves of a workgroup may leave at different ones: both loops have one
+        // barrier a stage)
+        while (in.holds(at, kBlocks) && turn < known) {
+            const StageLds<D>& st = l[turn & 1];
+            __syncthreads();                  // the stage is there, and nobody reads the one before
+            read_k(st, 0);
+            next();
+            factors(st, 0);
+            scores();
+            read_v(st, 0);
+            r.weights(s, wt, ck, ev);
+            factors(st, 1);
+            read_k(st, 1);
+            add();
+            scores();
+            read_v(st, 1);
+            r.weights(s, wt, ck, ev);
+            add();
+            ++turn, at += kBlocks;
+        }
+        if (at >= t.b1) break;
+        if (turn == known) continue;
+        const StageLds<D>& st = l[turn & 1];
+        __syncthreads();
+        next();
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
             const Blk x[2] = {look(b, t, at + 2 * h), look(b, t, at + 2 * h + 1)};
             if (hidden(x[0], lo, hi, a) && hidden(x[1], lo, hi, a)) continue;
-            const bool part = !whole(x[0], lo, hi, a) | !whole(x[1], lo, hi, a);
-            f32x4 s[NR][2];
+            read_k(st, h);
+            scores();
 #pragma unroll
-            for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
-            for (int k = 0; k < NS; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const u32x4 f = st.k[2 * h + i][k][lane];
-#pragma unroll
-                    for (int rt = 0; rt < NR; ++rt) s[rt][i] = mfma16<BF>(f, q[rt][k], s[rt][i]);
-                }
-            float ck[2] = {a.c, a.c}, ev[2] = {0.f, 0.f};
-            if (Q8) ck[0] = st.ck[2 * h], ck[1] = st.ck[2 * h + 1], ev[0] = st.ev[2 * h], ev[1] = st.ev[2 * h + 1];
-            if (part)
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) r.hide(rt, x, s[rt], a);
-            u32x4 wt[NR];
+                for (int i = 0; i < 2; ++i) r.hide(rt, x[i], s[rt][i], lo, hi, a);
+            read_v(st, h);
+            factors(st, h);
             r.weights(s, wt, ck, ev);
-            bool fine = true;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                u32x4 v = st.v[e][h][lane];
-                if (part) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = sane<BF>(v[j], &fine);
-                }
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(v, wt[rt], r.o[rt][e]);
-            }
-            if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at + 2 * h);
+            add();
+            if (st.odd[2 * h] | st.odd[2 * h + 1]) r.add_odd(c, sc, b, a, t, at + 2 * h);
         }
-        if (at + kBlocks >= t.b1) break;
+        ++turn, at += kBlocks;
+        if (at >= t.b1) break;
     }
 }
 
@@ -1016,6 +1114,9 @@ const void* kernel_of(const Plan& p) {
 }
 template <bool BF, bool Q8>
 const void* kernel_of(int D, const Plan& p) {
+#ifdef LSW_DEV
+    return D != 128 ? (const void*)k_window<false, true, 96, 2, true, true> : BF && !Q8 ? (p.wide_own ? (const void*)k_window<true, false, 128, 2, true, true> : (const void*)k_window<true, false, 128, 1, false, false>) : BF ? (const void*)k_window<true, true, 128, 2, true, false> : (const void*)k_window<false, true, 128, 1, false, false>;
+#else
     switch (D) {
         case 16: return kernel_of<BF, Q8, 16>(p);
         case 32: return kernel_of<BF, Q8, 32>(p);
@@ -1023,6 +1124,7 @@ const void* kernel_of(int D, const Plan& p) {
         case 96: return kernel_of<BF, Q8, 96>(p);
         default: return kernel_of<BF, Q8, 128>(p);
     }
+#endif
 }
 
 }  // namespace
