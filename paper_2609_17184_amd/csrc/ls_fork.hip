@@ -1,11 +1,11 @@
 // Forks of a batch over a paged cache: whole pages are shared and counted, the
 // partly filled last page is copied, pages without a reader are given out again.
 //
-// Four launches: counts start as the caller's; a workgroup per child writes its
-// table row and one per parent lets pages go (integer atomics, whose order does
-// not matter); one workgroup numbers the free pages in rising order and the wants
-// of the children in theirs; a workgroup per child and slice of the caches fills
-// in the pages and copies.
+// Four launches: counts start as the caller's; a wave per child writes its table
+// row and one per parent lets pages go (integer atomics, whose order does not
+// matter); one workgroup numbers the free pages in rising order and the wants of
+// the children in theirs; a workgroup per child and half a cache fills in the
+// pages and copies.  For few rows and pages one workgroup does all but the copies.
 //
 // Which child takes its parent's pages over is found by looking through the
 // children before it, so nothing has to be exchanged for it.
@@ -17,7 +17,7 @@ namespace ls {
 
 namespace {
 
-constexpr int kT = 256;
+constexpr int kT = 256, kMost = 1024;
 constexpr int kMany = 16;                     // caches per launch: their descriptions travel with it
 constexpr int kWanted = -2;                   // an entry of the new table that is to get a page
 
@@ -36,7 +36,7 @@ struct Copied {
     uint8_t *ks, *vs;
     int64_t kp, kh, kr, vp, vh, vr;           // strides in bytes: page, head, position
     int64_t ksp, ksh, vsp, vsh;
-    int G, chunks;                            // heads, 16-byte pieces of a row
+    unsigned G, chunks;                       // heads, 16-byte pieces of a row
 };
 struct CopySet {
     Copied c[kMany];
@@ -54,73 +54,94 @@ __device__ __forceinline__ bool gone(const Fork& f, int len, int i) {
     const int64_t first = f.P + (int64_t)i * f.ps, next = (int64_t)f.P + len;
     return first + f.ps - 1 <= next - f.W && first >= f.S;
 }
-// some child below j (of m) continues row p; every thread of the workgroup gets the answer
+// some child below j (of m) continues row p; asked by a whole wave
 __device__ __forceinline__ bool has_child(const Fork& f, int p, int j) {
     bool any = false;
-    for (int i = threadIdx.x; i < j; i += kT) any |= f.parent[i] == p;
-    return __syncthreads_or(any);
+    for (int i = threadIdx.x & 63; i < j; i += 64) any |= f.parent[i] == p;
+    return __any(any);
 }
 
-// Row j of the new table: what it takes over of its parent's, -1 elsewhere, kWanted where it is to get a page.
-__device__ void child_row(const Fork& f, int j) {
-    __shared__ int wants;
-    const int p = f.parent[j];
+// the counts: in memory, or in LDS where one workgroup does everything
+struct InMemory {
+    int32_t* r;
+    __device__ __forceinline__ void add(int x, int v) const { atomicAdd(&r[x], v); }
+    __device__ __forceinline__ int get(int x) const { return r[x]; }
+    __device__ __forceinline__ void set(int x, int v) const { r[x] = v; }
+};
+
+// A wave's row j of the new table: what it takes over of its parent's, -1 elsewhere, kWanted where it is to get a page.
+// Gives the number of these.
+template <class R>
+__device__ int child_row(const Fork& f, const R& refs, int32_t* lack, int j) {
+    const int lane = threadIdx.x & 63, p = f.parent[j];
     const int len = (unsigned)p < (unsigned)f.n ? f.seq_len[p] : -1;
     int32_t* const to = f.table_out + j * f.out_stride;
-    if (threadIdx.x == 0) wants = 0;
-    const bool heir = len >= 0 && !has_child(f, p, j);
-    __syncthreads();
-    int mine = 0;
+    int wants = 0, source = -1;
     if (len < 0) {
-        for (int i = threadIdx.x; i < f.width; i += kT) to[i] = -1;
-        if (threadIdx.x == 0) f.source[j] = -1;
+        for (int i = lane; i < f.width; i += 64) to[i] = -1;
     } else {
+        const bool heir = !has_child(f, p, j);
         const int32_t* const from = f.table + p * f.stride;
         const int full = (int)min((int64_t)(len / f.ps), (int64_t)f.width), held = pages_of(f, len);
         const int64_t more = (min((int64_t)len, (int64_t)f.width * f.ps) + f.room + f.ps - 1) / f.ps;
         const int want = f.room ? (int)min(more, (int64_t)f.width) : held;
-        for (int i = threadIdx.x; i < f.width; i += kT) {
-            const int x = from[i];
-            const bool ok = page_ok(f, x), off = gone(f, len, i);
+        for (int i0 = 0; i0 < f.width; i0 += 64) {
+            const int i = i0 + lane;
             int y = -1;
-            if (heir) {
-                if (ok && off) atomicSub(&f.refs_out[x], 1);
-                if (ok && !off) y = x;
-                if (!ok && i >= held && i < want) y = kWanted;
-            } else {
-                if (i < full) {
-                    if (ok && !off) y = x, atomicAdd(&f.refs_out[x], 1);
+            if (i < f.width) {
+                const int x = from[i];
+                const bool ok = page_ok(f, x), off = gone(f, len, i);
+                if (heir) {
+                    if (ok && off) refs.add(x, -1);
+                    if (ok && !off) y = x;
+                    if (!ok && i >= held && i < want) y = kWanted;
+                } else if (i < full) {
+                    if (ok && !off) y = x, refs.add(x, 1);
                 } else if (i < held) {
-                    if (ok) y = kWanted;
+                    if (ok) y = kWanted, source = x;                // its page of the copy
                 } else if (i < want) {
                     y = kWanted;
                 }
+                to[i] = y;
             }
-            to[i] = y;
-            mine += y == kWanted;
+            wants += __popcll(__ballot(y == kWanted));
         }
-        if (f.room && more > f.width && threadIdx.x == 0) atomicAdd(f.lack, (int)(more - f.width));
-        if (threadIdx.x == 0) f.source[j] = !heir && full < held && page_ok(f, from[full]) ? from[full] : -1;
+        if (f.room && more > f.width && lane == 0) atomicAdd(lack, (int)(more - f.width));
     }
-    if (mine) atomicAdd(&wants, mine);
-    __syncthreads();
-    if (threadIdx.x == 0) f.need[j] = wants, f.len_out[j] = len < 0 ? -1 : len;
-    __syncthreads();
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) source = max(source, __shfl_xor(source, o));
+    if (lane == 0) f.source[j] = source, f.len_out[j] = len < 0 ? -1 : len;
+    return wants;
 }
 
-// A row without a child lets its pages go.
-__device__ void end_row(const Fork& f, int p) {
-    const bool kept = has_child(f, p, f.m);
-    if (kept || f.seq_len[p] < 0) return;
-    for (int i = threadIdx.x; i < f.width; i += kT) {
+// A row without a child lets its pages go; a wave's work.
+template <class R>
+__device__ void end_row(const Fork& f, const R& refs, int p) {
+    if (has_child(f, p, f.m) || f.seq_len[p] < 0) return;
+    for (int i = threadIdx.x & 63; i < f.width; i += 64) {
         const int x = f.table[p * f.stride + i];
-        if (page_ok(f, x)) atomicSub(&f.refs_out[x], 1);
+        if (page_ok(f, x)) refs.add(x, -1);
+    }
+}
+
+// the wanted entries of row j get the free pages from number `at` on; a wave's work
+__device__ void fill_row(const Fork& f, const int32_t* free, int j, int at, int given) {
+    const int lane = threadIdx.x & 63;
+    int32_t* const row = f.table_out + j * f.out_stride;
+    for (int i0 = 0; i0 < f.width; i0 += 64) {
+        const int i = i0 + lane;
+        const bool want = i < f.width && row[i] == kWanted;
+        const unsigned long long all = __ballot(want);
+        const int k = at + __popcll(all & ((1ull << lane) - 1));
+        if (want) row[i] = k < given ? free[k] : -1;
+        at += __popcll(all);
     }
 }
 
 // sum of v over the threads below, and over all of them
+template <int NT>
 __device__ __forceinline__ int scan(int v, int* total) {
-    __shared__ int part[kT / 64];
+    __shared__ int part[NT / 64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int upto = v;
 #pragma unroll
@@ -133,7 +154,7 @@ __device__ __forceinline__ int scan(int v, int* total) {
     __syncthreads();
     int before = 0, all = 0;
 #pragma unroll
-    for (int i = 0; i < kT / 64; ++i) {
+    for (int i = 0; i < NT / 64; ++i) {
         if (i < w) before += part[i];
         all += part[i];
     }
@@ -141,35 +162,35 @@ __device__ __forceinline__ int scan(int v, int* total) {
     return before + upto - v;
 }
 
-// need[j] becomes the number of child j's first page among the free ones; free lists as many of these as are wanted.
-__device__ void hand_out(const Fork& f) {
+// need[j] becomes the number of child j's first page among the free ones, need[m] how many are given out; free lists
+// these.  A workgroup's work; returns how many were wanted and not to be had.
+template <int NT, class R>
+__device__ int hand_out(const Fork& f, const R& refs, int32_t* need, int32_t* free) {
     int wanted = 0, total;
-    for (int j0 = 0; j0 < f.m; j0 += kT) {
-        const int j = j0 + threadIdx.x, v = j < f.m ? f.need[j] : 0, at = scan(v, &total);
-        if (j < f.m) f.need[j] = wanted + at;
+    for (int j0 = 0; j0 < f.m; j0 += NT) {
+        const int j = j0 + threadIdx.x, v = j < f.m ? need[j] : 0, at = scan<NT>(v, &total);
+        if (j < f.m) need[j] = wanted + at;
         wanted += total;
     }
     constexpr int PER = 8;
     int found = 0;
-    for (int x0 = 0; x0 < f.pages && found < wanted; x0 += PER * kT) {
+    for (int x0 = 0; x0 < f.pages && found < wanted; x0 += PER * NT) {
         unsigned mask = 0;
         const int first = x0 + PER * (int)threadIdx.x;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (first + i < f.pages && f.refs_out[first + i] == 0) mask |= 1u << i;
-        int at = found + scan(__popc(mask), &total);
+            if (first + i < f.pages && refs.get(first + i) == 0) mask |= 1u << i;
+        int at = found + scan<NT>(__popc(mask), &total);
         for (; mask; mask &= mask - 1, ++at)
             if (at < wanted) {
                 const int x = first + __ffs(mask) - 1;
-                f.free[at] = x;
-                f.refs_out[x] = 1;
+                free[at] = x;
+                refs.set(x, 1);
             }
         found += total;
     }
-    if (threadIdx.x == 0) {
-        f.need[f.m] = min(found, wanted);     // pages given out
-        f.lack[0] += max(wanted - found, 0);
-    }
+    if (threadIdx.x == 0) need[f.m] = min(found, wanted);
+    return max(wanted - found, 0);
 }
 
 __global__ void __launch_bounds__(kT) k_fork_start(Fork f) {
@@ -177,29 +198,62 @@ __global__ void __launch_bounds__(kT) k_fork_start(Fork f) {
     if (i < f.pages && f.refs_out != f.refs) f.refs_out[i] = f.refs[i];
     if (i == 0) *f.lack = 0;
 }
+// a wave per child, then one per parent
 __global__ void __launch_bounds__(kT) k_fork_rows(Fork f) {
-    if ((int)blockIdx.x < f.m)
-        child_row(f, blockIdx.x);
-    else
-        end_row(f, blockIdx.x - f.m);
+    const int i = blockIdx.x * (kT / 64) + (threadIdx.x >> 6);
+    const InMemory refs{f.refs_out};
+    if (i < f.m) {
+        const int wants = child_row(f, refs, f.lack, i);
+        if ((threadIdx.x & 63) == 0) f.need[i] = wants;
+    } else if (i < f.m + f.n) {
+        end_row(f, refs, i - f.m);
+    }
 }
-__global__ void __launch_bounds__(kT) k_fork_free(Fork f) { hand_out(f); }
+__global__ void __launch_bounds__(kMost) k_fork_free(Fork f) {
+    const int lack = hand_out<kMost>(f, InMemory{f.refs_out}, f.need, f.free);
+    if (threadIdx.x == 0) *f.lack += lack;
+}
+
+// All of it but the copies for few rows and pages, with counts and lists in LDS: fork_drafts' 4 rows, 8 children and 190
+// pages TIME_SMALL us in all instead of 31.
+constexpr int kFewRows = 128, kFewPages = 4096;
+struct InLds {
+    int* r;
+    __device__ __forceinline__ void add(int x, int v) const { atomicAdd(&r[x], v); }
+    __device__ __forceinline__ int get(int x) const { return r[x]; }
+    __device__ __forceinline__ void set(int x, int v) const { r[x] = v; }
+};
+__global__ void __launch_bounds__(kMost) k_fork_small(Fork f) {
+    __shared__ int refs[kFewPages], free[kFewPages], need[kFewRows + 1], lack;
+    const int tid = threadIdx.x, w = tid >> 6;
+    for (int i = tid; i < f.pages; i += kMost) refs[i] = f.refs[i];
+    if (tid == 0) lack = 0;
+    __syncthreads();
+    for (int i = w; i < f.m + f.n; i += kMost / 64) {
+        if (i < f.m) {
+            const int wants = child_row(f, InLds{refs}, &lack, i);
+            if ((tid & 63) == 0) need[i] = wants;
+        } else {
+            end_row(f, InLds{refs}, i - f.m);
+        }
+    }
+    __syncthreads();
+    const int short_of = hand_out<kMost>(f, InLds{refs}, need, free);
+    __syncthreads();
+    const int given = need[f.m];
+    for (int i = tid; i < f.pages; i += kMost) f.refs_out[i] = refs[i];
+    for (int i = tid; i < given; i += kMost) f.free[i] = free[i];
+    for (int i = tid; i <= f.m; i += kMost) f.need[i] = need[i];
+    if (tid == 0) *f.lack = lack + short_of;
+    // (a row's wave is the one that wrote it)
+    for (int j = w; j < f.m; j += kMost / 64) fill_row(f, free, j, need[j], given);
+}
 
 // Workgroup (child, y, z): positions of the child's last page, half a cache (keys or values) and a share of the pieces
 // each; the first one fills in the child's wanted entries as well.
 __global__ void __launch_bounds__(kT) k_fork_copy(Fork f, CopySet set, int fill) {
     const int j = blockIdx.x, first = f.need[j], given = f.need[f.m], src = f.source[j];
-    if (fill && blockIdx.y == 0 && blockIdx.z == 0) {
-        int32_t* const row = f.table_out + j * f.out_stride;
-        int at = first, total;
-        for (int i0 = 0; i0 < f.width; i0 += kT) {
-            const int i = i0 + threadIdx.x;
-            const bool want = i < f.width && row[i] == kWanted;
-            const int k = at + scan(want, &total);
-            if (want) row[i] = k < given ? f.free[k] : -1;
-            at += total;
-        }
-    }
+    if (fill && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 64) fill_row(f, f.free, j, first, given);
     if (src < 0 || first >= given || (int)blockIdx.y >= 2 * set.n) return;
     const int dst = f.free[first], n = f.len_out[j] % f.ps;         // (the copy's page is the first that the child wants)
     const Copied& c = set.c[blockIdx.y >> 1];
@@ -208,18 +262,27 @@ __global__ void __launch_bounds__(kT) k_fork_copy(Fork f, CopySet set, int fill)
     const int64_t sp = val ? c.vp : c.kp, sh = val ? c.vh : c.kh, sr = val ? c.vr : c.kr;
     const char* const from = base + src * sp;
     char* const to = base + dst * sp;
-    const int per = n * c.chunks;
-    for (int64_t i = blockIdx.z * kT + threadIdx.x; i < (int64_t)c.G * per; i += gridDim.z * kT) {
-        const int g = (int)(i / per), r = (int)(i - (int64_t)g * per), q = r / c.chunks, x = r - q * c.chunks;
-        const int64_t at = g * sh + q * sr + 16 * x;
-        *(u32x4*)(to + at) = *(const u32x4*)(from + at);
+    const unsigned per = n * c.chunks, all = c.G * per, step = gridDim.z * kT;      // (below 2^30)
+    constexpr int AHEAD = 4;                  // pieces on their way
+    for (unsigned i0 = blockIdx.z * kT + threadIdx.x; i0 < all; i0 += AHEAD * step) {
+        u32x4 x[AHEAD];
+        int64_t at[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const unsigned i = min(i0 + k * step, all - 1), g = i / per, r = i - g * per, q = r / c.chunks;
+            at[k] = g * sh + q * sr + 16 * (r - q * c.chunks);
+            x[k] = *(const u32x4*)(from + at[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * step < all) *(u32x4*)(to + at[k]) = x[k];
     }
     if (c.ks && blockIdx.z == 0) {
         uint8_t* const scale = val ? c.vs : c.ks;
         const int64_t tp = val ? c.vsp : c.ksp, th = val ? c.vsh : c.ksh;
-        const int blocks = (n + kPageUnit - 1) / kPageUnit;
-        for (int i = threadIdx.x; i < c.G * blocks; i += kT) {
-            const int g = i / blocks, u = i - g * blocks;
+        const unsigned blocks = (n + kPageUnit - 1) / kPageUnit;
+        for (unsigned i = threadIdx.x; i < c.G * blocks; i += kT) {
+            const unsigned g = i / blocks, u = i - g * blocks;
             scale[dst * tp + g * th + u] = scale[src * tp + g * th + u];
         }
     }
@@ -263,7 +326,7 @@ int loopspec_fork_pages(const loopspec_fork_args* args, const loopspec_paged_cac
         if (rc || caches[i].page_size != ps || caches[i].n_pages != args->n_pages) return LOOPSPEC_EINVAL;
         const int e = eight ? 1 : 2;
         *d = Copied{(char*)c.k, (char*)c.v, s.k, s.v, c.kp * e, c.kh * e, c.ks * e, c.vp * e, c.vh * e, c.vs * e,
-                    s.kp, s.kh, s.vp, s.vh, c.G, c.D * e / 16};
+                    s.kp, s.kh, s.vp, s.vh, (unsigned)c.G, (unsigned)(c.D * e / 16)};
         return LOOPSPEC_OK;
     };
     CopySet set{};
@@ -275,18 +338,23 @@ int loopspec_fork_pages(const loopspec_fork_args* args, const loopspec_paged_cac
            args->seq_len_out_dev, args->table_out_dev, args->refs_out_dev, args->short_dev, ws, ws + m + 1, ws + 2 * m + 1};
     hipStream_t st = (hipStream_t)stream;
     void* kargs[] = {&f};
-    auto run = [&](const void* k, dim3 grid, void** a) { return hipLaunchKernel(k, grid, dim3(kT), a, 0, st) == hipSuccess; };
-    if (!run((const void*)k_fork_start, dim3((f.pages + kT - 1) / kT), kargs)) return LOOPSPEC_EHIP;
-    if (n + m && !run((const void*)k_fork_rows, dim3(n + m), kargs)) return LOOPSPEC_EHIP;
-    if (!m) return LOOPSPEC_OK;
-    if (!run((const void*)k_fork_free, dim3(1), kargs)) return LOOPSPEC_EHIP;
+    auto run = [&](const void* k, dim3 grid, dim3 block, void** a) { return hipLaunchKernel(k, grid, block, a, 0, st) == hipSuccess; };
     int fill = 1;
+    if (n + m <= kFewRows && f.pages <= kFewPages) {
+        if (!run((const void*)k_fork_small, dim3(1), dim3(kMost), kargs)) return LOOPSPEC_EHIP;
+        fill = 0;
+    } else {
+        if (!run((const void*)k_fork_start, dim3((f.pages + kT - 1) / kT), dim3(kT), kargs)) return LOOPSPEC_EHIP;
+        if (!run((const void*)k_fork_rows, dim3((n + m + kT / 64 - 1) / (kT / 64)), dim3(kT), kargs)) return LOOPSPEC_EHIP;
+        if (m && !run((const void*)k_fork_free, dim3(1), dim3(kMost), kargs)) return LOOPSPEC_EHIP;
+    }
+    if (!m) return LOOPSPEC_OK;
     for (int i = 0; i < n_caches || fill; i += kMany, fill = 0) {
         set.n = std::min(kMany, n_caches - i);
         for (int k = 0; k < set.n; ++k) describe(i + k, &set.c[k]);
         void* cargs[] = {&f, &set, &fill};
         const int y = std::max(1, 2 * set.n), z = std::max(1, std::min(16, 1024 / (y * m)));
-        if (!run((const void*)k_fork_copy, dim3(m, y, z), cargs)) return LOOPSPEC_EHIP;
+        if (!run((const void*)k_fork_copy, dim3(m, y, z), dim3(kT), cargs)) return LOOPSPEC_EHIP;
     }
     return LOOPSPEC_OK;
 }

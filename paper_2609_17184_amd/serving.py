@@ -288,23 +288,31 @@ def fork_pages(seq_len, table, parent, refs, caches, prefix_len: int = 0, window
     caches = list(caches)
     _need(bool(caches), "caches: one or more")
     dev, n_pages, page_size = caches[0].device, caches[0].n_pages, caches[0].page_size
-    _need(all(c.device == dev and c.n_pages == n_pages and c.page_size == page_size for c in caches),
-          "caches: on one device, of equal n_pages and page_size")
+    cs, sc = (B.PagedCacheC * len(caches))(), (B.PageScalesC * len(caches))()
+    for i, c in enumerate(caches):
+        if c.n_pages != n_pages or c.page_size != page_size or c.device != dev:
+            raise ValueError("caches: on one device, of equal n_pages and page_size")
+        cs[i] = c._for(torch.float16)._obj
+        if c._scales_ref is not None:
+            sc[i] = c._scales
     n, m = _size(seq_len.shape[0], "seq_len"), _size(parent.shape[0], "parent")
-    made = [torch.empty(shape, dtype=torch.int32, device=dev) for shape in ((m,), (m, table.shape[-1]), (n_pages,), (1,))]
-    a = B.ForkArgs(n, m, page_size, n_pages, _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table"),
-                   table.stride(0), _size(table.shape[1], "table"), _ints(parent, (m,), dev, "parent"),
-                   _ints(refs, (n_pages,), dev, "refs"), *(min(_whole(x, what), 1 << 30) for x, what in
-                                                           ((prefix_len, "prefix_len"), (window, "window"), (sinks, "sinks"), (room, "room"))),
-                   made[0].data_ptr(), made[1].data_ptr(), made[1].stride(0), made[2].data_ptr(), made[3].data_ptr())
+    lens, rows = _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table")
+    width = _size(table.shape[1], "table")
+    of, counts = _ints(parent, (m,), dev, "parent"), _ints(refs, (n_pages,), dev, "refs")
+    prefix_len, window, sinks, room = (min(_whole(x, what), 1 << 30) for x, what in (
+        (prefix_len, "prefix_len"), (window, "window"), (sinks, "sinks"), (room, "room")))
+    new_len = torch.empty((m,), dtype=torch.int32, device=dev)
+    new_table = torch.empty((m, width), dtype=torch.int32, device=dev)
+    new_refs = torch.empty((n_pages,), dtype=torch.int32, device=dev)
+    short = torch.empty((1,), dtype=torch.int32, device=dev)
+    a = B.ForkArgs(n, m, page_size, n_pages, lens, rows, table.stride(0), width, of, counts, prefix_len, window, sinks, room,
+                   new_len.data_ptr(), new_table.data_ptr(), width, new_refs.data_ptr(), short.data_ptr())
     L = B.load_library()
-    cs = (B.PagedCacheC * len(caches))(*(c._for(torch.float16)._obj for c in caches))
-    sc = (B.PageScalesC * len(caches))(*(B.PageScalesC() if c._scales_ref is None else c._scales for c in caches))
     nbytes = L.loopspec_fork_pages_workspace_bytes(m, n_pages)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _check(_launch(dev, L.loopspec_fork_pages, ctypes.byref(a), cs, sc, len(caches), ws.data_ptr(), nbytes),
            "loopspec_fork_pages")
-    return tuple(made)
+    return new_len, new_table, new_refs, short
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
