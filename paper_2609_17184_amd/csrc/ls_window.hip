@@ -49,8 +49,8 @@ struct WinArgs {
     uint16_t* out;
     int64_t ot, oh;
     float* lse;
-    float* part;                              // [rows][NP + NO][D], rows = tokens x heads
-    float* ml;                                // [rows][NP + NO][2]: reference (base 2), sum
+    float* part;                              // [rows][slots][D], rows = tokens x heads
+    float* ml;                                // [rows][slots][2]: reference (base 2), sum
     float c;                                  // scale * log2(e)
     int H, per;                               // query heads; per key/value head
     int W, S;                                 // window (kAll: none), sinks
@@ -58,6 +58,7 @@ struct WinArgs {
     int NO, CT;                               // chunks at most, tiles of 32 positions per chunk
     int NP, CP;                               // the prefix for the rows of all sequences at once: chunks (0: it is not), tiles per chunk
     int rb, rows, ptasks;                     // blocks of these rows, rows of a block, workgroups
+    int slots, fold;                          // partial results of a row; the own tasks take the prefix's in and finish the row
 };
 
 // ---- 8-bit operands
@@ -334,8 +335,8 @@ struct Tasks {
             t.hi = t.position(t.rows - 1, a.per);
             t.s = seen(b, a, cap, t.lo, t.hi);
             const int n_chunks = chunks_of(t.s.n, a.CT), tiles = (t.s.n + 1) / 2, each = (tiles + n_chunks - 1) / n_chunks;
-            t.splits = a.NP + n_chunks;
-            t.split = a.NP + ch;
+            t.splits = a.fold ? 1 : a.NP + n_chunks;
+            t.split = a.fold ? 0 : a.NP + ch;
             t.b0 = 2 * ch * each;
             t.b1 = min(t.s.n, t.b0 + 2 * each);
             t.low = max(t.lo, b.prefix) - a.W;
@@ -836,8 +837,14 @@ __device__ __forceinline__ void put_out(uint16_t* o, int m, const float (&v)[E])
     }
 }
 
+// the largest reference of a row's partial results from the prefix and `ref`
+__device__ __forceinline__ float top_of(const WinArgs& a, size_t row, float ref) {
+    for (int s = 0; s < a.NP; ++s) ref = fmaxf(ref, a.ml[(row * a.slots + s) * 2]);
+    return ref;
+}
+
 // a wave's rows without the workgroup's other waves: partial results, or whole ones
-template <bool BF, bool Q8, int D, int NR>
+template <bool BF, bool Q8, int D, int NR, bool FOLD>
 __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t end, Rows<BF, Q8, D, NR>& r, int row0) {
     constexpr int E = D / 16;
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
@@ -849,7 +856,7 @@ __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t e
         const int tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
         const size_t at = (size_t)tok * a.H + h;
         if (t.splits > 1) {
-            const size_t slot = at * (a.NP + a.NO) + t.split;
+            const size_t slot = at * a.slots + t.split;
             float* const p = a.part + slot * D;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -857,6 +864,23 @@ __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t e
                 for (int e = 0; e < E; ++e) p[column_of<Q8, E>(4 * gq + k, e)] = r.o[rt][e][k];
             if (gq == 0) a.ml[slot * 2] = r.ref[rt], a.ml[slot * 2 + 1] = r.sum[rt];
         } else {
+            if (FOLD && a.fold && r.hi[rt] >= 0) {
+                const float top = top_of(a, at, r.ref[rt]), f = __builtin_amdgcn_exp2f(r.ref[rt] - top);
+                r.sum[rt] *= f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) r.o[rt][e] *= f;
+                for (int s = 0; s < a.NP; ++s) {
+                    const size_t slot = at * a.slots + s;
+                    const float* const p = a.part + slot * D;
+                    const float g = __builtin_amdgcn_exp2f(a.ml[slot * 2] - top);
+                    r.sum[rt] = fmaf(a.ml[slot * 2 + 1], g, r.sum[rt]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) r.o[rt][e][k] = fmaf(p[column_of<Q8, E>(4 * gq + k, e)], g, r.o[rt][e][k]);
+                }
+                r.ref[rt] = top;
+            }
             const float inv = r.sum[rt] == 0.f ? 0.f : 1.0f / r.sum[rt];
             uint16_t* const o = a.out + (int64_t)tok * a.ot + h * a.oh;
 #pragma unroll
@@ -879,7 +903,7 @@ struct MeetLds {
 
 // the four waves' results of a workgroup's task, summed and stored
 template <bool BF, bool Q8, int D, int NR>
-__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t end, Rows<BF, Q8, D, NR>& r, MeetLds<D, NR>& l) {
+__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix, int64_t end, Rows<BF, Q8, D, NR>& r, MeetLds<D, NR>& l) {
     constexpr int E = D / 16;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, n = lane & 15, gq = lane >> 4;
     r.finish(end);
@@ -914,10 +938,22 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t en
             const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
             const size_t at = (size_t)tok * a.H + h;
             if (t.splits > 1) {
-                const size_t slot = at * (a.NP + a.NO) + t.split;
+                const size_t slot = at * a.slots + t.split;
                 *(f32x4*)(a.part + slot * D + d) = v;
                 if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
             } else {
+                if (a.fold && t.position(row, a.per) >= prefix) {       // (others see nothing)
+                    const float top = top_of(a, at, tp), f = __builtin_amdgcn_exp2f(tp - top);
+                    v *= f, sm *= f, tp = top;
+                    for (int s = 0; s < a.NP; ++s) {
+                        const size_t slot = at * a.slots + s;
+                        const float g = __builtin_amdgcn_exp2f(a.ml[slot * 2] - top);
+                        sm = fmaf(a.ml[slot * 2 + 1], g, sm);
+                        const f32x4 x = *(const f32x4*)(a.part + slot * D + d);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = fmaf(x[k], g, v[k]);
+                    }
+                }
                 const float inv = sm == 0.f ? 0.f : 1.0f / sm;
                 const u32x2 o = {pack2<BF>(v[0] * inv, v[1] * inv), pack2<BF>(v[2] * inv, v[3] * inv)};
                 *(u32x2*)(a.out + (int64_t)tok * a.ot + h * a.oh + d) = o;
@@ -928,48 +964,71 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int64_t en
     }
 }
 
-// One workgroup per task.  WIDE: blocks of 64 * NR rows, the four waves on different rows; else of 16 * NR rows, the four
-// waves on every fourth tile.  Workgroups below ptasks take the prefix for the rows of all sequences at once, the
-// others the sequences' tasks, in blocks of 16 rows where these are not WIDE_OWN.
-template <bool BF, bool Q8, int D, int NR, bool WIDE, bool WIDE_OWN>
-__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
-    constexpr int NO = WIDE && !WIDE_OWN ? 1 : NR;
-    union Lds {
-        StageLds<WIDE ? D : 16> st[2];
-        MeetLds<WIDE && WIDE_OWN ? 16 : D, WIDE ? 1 : NR> m;
-    };
-    __shared__ Lds l;
-    const int64_t end = b.prefix + (int64_t)b.width * c.unit * kPageUnit;
-    const bool prefix = (int)blockIdx.x < a.ptasks;
-    if (prefix && WIDE != WIDE_OWN) {
-        if constexpr (WIDE && !WIDE_OWN) {
-            Task t;
-            if (!prefix_task(c, b, a, t)) return;
-            Rows<BF, Q8, D, NR> r;
-            walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l.st, r);
-            store<BF, Q8, D, NR>(a, t, kAll, r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
-        }
-        return;
-    }
+// The next task of a workgroup or wave: the prefix's for workgroups below ptasks, which have one, else the sequences'.
+struct Asked {
     Tasks all;
-    for (int64_t task = (int)blockIdx.x - a.ptasks;; task += gridDim.x - a.ptasks) {
-        Task t;
+    int64_t task;
+    int step;
+    bool prefix, done = false;
+
+    __device__ __forceinline__ Asked(const WinArgs& a, int waves) : prefix((int)blockIdx.x < a.ptasks) {
+        const int w = waves > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+        task = (int64_t)((int)blockIdx.x - a.ptasks) * waves + w;
+        step = ((int)gridDim.x - a.ptasks) * waves;
+    }
+    __device__ __forceinline__ bool next(const PagedCache& c, const PagedBatch& b, const WinArgs& a, Task& t) {
         if (prefix) {
-            if (!prefix_task(c, b, a, t)) return;
-        } else {
-            if (!all.find(c, b, a, task, t)) return;
-            if (t.split >= t.splits) continue;                      // fewer chunks than the sequence's longest block of rows
+            if (done) return false;
+            done = true;
+            return prefix_task(c, b, a, t);
         }
-        Rows<BF, Q8, D, NO> r;
-        if constexpr (WIDE_OWN) {
-            __syncthreads();                  // an earlier task's LDS is read out
-            walk_wide<BF, Q8, D, NO>(c, sc, b, a, t, l.st, r);
-            store<BF, Q8, D, NO>(a, t, end, r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NO * 16);
-        } else {
-            walk<BF, Q8, D, NO>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
-            meet<BF, Q8, D, NO>(a, t, prefix ? (int64_t)kAll : end, r, l.m);
+        for (;;) {
+            if (!all.find(c, b, a, task, t)) return false;
+            task += step;
+            if (t.split < t.splits) return true;                    // (fewer chunks than the sequence's longest block of rows)
         }
-        if (prefix) return;
+    }
+    __device__ __forceinline__ int64_t end(const PagedCache& c, const PagedBatch& b) const {
+        return prefix ? (int64_t)kAll : b.prefix + (int64_t)b.width * c.unit * kPageUnit;
+    }
+};
+
+// A workgroup per task of up to 64 * NR rows, the four waves on different rows.
+template <bool BF, bool Q8, int D, int NR>
+__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window_wide(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
+    __shared__ StageLds<D> l[2];
+    Asked asked(a, 1);
+    Task t;
+    while (asked.next(c, b, a, t)) {
+        Rows<BF, Q8, D, NR> r;
+        __syncthreads();                      // an earlier task's LDS is read out
+        walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l, r);
+        store<BF, Q8, D, NR, false>(a, t, asked.end(c, b), r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
+    }
+}
+
+// A workgroup per task of up to 16 * NR rows, the four waves on every fourth tile.
+template <bool BF, bool Q8, int D, int NR>
+__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
+    __shared__ MeetLds<D, NR> l;
+    Asked asked(a, 1);
+    Task t;
+    while (asked.next(c, b, a, t)) {
+        Rows<BF, Q8, D, NR> r;
+        walk<BF, Q8, D, NR>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
+        meet<BF, Q8, D, NR>(a, t, b.prefix, asked.end(c, b), r, l);
+    }
+}
+
+// A wave per task of up to 16 rows.
+template <bool BF, bool Q8, int D>
+__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window_waves(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
+    Asked asked(a, 4);
+    Task t;
+    while (asked.next(c, b, a, t)) {
+        Rows<BF, Q8, D, 1> r;
+        walk<BF, Q8, D, 1>(c, sc, b, a, t, t.b0, 2, r);
+        store<BF, Q8, D, 1, true>(a, t, asked.end(c, b), r, 0);
     }
 }
 
@@ -991,8 +1050,8 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     int n = a.NP + chunks_of(seen(b, a, cap, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
     if (n == 1) return;                       // finished where it was computed
     if (place < 0) n = 0;                     // (the prefix was worked on for all rows)
-    const float* ml = a.ml + (size_t)row * (a.NP + a.NO) * 2;
-    const float* part = a.part + (size_t)row * (a.NP + a.NO) * D;
+    const float* ml = a.ml + (size_t)row * a.slots * 2;
+    const float* part = a.part + (size_t)row * a.slots * D;
     const int gl = D > 64 ? 32 : D / 4, groups = 64 / gl, g = lane / gl, d = lane % gl * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float top = kNone, sum = 0.f;
@@ -1037,11 +1096,14 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
 }
 
+enum { WIDE, SMALL, SMALL_2, WAVES };         // kernels
+
 struct Plan {
     int nr;                                   // tiles of 16 rows a wave has
     bool wide, wide_own;
-    int RT, NO, CT, NP, CP, rb, rows, ptasks;
-    int64_t tasks;
+    int RT, NO, CT, NP, CP, rb, rows, ptasks, groups;
+    int own, before, slots;                   // kernels of the sequences' tasks and of the prefix's; partial results of a row
+    bool fold;
 };
 
 // Rows per block, chunks and workgroups from the sizes that the host knows.
@@ -1079,18 +1141,30 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
     const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
     const int64_t blocks = std::min(rows, (rows + p->RT - 1) / p->RT + b.B) * c.G;
-    // about 1024 tasks where the tables are full, of at least two tiles a wave; prompts that fill the card are not cut
+    // About 1024 tasks where the tables are full, of at least two tiles a wave and 16 in all; prompts that fill the card are
+    // not cut.
     if (p->wide_own && blocks >= slots)
         p->CT = (int)tiles;
     else
-        p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(p->wide_own ? 16 : 8, (tiles * blocks / 1024 + 1) / 2 * 2));
+        p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(16, (tiles * blocks / 1024 + 1) / 2 * 2));
     p->NO = (int)((tiles + p->CT - 1) / p->CT);
-    p->tasks = blocks * p->NO;
+    const int64_t tasks = blocks * p->NO;
+    // A wave per task where there are enough short ones: 1024 tasks of 5 tiles (128 sequences of 1 to 259 positions, 8 heads)
+    // 22 us, by workgroups 32; 512 of 5 16.0 and 16.8.
+    const bool by_wave = !p->wide_own && p->CT <= 16 && tasks >= slots;
+    p->own = p->wide_own ? WIDE : by_wave ? WAVES : p->wide || p->nr == 1 ? SMALL : SMALL_2;
+    p->before = p->wide ? WIDE : p->nr == 1 ? SMALL : SMALL_2;
+    // Workgroups that go on from task to task fill the card once (64 rows over 4096 of 12000 positions 170 us, with twice as
+    // many 174); tasks of many rows are too unequal for that.
+    p->groups = (int)std::min<int64_t>(by_wave ? (tasks + 3) / 4 : tasks, p->wide_own ? 16384 : slots);
+    // Where the prefix has a launch of its own and a row's own positions are one task, that one finishes the row.
+    p->fold = together && p->own != p->before && p->NO == 1;
+    p->slots = p->fold ? p->NP : p->NP + p->NO > 1 ? p->NP + p->NO : 0;
     return LOOPSPEC_OK;
 }
 
 uint64_t bytes_of(const PagedCache& c, const PagedBatch& b, int H, const Plan& p) {
-    return p.NP + p.NO > 1 ? (uint64_t)b.T * H * (p.NP + p.NO) * (c.D + 2) * 4 : 0;
+    return (uint64_t)b.T * H * p.slots * (c.D + 2) * 4;
 }
 
 int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales, const loopspec_paged_batch* batch, int n_heads,
@@ -1107,22 +1181,25 @@ int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
 }
 
 template <bool BF, bool Q8, int D>
-const void* kernel_of(const Plan& p) {
-    if (p.wide_own) return (const void*)k_window<BF, Q8, D, 2, true, true>;
-    if (p.wide) return (const void*)k_window<BF, Q8, D, 2, true, false>;
-    return p.nr == 1 ? (const void*)k_window<BF, Q8, D, 1, false, false> : (const void*)k_window<BF, Q8, D, 2, false, false>;
+const void* kernel_of(int k) {
+    switch (k) {
+        case WIDE: return (const void*)k_window_wide<BF, Q8, D, 2>;
+        case SMALL: return (const void*)k_window<BF, Q8, D, 1>;
+        case SMALL_2: return (const void*)k_window<BF, Q8, D, 2>;
+        default: return (const void*)k_window_waves<BF, Q8, D>;
+    }
 }
 template <bool BF, bool Q8>
-const void* kernel_of(int D, const Plan& p) {
+const void* kernel_of(int D, int k) {
 #ifdef LSW_DEV
-    return D != 128 ? (const void*)k_window<false, true, 96, 2, true, true> : BF && !Q8 ? (p.wide_own ? (const void*)k_window<true, false, 128, 2, true, true> : (const void*)k_window<true, false, 128, 1, false, false>) : BF ? (const void*)k_window<true, true, 128, 2, true, false> : (const void*)k_window<false, true, 128, 1, false, false>;
+    return D != 128 ? (const void*)k_window_wide<false, true, 96, 2> : BF && !Q8 ? (k == WIDE ? (const void*)k_window_wide<true, false, 128, 2> : k == WAVES ? (const void*)k_window_waves<true, false, 128> : (const void*)k_window<true, false, 128, 1>) : BF ? (k == WIDE ? (const void*)k_window_wide<true, true, 128, 2> : (const void*)k_window_waves<true, true, 128>) : (const void*)k_window<false, true, 128, 1>;
 #else
     switch (D) {
-        case 16: return kernel_of<BF, Q8, 16>(p);
-        case 32: return kernel_of<BF, Q8, 32>(p);
-        case 64: return kernel_of<BF, Q8, 64>(p);
-        case 96: return kernel_of<BF, Q8, 96>(p);
-        default: return kernel_of<BF, Q8, 128>(p);
+        case 16: return kernel_of<BF, Q8, 16>(k);
+        case 32: return kernel_of<BF, Q8, 32>(k);
+        case 64: return kernel_of<BF, Q8, 64>(k);
+        case 96: return kernel_of<BF, Q8, 96>(k);
+        default: return kernel_of<BF, Q8, 128>(k);
     }
 #endif
 }
@@ -1164,16 +1241,27 @@ int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     WinArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
-              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * (p.NP + p.NO) * c.D, cs, args->n_heads,
+              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.slots * c.D, cs, args->n_heads,
               args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT,
-              p.NP, p.CP, p.rb, p.rows, p.ptasks};
+              p.NP, p.CP, p.rb, p.rows, 0, p.slots, p.fold};
     hipStream_t st = (hipStream_t)stream;
     const bool bf = cache->dtype == LOOPSPEC_BF16, q8 = scales != nullptr;
-    void* kargs[] = {&c, &s, &b, &a};
-    const void* f = bf ? q8 ? kernel_of<true, true>(c.D, p) : kernel_of<true, false>(c.D, p)
-                       : q8 ? kernel_of<false, true>(c.D, p) : kernel_of<false, false>(c.D, p);
-    if (hipLaunchKernel(f, dim3((unsigned)(p.ptasks + std::min<int64_t>(p.tasks, 16384))), dim3(kT), kargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
-    if (p.NP + p.NO > 1) {
+    auto run = [&](int kernel, int groups) {
+        void* kargs[] = {&c, &s, &b, &a};
+        const void* f = bf ? q8 ? kernel_of<true, true>(c.D, kernel) : kernel_of<true, false>(c.D, kernel)
+                           : q8 ? kernel_of<false, true>(c.D, kernel) : kernel_of<false, false>(c.D, kernel);
+        return hipLaunchKernel(f, dim3((unsigned)groups), dim3(kT), kargs, 0, st) == hipSuccess;
+    };
+    if (p.ptasks && p.own != p.before) {
+        a.ptasks = p.ptasks;
+        if (!run(p.before, p.ptasks)) return LOOPSPEC_EHIP;
+        a.ptasks = 0;
+        if (!run(p.own, p.groups)) return LOOPSPEC_EHIP;
+    } else {
+        a.ptasks = p.ptasks;
+        if (!run(p.own, p.ptasks + p.groups)) return LOOPSPEC_EHIP;
+    }
+    if (p.NP + p.NO > 1 && !p.fold) {
         void* jargs[] = {&c, &b, &a};
         const void* j = bf ? (const void*)k_window_join<true> : (const void*)k_window_join<false>;
         if (hipLaunchKernel(j, dim3((unsigned)((rows + 3) / 4)), dim3(kT), jargs, 0, st) != hipSuccess) return LOOPSPEC_EHIP;
