@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kT) k_append8(PagedCache c, PageScales sc, Pag
         const int seq = paged_place(b, t, &place);
         Run r{0, 0, place, -1, -1, -1, -1};
         if (seq >= 0 && place >= 0) {
-            const int start = b.q_start ? b.q_start[seq] : t, end = min(b.q_start ? b.q_start[seq + 1] : t + 1, b.T);
+            const int start = b.q_start ? max(b.q_start[seq], 0) : t, end = min(b.q_start ? b.q_start[seq + 1] : t + 1, b.T);
             r.keep = (int)(place & 15);
             if (t == start || r.keep == 0) {
                 r.n = min(16 - r.keep, end - t);
@@ -205,10 +205,14 @@ __global__ void __launch_bounds__(kT) k_append8(PagedCache c, PageScales sc, Pag
         for (int j = tid; j < r.n * half; j += kT) {
             const int t = j / half, f = j - t * half;
             const double turns = (double)(b.prefix + r.place + t) * a.freq[f] * 0.15915494309189533577;
+            // the fraction of a turn in two floats: one alone is off by 2^-26, which the codes' rounding shows (a key's error
+            // against 64 bits 8e-5 instead of 4e-5)
+            const double part = turns - rint(turns);
+            const float a0 = (float)part, a1 = 6.2831853f * (float)(part - (double)a0);
             float sn, cn;
-            sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cn);
-            cs[t][f] = cn;
-            cs[t][64 + f] = sn;
+            sincospif(2.0f * a0, &sn, &cn);
+            cs[t][f] = fmaf(-a1, sn, cn);
+            cs[t][64 + f] = fmaf(a1, cn, sn);
         }
         __syncthreads();
         const int first = by * kW + w, step = slices * kW;
