@@ -572,7 +572,8 @@ int loopspec_prefix_attention(const loopspec_paged_cache* cache, const loopspec_
  * Every 16 positions of a page, head by head, have a scale 2^(b - 127), b the byte
  * at k_dev + p * k_page + g * k_head + i for positions 16 i .. 16 i + 15 of head
  * g of page p (values alike); an element stands for code * scale.  b = 255 makes
- * its positions NaN. */
+ * its positions NaN.  Values' scales below 2^-64 count as 2^-64 (the append makes
+ * none). */
 typedef struct {
     void *k_dev, *v_dev;
     int64_t k_page, k_head, v_page, v_head;
@@ -602,8 +603,9 @@ int loopspec_rope_append_quantized(const loopspec_paged_cache* cache, const loop
  * cache is read.  Products are of the queries' type with fp32 sums; the weights are
  * rounded to that type (in fp16 those below 2^-32 of a row's largest vanish beside
  * their share of the sum; over 8-bit pages in fp16 a weight counts times its
- * value's scale for that).  A row's result does not depend on the other
- * sequences' contents.  window, sinks: >= 0.  workspace: 16-byte aligned, its
+ * value's scale for that).  Scores have to be finite in fp32; of those larger
+ * than 2^18 ones that differ by less than 2^-19 of themselves may count alike.  A
+ * row's result does not depend on the other sequences' contents.  window, sinks: >= 0.  workspace: 16-byte aligned, its
  * contents on entry do not matter.  Errors: EINVAL (arguments, workspace too
  * small; checked before any launch; tokens x heads up to 2^25), EHIP. */
 int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,

@@ -406,13 +406,17 @@ struct Rows {
     }
     struct Weights {
         float x[2][4], part, sum;
+        template <bool CAP = false>
         __device__ __forceinline__ void take(const f32x4 (&s)[2], float ref, const float (&ck)[2], const float (&ev)[2]) {
             float p[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float z = JOINT ? ev[h] - ref : -ref;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], ck[h], z));
+                for (int i = 0; i < 4; ++i) {
+                    x[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], ck[h], z));
+                    if (CAP) x[h][i] = x[h][i] > high ? high : x[h][i];
+                }
                 p[h] = (x[h][0] + x[h][1]) + (x[h][2] + x[h][3]);
             }
             part = p[0] + p[1];
@@ -423,7 +427,9 @@ struct Rows {
         }
     };
     // A new reference for the lane's row if some weight of its is high: the largest score so far gets the weight
-    // 2^(kTop - kRoom).  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.
+    // 2^(kTop - kRoom).  The tile's other rows keep theirs, since a row's roundings follow its own scores alone.  Where fp32
+    // no longer holds a difference of a reference and a score, the reference is rounded down, so that the largest score's
+    // weight is not lost, and weights behind 2^kTop are cut off there: scores that near each other count alike.
     __device__ __forceinline__ void raise(int rt, const f32x4 (&s)[2], float part, const float (&ck)[2], const float (&ev)[2]) {
         part = fmaxf(part, __shfl_xor(part, 16));
         part = fmaxf(part, __shfl_xor(part, 32));
@@ -433,7 +439,9 @@ struct Rows {
             mx = fmaxf(mx, fmaf(fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])), ck[h], JOINT ? ev[h] : 0.f));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float now = part > high ? fmaxf(ref[rt], mx + (kRoom - kTop<BF>)) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
+        mx += kRoom - kTop<BF>;
+        if (fabsf(mx) > 0x1p18f) mx *= mx > 0.f ? 1.f - 0x1p-21f : 1.f + 0x1p-21f;
+        const float now = part > high ? fmaxf(ref[rt], mx) : ref[rt], al = __builtin_amdgcn_exp2f(ref[rt] - now);
         ref[rt] = now;
         sum[rt] *= al;
 #pragma unroll
@@ -454,7 +462,7 @@ struct Rows {
             for (int rt = 0; rt < NR; ++rt)
                 if (__any(w[rt].part > high)) {
                     raise(rt, s[rt], w[rt].part, ck, ev);
-                    w[rt].take(s[rt], ref[rt], ck, ev);
+                    w[rt].template take<true>(s[rt], ref[rt], ck, ev);
                 }
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) sum[rt] += w[rt].sum, p[rt] = w[rt].packed();
@@ -1151,7 +1159,7 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     const int64_t tasks = blocks * p->NO;
     // A wave per task where there are enough short ones: 1024 tasks of 5 tiles (128 sequences of 1 to 259 positions, 8 heads)
     // 22 us, by workgroups 32; 512 of 5 16.0 and 16.8.
-    const bool by_wave = !p->wide_own && p->CT <= 16 && tasks >= slots;
+    const bool by_wave = !p->wide_own && p->RT == 16 && p->CT <= 16 && tasks >= slots;
     p->own = p->wide_own ? WIDE : by_wave ? WAVES : p->wide || p->nr == 1 ? SMALL : SMALL_2;
     p->before = p->wide ? WIDE : p->nr == 1 ? SMALL : SMALL_2;
     // Workgroups that go on from task to task fill the card once (64 rows over 4096 of 12000 positions 170 us, with twice as
@@ -1191,9 +1199,6 @@ const void* kernel_of(int k) {
 }
 template <bool BF, bool Q8>
 const void* kernel_of(int D, int k) {
-#ifdef LSW_DEV
-    return D != 128 ? (const void*)k_window_wide<false, true, 96, 2> : BF && !Q8 ? (k == WIDE ? (const void*)k_window_wide<true, false, 128, 2> : k == WAVES ? (const void*)k_window_waves<true, false, 128> : (const void*)k_window<true, false, 128, 1>) : BF ? (k == WIDE ? (const void*)k_window_wide<true, true, 128, 2> : (const void*)k_window_waves<true, true, 128>) : (const void*)k_window<false, true, 128, 1>;
-#else
     switch (D) {
         case 16: return kernel_of<BF, Q8, 16>(k);
         case 32: return kernel_of<BF, Q8, 32>(k);
@@ -1201,7 +1206,6 @@ const void* kernel_of(int D, int k) {
         case 96: return kernel_of<BF, Q8, 96>(k);
         default: return kernel_of<BF, Q8, 128>(k);
     }
-#endif
 }
 
 }  // namespace
