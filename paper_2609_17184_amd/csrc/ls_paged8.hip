@@ -255,7 +255,7 @@ extern "C" int loopspec_rope_append_quantized(const loopspec_paged_cache* cache,
     int L = 1;
     while (L * 16 < c.D) L *= 2;
     const int items = a.H + 2 * c.G;
-    int per = b.q_start && b.T >= 8ll * b.B ? 16 : 1;
+    int per = b.T > 1 << 22 || (b.q_start && b.T >= 8ll * b.B) ? 16 : 1;    // (a grid holds 2^32 threads)
     const int x = (b.T + per - 1) / per;
     // Slices of the heads, each of which takes the run's angles again: 1001 runs of 36 heads 60.6 us in one, 67.0 in two;
     // 180 runs of 165 heads 54.9 in nine, 58.5 in four, 65.2 in two.  Workgroups of 256 threads, whose share of the angles

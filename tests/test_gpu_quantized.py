@@ -212,3 +212,35 @@ def test_refusals():
         serving.rope_append(q, n, n, cache, c.batch)
     with pytest.raises(LoopSpecError):
         serving.window_attention(q, cache, c.batch)
+
+
+def test_more_tokens_than_workgroups_of_one_token():
+    """Over four million sequences of one token, most of them without positions: rows of padding stay as they are, and no
+    launch is too large."""
+    from paper_2609_17184_amd import serving
+    T = (1 << 22) + 37
+    at = [0, 5, 16, 1 << 22, T - 1]
+    g = torch.Generator().manual_seed(12)
+    lens = torch.full((T,), -1, dtype=torch.int32)
+    tables = torch.full((T, 1), -1, dtype=torch.int32)
+    for i, t in enumerate(at):
+        lens[t], tables[t, 0] = 1 + 3 * i, i
+    q, k, v = (torch.zeros((T, 1, 16), dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    rows = [torch.randn((len(at), 1, 16), generator=g).to(torch.bfloat16) for _ in range(3)]
+    for x, r in zip((q, k, v), rows):
+        x[at] = r.to(DEV)
+    codes = [torch.zeros((len(at), 1, 16, 16), dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2)]
+    scales = [torch.zeros((len(at), 1, 1), dtype=torch.uint8, device=DEV).view(torch.float8_e8m0fnu) for _ in range(2)]
+    out = torch.full_like(q, 3.0)
+    serving.rope_append(q, k, v, serving.QuantizedCache(*codes, *scales), serving.Batch(lens.to(DEV), tables.to(DEV)), out=out)
+    assert torch.equal(out[at].cpu(), rows[0])
+    out[at] = 3.0
+    assert (out == 3.0).all()
+    for x, c, s in zip(rows[1:], codes, scales):
+        got = stored(c, s, 16)
+        for i in range(len(at)):
+            e = exponent(x[i].double().abs().max().reshape(1)).item()
+            if i == 0:
+                assert torch.equal(got[i, 0, 0], e4m3(x[i, 0].double() * 2.0 ** -e) * 2.0 ** e)
+            else:                             # (the positions below have the scale 2^-127, which grows to the new one's)
+                assert torch.equal(got[i, 0, 3 * i], e4m3(x[i, 0].double() * 2.0 ** -e) * 2.0 ** e)
