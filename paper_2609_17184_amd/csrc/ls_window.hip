@@ -34,6 +34,7 @@ namespace ls {
 namespace {
 
 constexpr int kT = 256;
+constexpr int kWideRows = 128, kFewRows = 16;  // rows of a block where the waves share positions, and where each has its own
 constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
 constexpr int kGroupsMax = 1 << 23;            // workgroups of the prefix, for the same reason
 constexpr int kAll = 1 << 30;                 // a window that holds every position
@@ -52,6 +53,7 @@ struct WinArgs {
     float* part;                              // [rows][slots][D], rows = tokens x heads
     float* ml;                                // [rows][slots][2]: reference (base 2), sum
     float c;                                  // scale * log2(e)
+    int D;
     int H, per;                               // query heads; per key/value head
     int W, S;                                 // window (kAll: none), sinks
     int RT;                                   // rows of a block
@@ -549,11 +551,11 @@ __device__ __forceinline__ void load_q(const WinArgs& a, const Task& t, int row0
     }
 }
 
-// Few rows (16 or 32): the wave takes the tiles at, at + step, ... of the task; the next tile's keys and values come into
+// Few rows (16): the wave takes the tiles at, at + step, ... of the task; the next tile's keys and values come into
 // the registers of this one's as soon as a product has read them.
-template <bool BF, bool Q8, int D, int NR>
+template <bool BF, bool Q8, int D>
 __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a,
-                                     const Task& t, int at, int step, Rows<BF, Q8, D, NR>& r) {
+                                     const Task& t, int at, int step, Rows<BF, Q8, D, 1>& r) {
     constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
     const int gq = (threadIdx.x & 63) >> 4;
     r.start(t, b.prefix, a.per, 0);
@@ -573,8 +575,8 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, x));
         info[h] = x.info;
     }
-    u32x4 q[NR][NS];
-    load_q<BF, Q8, D, NR>(a, t, 0, q);
+    u32x4 q[1][NS];
+    load_q<BF, Q8, D, 1>(a, t, 0, q);
     const bool several = t.position(0, a.per) != t.hi;
     const Inner in = inner(b, a, t, t.lo, t.hi);
     for (int known = 31;; known += 32) {      // the last tile whose place the lanes hold
@@ -588,17 +590,11 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         }
         const bool more = at + step < t.b1;
         Where nx[2];
-        f32x4 s[NR][2];
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 s[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
         for (int k = 0; k < NS; ++k)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4 f = xk[h].get(k);
-#pragma unroll
-                for (int rt = 0; rt < NR; ++rt) s[rt][h] = mfma16<BF>(f, q[rt][k], s[rt][h]);
-            }
+            for (int h = 0; h < 2; ++h) s[0][h] = mfma16<BF>(xk[h].get(k), q[0][k], s[0][h]);
         if (more)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -609,17 +605,12 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         Blk x[2];
         if (part)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x[h] = look(b, t, at + h);
-        if (part)
-#pragma unroll
-            for (int rt = 0; rt < NR; ++rt) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (bad[h]) s[rt][h] = f32x4{NAN, NAN, NAN, NAN};
-                    r.hide(rt, x[h], s[rt][h], t.lo, t.hi, a);
-                }
+            for (int h = 0; h < 2; ++h) {
+                x[h] = look(b, t, at + h);
+                if (bad[h]) s[0][h] = f32x4{NAN, NAN, NAN, NAN};
+                r.hide(0, x[h], s[0][h], t.lo, t.hi, a);
             }
-        u32x4 w[NR];
+        u32x4 w[1];
         r.weights(s, w, ck, ev);
         uint32_t v[8][EW];
 #pragma unroll
@@ -647,8 +638,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
             u32x4 f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], sel);
-#pragma unroll
-            for (int rt = 0; rt < NR; ++rt) r.o[rt][e] = mfma16<BF>(f, w[rt], r.o[rt][e]);
+            r.o[0][e] = mfma16<BF>(f, w[0], r.o[0][e]);
         }
         if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at);
     }
@@ -845,10 +835,45 @@ __device__ __forceinline__ void put_out(uint16_t* o, int m, const float (&v)[E])
     }
 }
 
-// the largest reference of a row's partial results from the prefix and `ref`
-__device__ __forceinline__ float top_of(const WinArgs& a, size_t row, float ref) {
-    for (int s = 0; s < a.NP; ++s) ref = fmaxf(ref, a.ml[(row * a.slots + s) * 2]);
-    return ref;
+// The prefix's partial results of a row are taken in: N of its columns v (whose first is `p` in a partial result), its
+// reference and sum.  Several at a time, since each comes from memory.
+template <int N, class Column>
+__device__ __forceinline__ void take_in(const WinArgs& a, size_t row, float* ref, float* sum, float (&v)[N], Column column) {
+    constexpr int AHEAD = N > 8 ? 1 : 4;
+    const float* const ml = a.ml + row * a.slots * 2;
+    const float* const part = a.part + row * a.slots * (size_t)a.D;
+    float top = *ref;
+    for (int s0 = 0; s0 < a.NP; s0 += 8) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = ml[2 * min(s0 + k, a.NP - 1)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, x[k]);
+    }
+    const float f = __builtin_amdgcn_exp2f(*ref - top);
+    *sum *= f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= f;
+    for (int s0 = 0; s0 < a.NP; s0 += AHEAD) {
+        float2 m[AHEAD];
+        float x[AHEAD][N];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int s = min(s0 + k, a.NP - 1);
+            m[k] = *(const float2*)(ml + 2 * s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[k][i] = part[(size_t)s * a.D + column(i)];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (s0 + k < a.NP) {
+                const float g = __builtin_amdgcn_exp2f(m[k].x - top);
+                *sum = fmaf(m[k].y, g, *sum);
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = fmaf(x[k][i], g, v[i]);
+            }
+    }
+    *ref = top;
 }
 
 // a wave's rows without the workgroup's other waves: partial results, or whole ones
@@ -873,21 +898,12 @@ __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t e
             if (gq == 0) a.ml[slot * 2] = r.ref[rt], a.ml[slot * 2 + 1] = r.sum[rt];
         } else {
             if (FOLD && a.fold && r.hi[rt] >= 0) {
-                const float top = top_of(a, at, r.ref[rt]), f = __builtin_amdgcn_exp2f(r.ref[rt] - top);
-                r.sum[rt] *= f;
+                float v[4 * E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) r.o[rt][e] *= f;
-                for (int s = 0; s < a.NP; ++s) {
-                    const size_t slot = at * a.slots + s;
-                    const float* const p = a.part + slot * D;
-                    const float g = __builtin_amdgcn_exp2f(a.ml[slot * 2] - top);
-                    r.sum[rt] = fmaf(a.ml[slot * 2 + 1], g, r.sum[rt]);
+                for (int i = 0; i < 4 * E; ++i) v[i] = r.o[rt][i % E][i / E];
+                take_in<4 * E>(a, at, &r.ref[rt], &r.sum[rt], v, [gq](int i) { return column_of<Q8, E>(4 * gq + i / E, i % E); });
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) r.o[rt][e][k] = fmaf(p[column_of<Q8, E>(4 * gq + k, e)], g, r.o[rt][e][k]);
-                }
-                r.ref[rt] = top;
+                for (int i = 0; i < 4 * E; ++i) r.o[rt][i % E][i / E] = v[i];
             }
             const float inv = r.sum[rt] == 0.f ? 0.f : 1.0f / r.sum[rt];
             uint16_t* const o = a.out + (int64_t)tok * a.ot + h * a.oh;
@@ -903,72 +919,57 @@ __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t e
     }
 }
 
-template <int D, int NR>
+template <int D>
 struct MeetLds {
     float o[4][16][D + 4];
-    float ml[4][NR * 16][2];
+    float ml[4][16][2];
 };
 
 // the four waves' results of a workgroup's task, summed and stored
-template <bool BF, bool Q8, int D, int NR>
-__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix, int64_t end, Rows<BF, Q8, D, NR>& r, MeetLds<D, NR>& l) {
+template <bool BF, bool Q8, int D>
+__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix, int64_t end, Rows<BF, Q8, D, 1>& r, MeetLds<D>& l) {
     constexpr int E = D / 16;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, n = lane & 15, gq = lane >> 4;
     r.finish(end);
     __syncthreads();                          // an earlier task's LDS is read out
-#pragma unroll
-    for (int rt = 0; rt < NR; ++rt)
-        if (gq == 0) l.ml[w][rt * 16 + n][0] = r.ref[rt], l.ml[w][rt * 16 + n][1] = r.sum[rt];
+    if (gq == 0) l.ml[w][n][0] = r.ref[0], l.ml[w][n][1] = r.sum[0];
     __syncthreads();
+    float top = -INFINITY;
 #pragma unroll
-    for (int rt = 0; rt < NR; ++rt) {
-        if (rt * 16 >= t.rows) break;
-        float top = -INFINITY;
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, l.ml[i][n][0]);
+    const float f = __builtin_amdgcn_exp2f(r.ref[0] - top);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, l.ml[i][rt * 16 + n][0]);
-        const float f = __builtin_amdgcn_exp2f(r.ref[rt] - top);
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int e = 0; e < E; ++e) l.o[w][n][column_of<Q8, E>(4 * gq + i, e)] = r.o[0][e][i] * f;
+    __syncthreads();
+    for (int i = tid; i < t.rows * (D / 4); i += kT) {
+        const int row = i / (D / 4), d = i % (D / 4) * 4;
+        f32x4 v = *(const f32x4*)&l.o[0][row][d];
 #pragma unroll
-            for (int e = 0; e < E; ++e) l.o[w][n][column_of<Q8, E>(4 * gq + i, e)] = r.o[rt][e][i] * f;
-        __syncthreads();
-        for (int i = tid; i < 16 * (D / 4); i += kT) {
-            const int rr = i / (D / 4), d = i % (D / 4) * 4, row = rt * 16 + rr;
-            if (row >= t.rows) continue;
-            f32x4 v = *(const f32x4*)&l.o[0][rr][d];
+        for (int k = 1; k < 4; ++k) v += *(const f32x4*)&l.o[k][row][d];
+        float tp = -INFINITY, sm = 0.f;
 #pragma unroll
-            for (int k = 1; k < 4; ++k) v += *(const f32x4*)&l.o[k][rr][d];
-            float tp = -INFINITY, sm = 0.f;
+        for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sm += l.ml[k][row][1] * __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp);
-            const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
-            const size_t at = (size_t)tok * a.H + h;
-            if (t.splits > 1) {
-                const size_t slot = at * a.slots + t.split;
-                *(f32x4*)(a.part + slot * D + d) = v;
-                if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
-            } else {
-                if (a.fold && t.position(row, a.per) >= prefix) {       // (others see nothing)
-                    const float top = top_of(a, at, tp), f = __builtin_amdgcn_exp2f(tp - top);
-                    v *= f, sm *= f, tp = top;
-                    for (int s = 0; s < a.NP; ++s) {
-                        const size_t slot = at * a.slots + s;
-                        const float g = __builtin_amdgcn_exp2f(a.ml[slot * 2] - top);
-                        sm = fmaf(a.ml[slot * 2 + 1], g, sm);
-                        const f32x4 x = *(const f32x4*)(a.part + slot * D + d);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = fmaf(x[k], g, v[k]);
-                    }
-                }
-                const float inv = sm == 0.f ? 0.f : 1.0f / sm;
-                const u32x2 o = {pack2<BF>(v[0] * inv, v[1] * inv), pack2<BF>(v[2] * inv, v[3] * inv)};
-                *(u32x2*)(a.out + (int64_t)tok * a.ot + h * a.oh + d) = o;
-                if (a.lse && d == 0) a.lse[at] = sm == 0.f ? -INFINITY : tp * 0.69314718055994531f + logf(sm);
-            }
+        for (int k = 0; k < 4; ++k) sm += l.ml[k][row][1] * __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp);
+        const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
+        const size_t at = (size_t)tok * a.H + h;
+        if (t.splits > 1) {
+            const size_t slot = at * a.slots + t.split;
+            *(f32x4*)(a.part + slot * D + d) = v;
+            if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
+            continue;
         }
-        __syncthreads();
+        if (a.fold && t.position(row, a.per) >= prefix) {               // (others see nothing)
+            float x[4] = {v[0], v[1], v[2], v[3]};
+            take_in<4>(a, at, &tp, &sm, x, [d](int i) { return d + i; });
+            v = f32x4{x[0], x[1], x[2], x[3]};
+        }
+        const float inv = sm == 0.f ? 0.f : 1.0f / sm;
+        const u32x2 o = {pack2<BF>(v[0] * inv, v[1] * inv), pack2<BF>(v[2] * inv, v[3] * inv)};
+        *(u32x2*)(a.out + (int64_t)tok * a.ot + h * a.oh + d) = o;
+        if (a.lse && d == 0) a.lse[at] = sm == 0.f ? -INFINITY : tp * 0.69314718055994531f + logf(sm);
     }
 }
 
@@ -1001,9 +1002,10 @@ struct Asked {
     }
 };
 
-// A workgroup per task of up to 64 * NR rows, the four waves on different rows.
-template <bool BF, bool Q8, int D, int NR>
+// A workgroup per task of up to 128 rows, the four waves on different rows.
+template <bool BF, bool Q8, int D>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window_wide(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
+    constexpr int NR = kWideRows / 64;
     __shared__ StageLds<D> l[2];
     Asked asked(a, 1);
     Task t;
@@ -1015,16 +1017,16 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_
     }
 }
 
-// A workgroup per task of up to 16 * NR rows, the four waves on every fourth tile.
-template <bool BF, bool Q8, int D, int NR>
+// A workgroup per task of up to 16 rows, the four waves on every fourth tile.
+template <bool BF, bool Q8, int D>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
-    __shared__ MeetLds<D, NR> l;
+    __shared__ MeetLds<D> l;
     Asked asked(a, 1);
     Task t;
     while (asked.next(c, b, a, t)) {
-        Rows<BF, Q8, D, NR> r;
-        walk<BF, Q8, D, NR>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
-        meet<BF, Q8, D, NR>(a, t, b.prefix, asked.end(c, b), r, l);
+        Rows<BF, Q8, D, 1> r;
+        walk<BF, Q8, D>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
+        meet<BF, Q8, D>(a, t, b.prefix, asked.end(c, b), r, l);
     }
 }
 
@@ -1035,7 +1037,7 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_
     Task t;
     while (asked.next(c, b, a, t)) {
         Rows<BF, Q8, D, 1> r;
-        walk<BF, Q8, D, 1>(c, sc, b, a, t, t.b0, 2, r);
+        walk<BF, Q8, D>(c, sc, b, a, t, t.b0, 2, r);
         store<BF, Q8, D, 1, true>(a, t, asked.end(c, b), r, 0);
     }
 }
@@ -1077,16 +1079,16 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
         acc *= old;
         top = tp;
         const int m = min(64, n - i0);
-        for (int k0 = 0; k0 < m; k0 += 4 * groups) {
-            f32x4 x[4];
+        for (int k0 = 0; k0 < m; k0 += 8 * groups) {
+            f32x4 x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 8; ++j) {
                 const int k = k0 + j * groups + g;
                 x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (k < m && d < D) x[j] = *(const f32x4*)(part + (size_t)(i0 + k) * D + d);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 8; ++j) {
                 const float fk = __shfl(f, min(k0 + j * groups + g, 63));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[j][e], fk, acc[e]);
@@ -1104,11 +1106,10 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
 }
 
-enum { WIDE, SMALL, SMALL_2, WAVES };         // kernels
+enum { WIDE, SMALL, WAVES };                  // kernels
 
 struct Plan {
-    int nr;                                   // tiles of 16 rows a wave has
-    bool wide, wide_own;
+    bool wide_own;
     int RT, NO, CT, NP, CP, rb, rows, ptasks, groups;
     int own, before, slots;                   // kernels of the sequences' tasks and of the prefix's; partial results of a row
     bool fold;
@@ -1119,25 +1120,28 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     const int per = H / c.G;
     const int64_t rows = (int64_t)b.T * per, each = (rows + b.B - 1) / b.B;
     if (rows * c.G > kRowsMax) return LOOPSPEC_EINVAL;
-    p->wide_own = each > 32;
-    // rows of several sequences over the prefix at once, where none has enough of its own
+    // Blocks of 128 rows or of 16: 16 sequences' 16 tokens (64 rows a head each, 4000 positions) 48 us and 71, 52 and 47 over
+    // 8-bit pages; with 12 tokens 45 and 55, 51 and 39; one sequence's 16 tokens 21 and 16.
+    p->wide_own = each > 48;
+    // Rows of several sequences over the prefix at once, where none has enough of its own: 32 sequences behind 8000 positions
+    // 38 us, one by one 72.  Blocks of 128 of them or of 16: 256 rows over 4000 positions 20 us and 31, 128 rows 18 and 25,
+    // but the own positions' launch costs 10 more.
     const bool together = b.prefix > 0 && W == kAll && b.B > 1 && !p->wide_own;
-    p->wide = p->wide_own || (together && rows > 32);
-    p->nr = p->wide ? 2 : (together ? rows : each) > 16 ? 2 : 1;
-    p->RT = p->wide_own ? 64 * p->nr : p->wide ? 16 : 16 * p->nr;
+    const bool wide = p->wide_own || (together && rows > 128);
+    p->RT = p->wide_own ? kWideRows : kFewRows;
     const int slots = 512;                    // two workgroups a CU
     p->NP = p->CP = p->rb = p->rows = p->ptasks = 0;
     if (together) {
-        const int block = p->wide ? 64 * p->nr : 16 * p->nr;
+        const int block = wide ? kWideRows : kFewRows;
         p->rb = (int)((rows + block - 1) / block);
         p->rows = (int)((rows + p->rb * 16 - 1) / (p->rb * 16) * 16);
-        // the number of chunks whose rounds of resident workgroups take the least time, a workgroup's start and end
-        // counted as two steps of 128 positions
+        // The number of chunks that takes the least time, in steps of 128 positions: rounds of resident workgroups, whose start
+        // and end count as two, and the partial results (512 rows over 4000 positions: 8 chunks 27 + 26 us, 16 chunks 30 + 37).
         const int64_t steps = (b.prefix + 127) / 128, heads = (int64_t)c.G * p->rb;
         int64_t best = -1;
         for (int64_t np = 1; np <= std::min<int64_t>(steps, 128); ++np) {
             const int64_t len = (steps + np - 1) / np, n = (steps + len - 1) / len;
-            const int64_t cost = (heads * n + slots - 1) / slots * (len + 2);
+            const int64_t cost = (heads * n + slots - 1) / slots * (len + 2) * slots + 6 * heads * n;
             if (best < 0 || cost < best) best = cost, p->NP = (int)n, p->CP = (int)(len * 4);
         }
         const int64_t pairs = ((int64_t)c.G * p->NP + 7) / 8 * 8;
@@ -1148,25 +1152,27 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     int64_t most = (together ? 0 : (b.prefix + 15) / 16) + (int64_t)b.width * c.unit;
     if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
     const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
-    const int64_t blocks = std::min(rows, (rows + p->RT - 1) / p->RT + b.B) * c.G;
-    // About 1024 tasks where the tables are full, of at least two tiles a wave and 16 in all; prompts that fill the card are
-    // not cut.
-    if (p->wide_own && blocks >= slots)
+    const int64_t seqs = std::min(b.B, b.T), blocks = (seqs + std::max<int64_t>(rows - seqs * per, 0) / p->RT) * c.G;
+    // About 1024 tasks where the tables are full (over 18 batches of ragged lengths 384 to 1536 are within 3 %), of at least
+    // two tiles a wave.  What is short (300 positions 12 us, in chunks of 8 tiles 11 + 5) is not cut, nor are prompts and
+    // windows, whose tasks are alike, that fill the card (64 rows over 4096 of 12000 positions 168 us, cut in two 172 + 6).
+    if ((!p->wide_own && tiles <= 16) || ((p->wide_own || W < kAll) && blocks >= slots))
         p->CT = (int)tiles;
     else
-        p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(16, (tiles * blocks / 1024 + 1) / 2 * 2));
+        p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(p->wide_own ? 16 : 8, (tiles * blocks / 1024 + 1) / 2 * 2));
     p->NO = (int)((tiles + p->CT - 1) / p->CT);
     const int64_t tasks = blocks * p->NO;
-    // A wave per task where there are enough short ones: 1024 tasks of 5 tiles (128 sequences of 1 to 259 positions, 8 heads)
-    // 22 us, by workgroups 32; 512 of 5 16.0 and 16.8.
-    const bool by_wave = !p->wide_own && p->RT == 16 && p->CT <= 16 && tasks >= slots;
-    p->own = p->wide_own ? WIDE : by_wave ? WAVES : p->wide || p->nr == 1 ? SMALL : SMALL_2;
-    p->before = p->wide ? WIDE : p->nr == 1 ? SMALL : SMALL_2;
-    // Workgroups that go on from task to task fill the card once (64 rows over 4096 of 12000 positions 170 us, with twice as
-    // many 174); tasks of many rows are too unequal for that.
+    // A wave per task where there are enough short ones (8 heads, up to 250 positions): 128 sequences 22 us, by workgroups 26;
+    // 64 of them 19 and 17; 512 of up to 60 positions 29 and 71.
+    const bool by_wave = !p->wide_own && p->NO == 1 && p->CT <= 16 && tasks >= 2 * slots;
+    p->own = p->wide_own ? WIDE : by_wave ? WAVES : SMALL;
+    p->before = wide ? WIDE : SMALL;
+    // Workgroups that go on from task to task fill the card once (the same rows cut in two 172 us, with a workgroup each 174);
+    // tasks of many rows are too unequal for that.
     p->groups = (int)std::min<int64_t>(by_wave ? (tasks + 3) / 4 : tasks, p->wide_own ? 16384 : slots);
-    // Where the prefix has a launch of its own and a row's own positions are one task, that one finishes the row.
-    p->fold = together && p->own != p->before && p->NO == 1;
+    // Where the prefix has a launch of its own and a row's own positions are one task, that one finishes the row: waves behind
+    // 5 chunks 28 us, with a join 21 + 14, behind 16 chunks 37 and 16 + 11; workgroups behind 32 chunks 20 and 13 + 10.
+    p->fold = together && p->own != p->before && p->NO == 1 && p->NP <= (by_wave ? 8 : 32);
     p->slots = p->fold ? p->NP : p->NP + p->NO > 1 ? p->NP + p->NO : 0;
     return LOOPSPEC_OK;
 }
@@ -1191,9 +1197,8 @@ int check(const loopspec_paged_cache* cache, const loopspec_page_scales* scales,
 template <bool BF, bool Q8, int D>
 const void* kernel_of(int k) {
     switch (k) {
-        case WIDE: return (const void*)k_window_wide<BF, Q8, D, 2>;
-        case SMALL: return (const void*)k_window<BF, Q8, D, 1>;
-        case SMALL_2: return (const void*)k_window<BF, Q8, D, 2>;
+        case WIDE: return (const void*)k_window_wide<BF, Q8, D>;
+        case SMALL: return (const void*)k_window<BF, Q8, D>;
         default: return (const void*)k_window_waves<BF, Q8, D>;
     }
 }
@@ -1245,7 +1250,7 @@ int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_
     if (need && (!workspace_dev || ((uintptr_t)workspace_dev & 15) || workspace_bytes < need)) return LOOPSPEC_EINVAL;
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     WinArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
-              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.slots * c.D, cs, args->n_heads,
+              args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.slots * c.D, cs, c.D, args->n_heads,
               args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT,
               p.NP, p.CP, p.rb, p.rows, 0, p.slots, p.fold};
     hipStream_t st = (hipStream_t)stream;

@@ -106,7 +106,35 @@ def windowed(c, window, sinks, scale):
                    v.abs().amax((0, 2))[:, None])
 
 
-def check_window(c, window, sinks, scale, out, lse, before):
+def behind_a_prefix(c, scale):
+    """The same without a window for batches of one token per sequence, whose sums over the prefix take too long one by one:
+    all of them at once."""
+    per, B, most = c.H // c.G, len(c.new), max(c.lens)
+    q = c.q[c.first:c.first + B].double().reshape(B, c.G, per, c.D)
+    own = [torch.zeros((B, most, c.G, c.D), dtype=torch.float64) for _ in "kv"]
+    for b, n in enumerate(c.lens):
+        for x, pages in zip(own, (c.k, c.v)):
+            x[b, :n] = c.get(pages, c.tables[b], n)
+    (kp, vp), (ko, vo) = (c.get(x, c.ptable, c.prefix) for x in (c.k, c.v)), own
+    behind = torch.arange(most)[None] >= torch.tensor(c.lens)[:, None]
+    rows = [[] for _ in range(5)]
+    for g in range(c.G):
+        # [positions, D] of the prefix and [B, positions, D] of each sequence
+        both = lambda a, p, o: torch.cat([(a.reshape(-1, c.D) @ p[:, g].T).reshape(B, per, -1), a @ o[:, :, g].transpose(1, 2)], 2)  # noqa: E731
+        mix = lambda w, p, o: (w[:, :, :c.prefix].reshape(B * per, -1) @ p[:, g]).reshape(B, per, c.D) + w[:, :, c.prefix:] @ o[:, :, g]  # noqa: E731
+        s = both(q[:, g], kp, ko) * scale
+        s[:, :, c.prefix:].masked_fill_(behind[:, None], -math.inf)
+        big = both(q[:, g].abs(), kp.abs(), ko.abs()).amax(2) * scale
+        w = torch.softmax(s, 2)
+        top = torch.maximum(vp[:, g].abs().max(), vo[:, :, g].abs().amax((1, 2)))[:, None].expand(B, per)
+        for to, x in zip(rows, (mix(w, vp, vo), torch.logsumexp(s, 2), mix(w, vp.abs(), vo.abs()), big, top)):
+            to.append(x)
+    ref, lse, mean, big, top = (torch.stack(x, 1).flatten(1, 2) for x in rows)
+    for b in range(B):
+        yield c.first + b, ref[b], lse[b], mean[b], big[b], top[b][:, None]
+
+
+def check_window(c, window, sinks, scale, out, lse, before, rows=None):
     """A weight is rounded to 16 bits (half a step), the output once more; the score's fp32 sum of D products is off by at
     most (D + 8) 2^-24 of the sum of their magnitudes, which moves a weight by as much; sums over n positions add n 2^-24;
     weights (times their values' scale) below 2^-31 of the largest vanish.  fp16's subnormals are spaced 2^-24."""
@@ -114,7 +142,7 @@ def check_window(c, window, sinks, scale, out, lse, before):
     got, glse = out.cpu().double(), lse.cpu().double()
     seen = torch.zeros(len(c.q), dtype=torch.bool)
     worst = 0.0
-    for t, ref, rlse, mean, big, most in windowed(c, window, sinks, scale):
+    for t, ref, rlse, mean, big, most in rows or windowed(c, window, sinks, scale):
         seen[t] = True
         n = c.prefix + max(c.lens) + 16
         ds = ((c.D + 8) * 2.0 ** -24 * big + n * 2.0 ** -24)[:, None]

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from gpu_common import log
-from quantized_common import Quantized, check_window
+from quantized_common import Quantized, behind_a_prefix, check_window, windowed
 from serving_common import Case
 from test_gpu_window import attend, check
 
@@ -32,6 +32,26 @@ def test_many_sequences(spec, eight):
     c = (Quantized if eight else Case)(H, G, D, page, dt, new, lens, prefix, seed=4)
     worst = max(check(c, *w) for w in [(0, 0), (20, 3), (100, 0)])
     log(f"[window] {spec[:5]} x {len(new)}, {'8' if eight else '16'} bits: worst {worst:.2f} of tolerance")
+
+
+# heads, key/value heads, sequences, prefix: prefixes of few rows and of many, few chunks and many, own positions by
+# workgroups and by waves, with and without a join of their own
+BEHIND = [(8, 2, 3, 3001), (8, 2, 20, 9000), (16, 4, 40, 700), (2, 1, 500, 30000), (8, 2, 513, 9000), (8, 2, 513, 200), (64, 64, 20, 2500), (32, 8, 140, 5000)]
+
+
+@pytest.mark.parametrize("shape", BEHIND, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("D,eight", [(16, False), (32, True)])
+def test_behind_long_prefixes(shape, D, eight):
+    H, G, B, P = shape
+    c = (Quantized if eight else Case)(H, G, D, 32, "bf16" if D == 16 else "f16", [1] * B, [i * 7 % 90 + 1 for i in range(B)], P, seed=11)
+    scale = D ** -0.5
+    if B < 4:
+        for a, b in zip(behind_a_prefix(c, scale), windowed(c, 0, 0, scale)):
+            for x, y in zip(a[1:], b[1:]):
+                torch.testing.assert_close(x, y, rtol=1e-12, atol=1e-12)
+    out, lse = attend(c, 0, 0)
+    worst = check_window(c, 0, 0, scale, out, lse, torch.full(c.q.shape, 3.0, dtype=c.dtype), behind_a_prefix(c, scale))
+    log(f"[window] {shape} head_dim {D}, {'8' if eight else '16'} bits: worst {worst:.2f} of tolerance")
 
 
 @pytest.mark.parametrize("eight", [False, True])
