@@ -35,6 +35,7 @@ namespace {
 
 constexpr int kT = 256;
 constexpr int kWideRows = 128, kFewRows = 16;  // rows of a block where the waves share positions, and where each has its own
+constexpr int kUncut = 24;                    // tiles of 32 positions that blocks of few rows take in one piece
 constexpr int kRowsMax = 1 << 25;              // tokens x heads: the join's grid holds 2^32 threads
 constexpr int kGroupsMax = 1 << 23;            // workgroups of the prefix, for the same reason
 constexpr int kAll = 1 << 30;                 // a window that holds every position
@@ -293,9 +294,10 @@ __device__ __forceinline__ bool hidden(const Blk& x, int lo, int hi, const WinAr
 // only the device knows; whoever asks for rising numbers walks the sequences once.
 struct Tasks {
     int base = 0;                             // the sequences before it hold `done` tasks
-    int64_t done = 0;
+    int64_t done = 0, last = INT64_MAX;       // the last 64 sequences' tasks end there
 
     __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, int64_t task, Task& t) {
+        if (task >= last) return false;       // (without asking for the lengths again)
         const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
         const int lane = threadIdx.x & 63, PB = (b.prefix + 15) >> 4;
         for (; base < b.B; base += 64) {
@@ -314,19 +316,20 @@ struct Tasks {
                 if (lane >= o) upto += v;
             }
             const unsigned long long over = __ballot(done + upto > task);
+            const int64_t end = done + (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32) |
+                                                 (unsigned)__builtin_amdgcn_readlane((int)upto, 63));
+            if (b.B - base <= 64) last = end;
             if (!over) {
-                done += (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32) |
-                                  (unsigned)__builtin_amdgcn_readlane((int)upto, 63));
+                done = end;
                 continue;
             }
             const int hit = __ffsll(over) - 1, sq = base + hit;
-            const int64_t at64 = task - (done + upto - mine);
-            const unsigned rest_lo = (unsigned)__builtin_amdgcn_readlane((int)at64, hit), rest_hi = (unsigned)__builtin_amdgcn_readlane((int)(at64 >> 32), hit);
-            const uint64_t rest = (uint64_t)rest_hi << 32 | rest_lo;
+            // (one sequence's tasks are below 2^31: its blocks of rows are, and chunks go down as these go up)
+            const unsigned rest = (unsigned)__builtin_amdgcn_readlane((int)(task - (done + upto - mine)), hit);
             const int n = __builtin_amdgcn_readlane(q.n, hit), first = __builtin_amdgcn_readlane(q.first, hit);
             const int ncs = __builtin_amdgcn_readlane(nc, hit), blocks = __builtin_amdgcn_readlane(nb, hit);
             t.g = (int)(rest % (unsigned)c.G);
-            const uint64_t rc = rest / (unsigned)c.G;
+            const unsigned rc = rest / (unsigned)c.G;
             const int ch = (int)(rc % (unsigned)ncs), rb = blocks - 1 - (int)(rc / (unsigned)ncs);
             t.table = b.table + sq * b.table_stride;
             t.tok0 = __builtin_amdgcn_readlane(q.start, hit);
@@ -560,6 +563,8 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
     const int gq = (threadIdx.x & 63) >> 4;
     r.start(t, b.prefix, a.per, 0);
     if (at >= t.b1) return;
+    u32x4 q[1][NS];                           // (on their way while the pages are looked up)
+    load_q<BF, Q8, D, 1>(a, t, 0, q);
     Keys<BF, Q8, D> xk[2];
     Vals<BF, Q8, E> xv[2][4];
     // lane 2 j + h: block h of the wave's tile j of 32
@@ -575,8 +580,6 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, x));
         info[h] = x.info;
     }
-    u32x4 q[1][NS];
-    load_q<BF, Q8, D, 1>(a, t, 0, q);
     const bool several = t.position(0, a.per) != t.hi;
     const Inner in = inner(b, a, t, t.lo, t.hi);
     for (int known = 31;; known += 32) {      // the last tile whose place the lanes hold
@@ -1125,11 +1128,14 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     p->wide_own = each > 48;
     // Rows of several sequences over the prefix at once, where none has enough of its own: 32 sequences behind 8000 positions
     // 38 us, one by one 72.  Blocks of 128 of them or of 16: 256 rows over 4000 positions 20 us and 31, 128 rows 18 and 25,
-    // but the own positions' launch costs 10 more.
-    const bool together = b.prefix > 0 && W == kAll && b.B > 1 && !p->wide_own;
+    // but the own positions' launch then costs 10 more.  Short prefixes and own positions stay one task a sequence (8 sequences
+    // behind 400 positions 13 us, the prefix apart 10 + 5; 64 of them 19 and 12 + 13).
+    const int64_t seqs = std::min(b.B, b.T), held = (int64_t)b.width * c.unit;    // blocks of 16 that a table holds
+    const int slots = 512;                    // two workgroups a CU
+    const bool brief = ((b.prefix + 15) / 16 + held + 1) / 2 <= kUncut && (seqs + std::max<int64_t>(rows - seqs * per, 0) / kFewRows) * c.G <= slots;
+    const bool together = b.prefix > 0 && W == kAll && b.B > 1 && !p->wide_own && !brief;
     const bool wide = p->wide_own || (together && rows > 128);
     p->RT = p->wide_own ? kWideRows : kFewRows;
-    const int slots = 512;                    // two workgroups a CU
     p->NP = p->CP = p->rb = p->rows = p->ptasks = 0;
     if (together) {
         const int block = wide ? kWideRows : kFewRows;
@@ -1149,14 +1155,14 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
         p->ptasks = (int)(pairs * p->rb);
     }
     // blocks of 16 positions that a block of rows may see
-    int64_t most = (together ? 0 : (b.prefix + 15) / 16) + (int64_t)b.width * c.unit;
+    int64_t most = (together ? 0 : (b.prefix + 15) / 16) + held;
     if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
     const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
-    const int64_t seqs = std::min(b.B, b.T), blocks = (seqs + std::max<int64_t>(rows - seqs * per, 0) / p->RT) * c.G;
+    const int64_t blocks = (seqs + std::max<int64_t>(rows - seqs * per, 0) / p->RT) * c.G;
     // About 1024 tasks where the tables are full (over 18 batches of ragged lengths 384 to 1536 are within 3 %), of at least
-    // two tiles a wave.  What is short (300 positions 12 us, in chunks of 8 tiles 11 + 5) is not cut, nor are prompts and
+    // two tiles a wave.  What is short (700 positions 15 us, in chunks of 8 tiles 11 + 5) is not cut, nor are prompts and
     // windows, whose tasks are alike, that fill the card (64 rows over 4096 of 12000 positions 168 us, cut in two 172 + 6).
-    if ((!p->wide_own && tiles <= 16) || ((p->wide_own || W < kAll) && blocks >= slots))
+    if ((!p->wide_own && tiles <= kUncut) || ((p->wide_own || W < kAll) && blocks >= slots))
         p->CT = (int)tiles;
     else
         p->CT = (int)std::min<int64_t>(tiles, std::max<int64_t>(p->wide_own ? 16 : 8, (tiles * blocks / 1024 + 1) / 2 * 2));

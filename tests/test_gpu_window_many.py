@@ -69,11 +69,11 @@ def test_rows_that_see_nothing_behind_a_prefix(heads, kv, eight):
 
 
 @pytest.mark.parametrize("eight", [False, True])
-@pytest.mark.parametrize("many", [10, 90])
-def test_values_that_are_not_finite_in_a_prefix_and_behind(many, eight):
+@pytest.mark.parametrize("many,prefix", [(10, 200), (10, 900), (90, 200), (90, 900)])
+def test_values_that_are_not_finite_in_a_prefix_and_behind(many, prefix, eight):
     """NaN in the prefix reaches every row; NaN in one sequence's own positions reaches that sequence alone."""
     from paper_2609_17184_amd import serving
-    c = (Quantized if eight else Case)(16, 8, 64, 16, "bf16", [1] * many, [20 + i for i in range(many)], 200, seed=6)
+    c = (Quantized if eight else Case)(16, 8, 64, 16, "bf16", [1] * many, [20 + i for i in range(many)], prefix, seed=6)
     q = c.q.to(DEV)
     ref = serving.window_attention(q, c.cache, c.batch)
     vd = c.vd.view(torch.uint8) if eight else c.vd
