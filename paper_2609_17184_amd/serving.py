@@ -54,9 +54,9 @@ def _whole(n, what: str) -> int:
 
 def _ints(t, shape, device, what: str):
     import torch
-    _need(t.dtype == torch.int32 and t.device == device and t.dim() == len(shape) and t.stride(-1) == 1
-          and all(n is None or n == m for n, m in zip(shape, t.shape)),
-          f"{what}: int32, unit stride, shape {list(shape)} on {device}")
+    if not (t.dtype is torch.int32 and t.device == device and t.dim() == len(shape) and t.stride(-1) == 1
+            and shape[0] in (None, t.shape[0]) and shape[-1] in (None, t.shape[-1])):
+        raise ValueError(f"{what}: int32, unit stride, shape {list(shape)} on {device}")
     return t.data_ptr()
 
 
@@ -64,7 +64,7 @@ def _launch(device, call, *args) -> int:
     """One call of the library on the device's current stream."""
     import torch
     stream = torch._C._cuda_getCurrentRawStream(device.index)   # torch.cuda.current_stream without its object, 2 us
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device.index:
         return call(*args, stream)
     with torch.cuda.device(device):
         return call(*args, stream)
@@ -90,6 +90,7 @@ class PagedCache:
         self._c = B.PagedCacheC(_dtype(k), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, k.data_ptr(),
                                 v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
         self._ref = ctypes.byref(self._c)
+        self._raw = bytes(self._c), bytes(ctypes.sizeof(B.PageScalesC))         # (for lists of caches; no scales)
 
     _scales_ref = None
 
@@ -122,6 +123,7 @@ class QuantizedCache:
         self._by_type = {t: B.PagedCacheC(d, *k.shape[:1], self.page_size, self.n_kv_heads, self.head_dim, k.data_ptr(),
                                           v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
                          for t, d in ((torch.float16, B.F16), (torch.bfloat16, B.BF16))}
+        self._raw = bytes(self._by_type[torch.float16]), bytes(self._scales)
 
     def _for(self, dtype):
         if dtype not in self._by_type:
@@ -263,7 +265,7 @@ def window_attention(q, cache, batch: Batch, window: int = 0, sinks: int = 0, sc
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
     _prefix_held(cache, batch)
     # (a window or sinks beyond all positions are those of all positions)
-    window, sinks = (min(_whole(n, what), 1 << 30) for n, what in ((window, "window"), (sinks, "sinks")))
+    window, sinks = min(_whole(window, "window"), 1 << 30), min(_whole(sinks, "sinks"), 1 << 30)
     L, ref, c = B.load_library(), batch._with(tokens, cache), cache._for(q.dtype)
     nbytes = L.loopspec_window_attention_workspace_bytes(c, cache._scales_ref, ref, heads, window, sinks)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
@@ -284,32 +286,26 @@ def fork_pages(seq_len, table, parent, refs, caches, prefix_len: int = 0, window
     `room` more positions.  table's entries without a page lie outside the cache (-1), also those behind a row's last
     page.  Returns (seq_len, table, refs, short), new int32 tensors: short [1] counts the pages that were not to be had,
     whose entries are -1."""
-    import torch
     caches = list(caches)
     _need(bool(caches), "caches: one or more")
     dev, n_pages, page_size = caches[0].device, caches[0].n_pages, caches[0].page_size
-    cs, sc = (B.PagedCacheC * len(caches))(), (B.PageScalesC * len(caches))()
-    for i, c in enumerate(caches):
+    for c in caches:
         if c.n_pages != n_pages or c.page_size != page_size or c.device != dev:
             raise ValueError("caches: on one device, of equal n_pages and page_size")
-        cs[i] = c._for(torch.float16)._obj
-        if c._scales_ref is not None:
-            sc[i] = c._scales
+    cs, sc = (kind.from_buffer_copy(b"".join([c._raw[i] for c in caches]))
+              for i, kind in enumerate((B.PagedCacheC * len(caches), B.PageScalesC * len(caches))))
     n, m = _size(seq_len.shape[0], "seq_len"), _size(parent.shape[0], "parent")
     lens, rows = _ints(seq_len, (n,), dev, "seq_len"), _ints(table, (n, None), dev, "table")
     width = _size(table.shape[1], "table")
     of, counts = _ints(parent, (m,), dev, "parent"), _ints(refs, (n_pages,), dev, "refs")
-    prefix_len, window, sinks, room = (min(_whole(x, what), 1 << 30) for x, what in (
-        (prefix_len, "prefix_len"), (window, "window"), (sinks, "sinks"), (room, "room")))
-    new_len = torch.empty((m,), dtype=torch.int32, device=dev)
-    new_table = torch.empty((m, width), dtype=torch.int32, device=dev)
-    new_refs = torch.empty((n_pages,), dtype=torch.int32, device=dev)
-    short = torch.empty((1,), dtype=torch.int32, device=dev)
+    prefix_len, window = min(_whole(prefix_len, "prefix_len"), 1 << 30), min(_whole(window, "window"), 1 << 30)
+    sinks, room = min(_whole(sinks, "sinks"), 1 << 30), min(_whole(room, "room"), 1 << 30)
+    new_len, new_table, new_refs, short = (refs.new_empty(shape) for shape in ((m,), (m, width), (n_pages,), (1,)))
     a = B.ForkArgs(n, m, page_size, n_pages, lens, rows, table.stride(0), width, of, counts, prefix_len, window, sinks, room,
                    new_len.data_ptr(), new_table.data_ptr(), width, new_refs.data_ptr(), short.data_ptr())
     L = B.load_library()
     nbytes = L.loopspec_fork_pages_workspace_bytes(m, n_pages)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ws = refs.new_empty((nbytes // 4,))         # (whole words)
     _check(_launch(dev, L.loopspec_fork_pages, ctypes.byref(a), cs, sc, len(caches), ws.data_ptr(), nbytes),
            "loopspec_fork_pages")
     return new_len, new_table, new_refs, short
