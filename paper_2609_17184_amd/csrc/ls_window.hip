@@ -85,6 +85,13 @@ __device__ __forceinline__ constexpr int column_of(int m, int e) {
     return Q8 && E == 6 ? (e < 4 ? 4 * m + e : 64 + 2 * m + e - 4) : E * m + e;
 }
 
+// Offsets of a lane in 16 positions, in bytes.  `same` says nothing about them to the compiler, which would otherwise make
+// 64-bit addresses of them outside the loops and add these to every block's base, 2 registers and an instruction a load.
+struct Offsets {
+    uint32_t a, b;
+    __device__ __forceinline__ void same() { asm("" : "+v"(a), "+v"(b)); }
+};
+
 // A lane's part of the keys of 16 positions.
 template <bool BF, bool Q8, int D>
 struct Keys;
@@ -92,11 +99,12 @@ template <bool BF, int D>
 struct Keys<BF, false, D> {
     static constexpr int NS = (D + 31) / 32;
     u32x4 w[NS];
-    __device__ __forceinline__ void load(const char* b, uint32_t row, int gq) {
+    static __device__ __forceinline__ Offsets offsets(uint32_t row, int gq) { return Offsets{2 * row + 16 * gq, 0}; }
+    __device__ __forceinline__ void load(const char* b, const Offsets& o, int gq) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             w[s] = u32x4{0, 0, 0, 0};
-            if (D % 32 == 0 || gq < 2) w[s] = *(const u32x4*)(b + 64 * s + (2 * row + 16 * gq));
+            if (D % 32 == 0 || gq < 2) w[s] = *(const u32x4*)(b + o.a + 64 * s);
         }
     }
     __device__ __forceinline__ u32x4 get(int s) const { return w[s]; }
@@ -108,15 +116,16 @@ template <bool BF, int D>
 struct Keys<BF, true, D> {
     static constexpr int NS = (D + 31) / 32;
     uint32_t w[2 * NS];
-    __device__ __forceinline__ void load(const char* b, uint32_t row, int gq) {
+    static __device__ __forceinline__ Offsets offsets(uint32_t row, int gq) { return Offsets{row + 16 * gq, row + 8 * gq}; }
+    __device__ __forceinline__ void load(const char* b, const Offsets& o, int gq) {
 #pragma unroll
         for (int m = 0; m < D / 64; ++m) {
-            const u32x4 u = *(const u32x4*)(b + 64 * m + (row + 16 * gq));
+            const u32x4 u = *(const u32x4*)(b + o.a + 64 * m);
             w[4 * m] = u[0], w[4 * m + 1] = u[1], w[4 * m + 2] = u[2], w[4 * m + 3] = u[3];
         }
         if constexpr (D % 64 != 0) {
             u32x2 u = {0, 0};
-            if (D % 32 == 0 || gq < 2) u = *(const u32x2*)(b + D / 64 * 64 + (row + 8 * gq));
+            if (D % 32 == 0 || gq < 2) u = *(const u32x2*)(b + o.b + D / 64 * 64);
             w[2 * NS - 2] = u[0], w[2 * NS - 1] = u[1];
         }
     }
@@ -132,21 +141,22 @@ struct Vals;
 template <bool BF, int E>
 struct Vals<BF, false, E> {
     uint32_t w[(E + 1) / 2];
-    __device__ __forceinline__ void load(const char* p, uint32_t row, int n) {
-        const uint32_t off = 2 * row + 2 * E * n;
+    static __device__ __forceinline__ Offsets offsets(uint32_t row, int n) { return Offsets{2 * row + 2 * E * n, 0}; }
+    __device__ __forceinline__ void load(const char* p, const Offsets& f) {
+        p += f.a;
         if constexpr (E == 8) {
-            const u32x4 u = *(const u32x4*)(p + off);
+            const u32x4 u = *(const u32x4*)p;
             w[0] = u[0], w[1] = u[1], w[2] = u[2], w[3] = u[3];
         } else if constexpr (E == 6) {
-            const uint32_t* q = (const uint32_t*)(p + off);         // 12 bytes, 4-byte aligned
+            const uint32_t* q = (const uint32_t*)p;                 // 12 bytes, 4-byte aligned
             w[0] = q[0], w[1] = q[1], w[2] = q[2];
         } else if constexpr (E == 4) {
-            const u32x2 u = *(const u32x2*)(p + off);
+            const u32x2 u = *(const u32x2*)p;
             w[0] = u[0], w[1] = u[1];
         } else if constexpr (E == 2) {
-            w[0] = *(const uint32_t*)(p + off);
+            w[0] = *(const uint32_t*)p;
         } else {
-            w[0] = *(const uint16_t*)(p + off);
+            w[0] = *(const uint16_t*)p;
         }
     }
     __device__ __forceinline__ void wide(uint32_t (&o)[(E + 1) / 2], float) const {
@@ -157,20 +167,20 @@ struct Vals<BF, false, E> {
 template <bool BF, int E>
 struct Vals<BF, true, E> {
     uint32_t w[(E + 3) / 4];
-    __device__ __forceinline__ void load(const char* p, uint32_t row, int n) {
-        p += row;
+    static __device__ __forceinline__ Offsets offsets(uint32_t row, int n) { return Offsets{row + (E == 6 ? 4 : E) * n, row + 2 * n}; }
+    __device__ __forceinline__ void load(const char* p, const Offsets& f) {
         if constexpr (E == 8) {
-            const u32x2 u = *(const u32x2*)(p + 8 * n);
+            const u32x2 u = *(const u32x2*)(p + f.a);
             w[0] = u[0], w[1] = u[1];
         } else if constexpr (E == 6) {
-            w[0] = *(const uint32_t*)(p + 4 * n);
-            w[1] = *(const uint16_t*)(p + 64 + 2 * n);
+            w[0] = *(const uint32_t*)(p + f.a);
+            w[1] = *(const uint16_t*)(p + f.b + 64);
         } else if constexpr (E == 4) {
-            w[0] = *(const uint32_t*)(p + 4 * n);
+            w[0] = *(const uint32_t*)(p + f.a);
         } else if constexpr (E == 2) {
-            w[0] = *(const uint16_t*)(p + 2 * n);
+            w[0] = *(const uint16_t*)(p + f.a);
         } else {
-            w[0] = *(const uint8_t*)(p + n);
+            w[0] = *(const uint8_t*)(p + f.a);
         }
     }
     __device__ __forceinline__ void wide(uint32_t (&o)[(E + 1) / 2], float scale) const {
@@ -248,14 +258,15 @@ __device__ __forceinline__ Inner inner(const PagedBatch& b, const WinArgs& a, co
     const int vb = block_of(x, P, PB), j0 = vb < PB ? 16 * vb : P + 16 * (vb - PB);
     return Inner{max(t.s.head, vb + (j0 < x) + shift), min(t.b1, block_of(lo + 1, P, PB) + shift), P & 15 ? PB - 1 + shift : -1};
 }
-// Where 64 blocks of the list are, one in each lane: page, and in one word the scale bytes (keys', values' << 8), kBad (the
-// page is none of the cache's, or a scale is NaN) and the block of the page.
-constexpr int kBad = 1 << 16, kUnit = 20;
+// Where 64 blocks of the list are, one in each lane: offsets of the head's keys and values in bytes, and in one word the
+// scale bytes (keys', values' << 8), kBad (the page is none of the cache's, or a scale is NaN) and kPart (not in `whole`).
+constexpr int kBad = 1 << 16, kPart = 1 << 17;
 struct Where {
-    int id, info;
+    int64_t k, v;
+    int info;
 };
 template <bool Q8>
-__device__ __forceinline__ Where where(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const Task& t, int i) {
+__device__ __forceinline__ Where where(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const Task& t, const Inner& whole, int i) {
     const int PB = (b.prefix + 15) >> 4, vb = i < t.s.head ? i : i - t.s.head + t.s.from;
     const bool pre = vb < PB, in = i < t.b1;
     const unsigned o = pre ? vb : vb - PB, at = unit_div(o, c.magic);
@@ -264,26 +275,20 @@ __device__ __forceinline__ Where where(const PagedCache& c, const PageScales& sc
     const int raw = *(held ? (pre ? b.prefix_table : t.table) + at : b.seq_len);
     const bool ok = held && (unsigned)raw < (unsigned)c.n_pages;
     const int id = ok ? raw : 0;              // (behind the list's end any page will do)
-    int info = unit << kUnit | (in && !ok ? kBad : 0);
+    int info = (in && !ok ? kBad : 0) | (whole.holds(i, 1) ? 0 : kPart);
     if (Q8) {
         const int kb = sc.k[id * sc.kp + t.g * sc.kh + unit], vb8 = sc.v[id * sc.vp + t.g * sc.vh + unit];
         info |= kb | vb8 << 8 | (in && (kb == 255 || vb8 == 255) ? kBad : 0);
     }
-    return Where{id, info};
+    constexpr int size = Q8 ? 1 : 2;
+    return Where{(id * c.kp + t.g * c.kh + (int64_t)(unit * kPageUnit) * c.ks) * size,
+                 (id * c.vp + t.g * c.vh + (int64_t)(unit * kPageUnit) * c.vs) * size, info};
+}
+__device__ __forceinline__ int64_t lane_of(int64_t x, int j) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, j));
 }
 __device__ __forceinline__ Where lane_of(const Where& x, int j) {
-    return Where{__builtin_amdgcn_readlane(x.id, j), __builtin_amdgcn_readlane(x.info, j)};
-}
-// the block's keys and values of the task's head
-template <bool Q8>
-__device__ __forceinline__ const char* keys_at(const PagedCache& c, const Task& t, const Where& x) {
-    const int64_t at = x.id * c.kp + t.g * c.kh + (int64_t)((x.info >> kUnit) * kPageUnit) * c.ks;
-    return (const char*)c.k + (Q8 ? at : 2 * at);
-}
-template <bool Q8>
-__device__ __forceinline__ const char* values_at(const PagedCache& c, const Task& t, const Where& x) {
-    const int64_t at = x.id * c.vp + t.g * c.vh + (int64_t)((x.info >> kUnit) * kPageUnit) * c.vs;
-    return (const char*)c.v + (Q8 ? at : 2 * at);
+    return Where{lane_of(x.k, j), lane_of(x.v, j), __builtin_amdgcn_readlane(x.info, j)};
 }
 // none of the rows from position lo to hi sees any of it
 __device__ __forceinline__ bool hidden(const Blk& x, int lo, int hi, const WinArgs& a) {
@@ -483,10 +488,10 @@ struct Rows {
         const int gq = (threadIdx.x & 63) >> 4;
         for (int i = 0; i < 32; ++i) {
             const Blk y = look(b, t, at + (i >> 4));
-            const Where w = where<Q8>(c, sc, b, t, at + (i >> 4));
+            const Where w = where<Q8>(c, sc, b, t, Inner{}, at + (i >> 4));
             if ((i & 15) >= y.nv || (w.info & kBad)) continue;
             const int j = y.j0 + (i & 15);
-            const char* const from = values_at<Q8>(c, t, w) + (int64_t)(i & 15) * c.vs * (Q8 ? 1 : 2);
+            const char* const from = (const char*)c.v + w.v + (int64_t)(i & 15) * c.vs * (Q8 ? 1 : 2);
             const float scale = Q8 && BF ? ldexpf(1.f, value_exp(w.info >> 8 & 255)) : 1.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -522,16 +527,23 @@ struct Rows {
 
 // The keys and the values of 16 positions in a wave's registers.
 template <bool BF, bool Q8, int D>
-__device__ __forceinline__ void load_k(Keys<BF, Q8, D>& k, const PagedCache& c, const char* at) {
-    const int lane = threadIdx.x & 63;
-    k.load(at, (lane & 15) * (uint32_t)c.ks, lane >> 4);
-}
-template <bool BF, bool Q8, int D>
-__device__ __forceinline__ void load_v(Vals<BF, Q8, D / 16> (&v)[4], const PagedCache& c, const char* at) {
-    const int lane = threadIdx.x & 63;
+struct Loader {
+    Offsets k, v;
+    __device__ __forceinline__ explicit Loader(const PagedCache& c) {
+        const int lane = threadIdx.x & 63;
+        k = Keys<BF, Q8, D>::offsets((lane & 15) * (uint32_t)c.ks, lane >> 4);
+        v = Vals<BF, Q8, D / 16>::offsets(4 * (lane >> 4) * (uint32_t)c.vs, lane & 15);
+    }
+    __device__ __forceinline__ void keys(Keys<BF, Q8, D>& to, const PagedCache& c, const Where& x) {
+        k.same();
+        to.load((const char*)c.k + x.k, k, (threadIdx.x & 63) >> 4);
+    }
+    __device__ __forceinline__ void values(Vals<BF, Q8, D / 16> (&to)[4], const PagedCache& c, const Where& x) {
+        v.same();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i].load(at + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), 4 * (lane >> 4) * (uint32_t)c.vs, lane & 15);
-}
+        for (int i = 0; i < 4; ++i) to[i].load((const char*)c.v + x.v + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), v);
+    }
+};
 // What a block's scale bytes say: the scores' factor and the values' exponent.
 template <bool Q8>
 __device__ __forceinline__ void scales_of(const WinArgs& a, int info, float* ck, float* ev) {
@@ -570,18 +582,19 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
     // lane 2 j + h: block h of the wave's tile j of 32
     const int lane = threadIdx.x & 63;
     const int at0 = at + (lane & 1);
-    auto find = [&](int j) { return where<Q8>(c, sc, b, t, at0 + step * (j + (lane >> 1))); };
+    const Inner in = inner(b, a, t, t.lo, t.hi);
+    auto find = [&](int j) { return where<Q8>(c, sc, b, t, in, at0 + step * (j + (lane >> 1))); };
+    Loader<BF, Q8, D> load(c);
     Where run = find(0);
     int turn = 0, info[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const Where x = lane_of(run, h);
-        load_k<BF, Q8, D>(xk[h], c, keys_at<Q8>(c, t, x));
-        load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, x));
+        load.keys(xk[h], c, x);
+        load.values(xv[h], c, x);
         info[h] = x.info;
     }
     const bool several = t.position(0, a.per) != t.hi;
-    const Inner in = inner(b, a, t, t.lo, t.hi);
     for (int known = 31;; known += 32) {      // the last tile whose place the lanes hold
     for (; at < t.b1 && turn < known; at += step, ++turn) {
         float ck[2], ev[2];
@@ -602,9 +615,9 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 nx[h] = lane_of(run, (2 * turn + 2 + h) & 63);
-                load_k<BF, Q8, D>(xk[h], c, keys_at<Q8>(c, t, nx[h]));
+                load.keys(xk[h], c, nx[h]);
             }
-        const bool part = bad[0] | bad[1] | !in.holds(at, 2);
+        const bool part = (info[0] | info[1]) & (kBad | kPart);
         Blk x[2];
         if (part)
 #pragma unroll
@@ -620,7 +633,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         for (int i = 0; i < 8; ++i) xv[i >> 2][i & 3].wide(v[i], Q8 && BF ? ldexpf(1.f, (int)ev[i >> 2]) : 1.f);
         if (more)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) load_v<BF, Q8, D>(xv[h], c, values_at<Q8>(c, t, nx[h])), info[h] = nx[h].info;
+            for (int h = 0; h < 2; ++h) load.values(xv[h], c, nx[h]), info[h] = nx[h].info;
         bool fine = true;
         if (part) {
 #pragma unroll
@@ -677,18 +690,27 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
     // positions of the wave's first and last row
     const int hi = idle ? -1 : t.position(last, a.per), first = idle ? -1 : t.position(row0, a.per);
     const int lo = first < b.prefix && t.pos0 != kNowhere ? -1 : first;
-    const Inner in = inner(b, a, t, lo, hi), all = inner(b, a, t, t.lo, t.hi);
+    const Inner in = inner(b, a, t, lo, hi);
     Keys<BF, Q8, D> xk;
     Vals<BF, Q8, E> xv[4];
     // lane j: the block that the wave brings of stage j of 64
     Where run;
     int turn = 0, info = 0;                   // turn: of the stage that is worked on
-    auto find = [&](int j) { run = where<Q8>(c, sc, b, t, t.b0 + kBlocks * (j + lane) + w); };
+    auto find = [&](int j) { run = where<Q8>(c, sc, b, t, inner(b, a, t, t.lo, t.hi), t.b0 + kBlocks * (j + lane) + w); };
+    Loader<BF, Q8, D> load(c);
     auto bring = [&](int j) {
         const Where x = lane_of(run, j & 63);
-        load_k<BF, Q8, D>(xk, c, keys_at<Q8>(c, t, x));
-        load_v<BF, Q8, D>(xv, c, values_at<Q8>(c, t, x));
+        load.keys(xk, c, x);
+        load.values(xv, c, x);
         info = x.info;
+    };
+    auto write_v = [&](StageLds<D>& s, const uint32_t (&v)[4][EW]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel),
+                                                          __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel)};
+        }
     };
     auto put = [&](int at, StageLds<D>& s) {
         float ck, ev;
@@ -698,8 +720,9 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
         uint32_t v[4][EW];
 #pragma unroll
         for (int i = 0; i < 4; ++i) xv[i].wide(v[i], scale);
-        bool odd = false;
-        if (bad || !all.holds(at, 1)) {       // some row does not see some of it: a zero weight keeps no NaN out
+#pragma unroll
+        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = xk.get(k);
+        if (info & (kBad | kPart)) {          // some row does not see some of it: a zero weight keeps no NaN out
             const Blk y = look(b, t, at);
             bool fine = true;
 #pragma unroll
@@ -709,27 +732,25 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
 #pragma unroll
                 for (int m = 0; m < EW; ++m) v[i][m] = some ? sane<BF>(v[i][m], &fine) : 0;
             }
-            odd = __any(!fine);
-        }
-        if (lane == 0) s.odd[w] = odd;
+            fine = !__any(!fine);
+            if (lane == 0) s.odd[w] = !fine;
+            if (bad)                          // its scores are NaN
 #pragma unroll
-        for (int k = 0; k < NS; ++k) s.k[w][k][lane] = xk.get(k);
-        if (bad)                              // its scores are NaN
-#pragma unroll
-            for (int k = 0; k < NS; ++k) s.k[w][k][lane] = u32x4{~0u, ~0u, ~0u, ~0u};
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
-            ((u32x2*)&s.v[e][w >> 1][lane])[w & 1] = u32x2{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel),
-                                                          __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel)};
+                for (int k = 0; k < NS; ++k) s.k[w][k][lane] = u32x4{~0u, ~0u, ~0u, ~0u};
+            write_v(s, v);
+        } else {
+            if (lane == 0) s.odd[w] = 0;
+            write_v(s, v);
         }
         if (Q8 && lane == 0) s.ck[w] = bad ? 1.f : ck, s.ev[w] = bad ? 0.f : ev;
     };
     int at = t.b0;
-    find(0);
-    bring(0);
+    // (the queries first: loads come back in order, and one that is still out when the loop begins would be waited for in
+    // every stage)
     u32x4 q[NR][NS];
     load_q<BF, Q8, D, NR>(a, t, row0, q);
+    find(0);
+    bring(0);
     put(at + w, l[0]);
     if (at + kBlocks < t.b1) bring(1);
     // the next stage to LDS, the one after that on its way
@@ -783,7 +804,8 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
         if (turn == known) find(turn + 2), known += 64;
         // stages that all rows of the wave see (waves of a workgroup may leave at different ones: both loops have one
         // barrier a stage)
-        while (in.holds(at, kBlocks) && turn < known) {
+        const int to = !in.holds(at, kBlocks) ? INT32_MIN : in.pb < at ? in.w1 - kBlocks : min(in.w1, in.pb) - kBlocks;
+        while (at <= to && turn < known) {
             const StageLds<D>& st = l[turn & 1];
             __syncthreads();                  // the stage is there, and nobody reads the one before
             read_k(st, 0);
