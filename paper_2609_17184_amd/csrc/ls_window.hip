@@ -56,8 +56,10 @@ struct WinArgs {
     float c;                                  // scale * log2(e)
     int D;
     int H, per;                               // query heads; per key/value head
+    unsigned magic;                           // for quotients by per
     int W, S;                                 // window (kAll: none), sinks
     int RT;                                   // rows of a block
+    int most;                                 // blocks of 16 positions that a block of rows sees at most
     int NO, CT;                               // chunks at most, tiles of 32 positions per chunk
     int NP, CP;                               // the prefix for the rows of all sequences at once: chunks (0: it is not), tiles per chunk
     int rb, rows, ptasks;                     // blocks of these rows, rows of a block, workgroups
@@ -227,15 +229,23 @@ __device__ __forceinline__ int chunks_of(int n, int CT) { return max(1, ((n + 1)
 struct Task {
     const int32_t* table;
     int b0, b1;                               // its part of the list of blocks (b1 is the list's end or even)
-    int g, tok0, r0, rows;                    // row r of the block: row r0 + r of the tokens from tok0 (r < rows)
+    int g, tok0, lead, rows;                  // row r of the block: row lead + r of the tokens from tok0 on (r < rows, lead < per)
     int pos0;                                 // position of token tok0; kNowhere: all rows stand at hi
     int lo, hi;                               // of the first and last row (lo -1: some rows see nothing)
     int low;                                  // positions above it (or below the sinks) are seen by some row
     Seen s;
     int split, splits;                        // where the partial results go; 1: the results are whole
 
-    __device__ __forceinline__ int token(int r, int per) const { return tok0 + (r0 + r) / per; }
-    __device__ __forceinline__ int position(int r, int per) const { return pos0 == kNowhere ? hi : pos0 + (r0 + r) / per; }
+    __device__ __forceinline__ int offset(int r, const WinArgs& a) const { return (int)unit_div((unsigned)(lead + r), a.magic); }
+    __device__ __forceinline__ int token(int r, const WinArgs& a) const { return tok0 + offset(r, a); }
+    __device__ __forceinline__ int head(int r, const WinArgs& a) const { return g * a.per + lead + r - a.per * offset(r, a); }
+    __device__ __forceinline__ int position(int r, const WinArgs& a) const { return pos0 == kNowhere ? hi : pos0 + offset(r, a); }
+    // row r0 of the tokens from t0 on is the block's first
+    __device__ __forceinline__ void begin(int t0, int r0, const WinArgs& a) {
+        const int q = (int)((unsigned)r0 / (unsigned)a.per);
+        tok0 = t0 + q;
+        lead = r0 - q * a.per;
+    }
 };
 
 // 16 positions of a task's list: the first one and how many there are (0: behind the list's end)
@@ -297,58 +307,69 @@ __device__ __forceinline__ bool hidden(const Blk& x, int lo, int hi, const WinAr
 
 // The tasks, numbered sequence by sequence: (row block from the last on, chunk, key/value head).  How many there are
 // only the device knows; whoever asks for rising numbers walks the sequences once.
+// the lane's value added to those of all lanes below (no sum passes 2^32 - 1)
+__device__ __forceinline__ unsigned sum_upto(unsigned v) {
+    const auto add = [](unsigned x, unsigned y) { return x + y < x ? ~0u : x + y; };
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));         // the lane 1, 2, 4, 8 below, in rows of 16
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));        // a row's last lane to the next row
+    v = add(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));        // lane 31 to the upper half
+    return v;
+}
+
 struct Tasks {
     int base = 0;                             // the sequences before it hold `done` tasks
-    int64_t done = 0, last = INT64_MAX;       // the last 64 sequences' tasks end there
+    unsigned done = 0, last = ~0u;            // the last 64 sequences' tasks end there
 
-    __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, int64_t task, Task& t) {
+    template <int RT>
+    __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, unsigned task, Task& t) {
         if (task >= last) return false;       // (without asking for the lengths again)
         const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
         const int lane = threadIdx.x & 63, PB = (b.prefix + 15) >> 4;
         for (; base < b.B; base += 64) {
             Seq q{0, 0, 0};
             if (base + lane < b.B) q = seq_at(b, base + lane);
-            const int nb = (int)(((int64_t)q.n * a.per + a.RT - 1) / a.RT);
+            const int nb = (q.n * a.per + RT - 1) / RT;             // (rows are below 2^26)
             // chunks of its blocks of rows at most
             int most = (a.NP ? 0 : PB) + (int)((min(max((int64_t)q.first + q.n, (int64_t)0), cap) + 15) >> 4);
-            if (a.W < kAll) most = min(most, (int)(((int64_t)a.W + a.RT / a.per + 2 + 15) / 16 + 3 + ((int64_t)a.S + 15) / 16));
-            const int nc = chunks_of(most, a.CT);
-            const int64_t mine = (int64_t)nb * nc * c.G;
-            int64_t upto = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const int64_t v = __shfl_up(upto, o);
-                if (lane >= o) upto += v;
-            }
-            const unsigned long long over = __ballot(done + upto > task);
-            const int64_t end = done + (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32) |
-                                                 (unsigned)__builtin_amdgcn_readlane((int)upto, 63));
-            if (b.B - base <= 64) last = end;
+            most = min(most, a.most);
+            const int nc = a.NO == 1 ? 1 : chunks_of(most, a.CT);
+            const unsigned mine = (unsigned)nb * nc * c.G;          // (below 2^31: chunks go down as blocks go up)
+            const unsigned upto = sum_upto(mine);
+            const unsigned long long over = __ballot(upto > task - done);
+            const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+            if (b.B - base <= 64) last = done + all < done ? ~0u : done + all;
             if (!over) {
-                done = end;
+                done = done + all < done ? ~0u : done + all;
                 continue;
             }
             const int hit = __ffsll(over) - 1, sq = base + hit;
-            // (one sequence's tasks are below 2^31: its blocks of rows are, and chunks go down as these go up)
-            const unsigned rest = (unsigned)__builtin_amdgcn_readlane((int)(task - (done + upto - mine)), hit);
+            const unsigned rest = (unsigned)__builtin_amdgcn_readlane((int)(task - done - (upto - mine)), hit);
             const int n = __builtin_amdgcn_readlane(q.n, hit), first = __builtin_amdgcn_readlane(q.first, hit);
             const int ncs = __builtin_amdgcn_readlane(nc, hit), blocks = __builtin_amdgcn_readlane(nb, hit);
-            t.g = (int)(rest % (unsigned)c.G);
-            const unsigned rc = rest / (unsigned)c.G;
-            const int ch = (int)(rc % (unsigned)ncs), rb = blocks - 1 - (int)(rc / (unsigned)ncs);
+            const unsigned rc = rest / (unsigned)c.G, above = ncs == 1 ? rc : rc / (unsigned)ncs;
+            if (above >= (unsigned)blocks) return false;            // (only where first tokens do not ascend)
+            t.g = (int)(rest - rc * c.G);
+            const int ch = (int)(rc - above * ncs), rb = blocks - 1 - (int)above;
             t.table = b.table + sq * b.table_stride;
-            t.tok0 = __builtin_amdgcn_readlane(q.start, hit);
-            t.pos0 = b.prefix + first;
-            t.r0 = rb * a.RT;
-            t.rows = (int)min((int64_t)a.RT, (int64_t)n * a.per - t.r0);
-            t.lo = t.position(0, a.per);
-            t.hi = t.position(t.rows - 1, a.per);
+            t.begin(__builtin_amdgcn_readlane(q.start, hit), rb * RT, a);
+            t.pos0 = b.prefix + first + (t.tok0 - __builtin_amdgcn_readlane(q.start, hit));
+            t.rows = min(RT, n * a.per - rb * RT);
+            t.lo = t.pos0;
+            t.hi = t.position(t.rows - 1, a);
             t.s = seen(b, a, cap, t.lo, t.hi);
-            const int n_chunks = chunks_of(t.s.n, a.CT), tiles = (t.s.n + 1) / 2, each = (tiles + n_chunks - 1) / n_chunks;
-            t.splits = a.fold ? 1 : a.NP + n_chunks;
-            t.split = a.fold ? 0 : a.NP + ch;
-            t.b0 = 2 * ch * each;
-            t.b1 = min(t.s.n, t.b0 + 2 * each);
+            t.b0 = 0, t.b1 = t.s.n;
+            t.splits = 1;
+            if (a.NO > 1) {
+                const int n_chunks = chunks_of(t.s.n, a.CT), tiles = (t.s.n + 1) / 2, each = (tiles + n_chunks - 1) / n_chunks;
+                t.splits = n_chunks;
+                t.b0 = 2 * ch * each;
+                t.b1 = min(t.s.n, t.b0 + 2 * each);
+            }
+            t.split = ch;
+            if (!a.fold) t.splits += a.NP, t.split += a.NP;
             t.low = max(t.lo, b.prefix) - a.W;
             if (t.lo < b.prefix) t.lo = -1;
             return true;
@@ -368,9 +389,8 @@ __device__ __forceinline__ bool prefix_task(const PagedCache& c, const PagedBatc
     t.s = Seen{0, 0, PB};
     t.b0 = 2 * t.split * a.CP;
     t.b1 = min(PB, t.b0 + 2 * a.CP);
-    t.tok0 = 0;
-    t.r0 = rb * a.rows;
-    t.rows = min(a.rows, b.T * a.per - t.r0);
+    t.begin(0, rb * a.rows, a);
+    t.rows = min(a.rows, b.T * a.per - rb * a.rows);
     t.pos0 = kNowhere;
     t.lo = t.hi = b.prefix - 1;
     t.low = t.lo - a.W;
@@ -389,10 +409,10 @@ struct Rows {
     float ref[NR], sum[NR];                   // weights are 2^(c * score (+ e) - ref)
     int hi[NR];                               // the lane's rows' positions; -1: they see nothing
 
-    __device__ __forceinline__ void start(const Task& t, int P, int per, int row0) {
+    __device__ __forceinline__ void start(const Task& t, int P, const WinArgs& a, int row0) {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
-            const int i = row0 + rt * 16 + (threadIdx.x & 15), p = t.position(i, per);
+            const int i = row0 + rt * 16 + (threadIdx.x & 15), p = t.position(i, a);
             hi[rt] = i < t.rows && (p >= P || t.pos0 == kNowhere) ? p : -1;
             ref[rt] = kNone, sum[rt] = 0.f;
 #pragma unroll
@@ -556,7 +576,7 @@ __device__ __forceinline__ void load_q(const WinArgs& a, const Task& t, int row0
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
-        const int i = row0 + rt * 16 + n, tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+        const int i = row0 + rt * 16 + n, tok = t.token(i, a), h = t.head(i, a);
 #pragma unroll
         for (int s = 0; s < (D + 31) / 32; ++s) {
             const int d = Keys<BF, Q8, D>::first(s, gq);
@@ -573,7 +593,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
                                      const Task& t, int at, int step, Rows<BF, Q8, D, 1>& r) {
     constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
     const int gq = (threadIdx.x & 63) >> 4;
-    r.start(t, b.prefix, a.per, 0);
+    r.start(t, b.prefix, a, 0);
     if (at >= t.b1) return;
     u32x4 q[1][NS];                           // (on their way while the pages are looked up)
     load_q<BF, Q8, D, 1>(a, t, 0, q);
@@ -594,7 +614,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
         load.values(xv[h], c, x);
         info[h] = x.info;
     }
-    const bool several = t.position(0, a.per) != t.hi;
+    const bool several = t.position(0, a) != t.hi;
     for (int known = 31;; known += 32) {      // the last tile whose place the lanes hold
     for (; at < t.b1 && turn < known; at += step, ++turn) {
         float ck[2], ev[2];
@@ -683,12 +703,12 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
     constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
     const int lane = threadIdx.x & 63, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = w * NR * 16;             // the wave's rows of the block
-    r.start(t, b.prefix, a.per, row0);
+    r.start(t, b.prefix, a, row0);
     if (t.b0 >= t.b1) return;
     const int last = min(row0 + 16 * NR, t.rows) - 1;
     const bool idle = last < row0;
     // positions of the wave's first and last row
-    const int hi = idle ? -1 : t.position(last, a.per), first = idle ? -1 : t.position(row0, a.per);
+    const int hi = idle ? -1 : t.position(last, a), first = idle ? -1 : t.position(row0, a);
     const int lo = first < b.prefix && t.pos0 != kNowhere ? -1 : first;
     const Inner in = inner(b, a, t, lo, hi);
     Keys<BF, Q8, D> xk;
@@ -911,7 +931,7 @@ __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t e
     for (int rt = 0; rt < NR; ++rt) {
         const int i = row0 + rt * 16 + n;
         if (i >= t.rows) continue;
-        const int tok = t.token(i, a.per), h = t.g * a.per + (t.r0 + i) % a.per;
+        const int tok = t.token(i, a), h = t.head(i, a);
         const size_t at = (size_t)tok * a.H + h;
         if (t.splits > 1) {
             const size_t slot = at * a.slots + t.split;
@@ -978,7 +998,7 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix
         for (int k = 0; k < 4; ++k) tp = fmaxf(tp, l.ml[k][row][0]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) sm += l.ml[k][row][1] * __builtin_amdgcn_exp2f(l.ml[k][row][0] - tp);
-        const int tok = t.token(row, a.per), h = t.g * a.per + (t.r0 + row) % a.per;
+        const int tok = t.token(row, a), h = t.head(row, a);
         const size_t at = (size_t)tok * a.H + h;
         if (t.splits > 1) {
             const size_t slot = at * a.slots + t.split;
@@ -986,7 +1006,7 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix
             if (d == 0) a.ml[slot * 2] = tp, a.ml[slot * 2 + 1] = sm;
             continue;
         }
-        if (a.fold && t.position(row, a.per) >= prefix) {               // (others see nothing)
+        if (a.fold && t.position(row, a) >= prefix) {               // (others see nothing)
             float x[4] = {v[0], v[1], v[2], v[3]};
             take_in<4>(a, at, &tp, &sm, x, [d](int i) { return d + i; });
             v = f32x4{x[0], x[1], x[2], x[3]};
@@ -1001,15 +1021,15 @@ __device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix
 // The next task of a workgroup or wave: the prefix's for workgroups below ptasks, which have one, else the sequences'.
 struct Asked {
     Tasks all;
-    int64_t task;
-    int step;
+    unsigned task, step;
     bool prefix, done = false;
 
     __device__ __forceinline__ Asked(const WinArgs& a, int waves) : prefix((int)blockIdx.x < a.ptasks) {
         const int w = waves > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-        task = (int64_t)((int)blockIdx.x - a.ptasks) * waves + w;
-        step = ((int)gridDim.x - a.ptasks) * waves;
+        task = (blockIdx.x - a.ptasks) * waves + w;
+        step = (gridDim.x - a.ptasks) * waves;
     }
+    template <int RT>
     __device__ __forceinline__ bool next(const PagedCache& c, const PagedBatch& b, const WinArgs& a, Task& t) {
         if (prefix) {
             if (done) return false;
@@ -1017,8 +1037,8 @@ struct Asked {
             return prefix_task(c, b, a, t);
         }
         for (;;) {
-            if (!all.find(c, b, a, task, t)) return false;
-            task += step;
+            if (!all.template find<RT>(c, b, a, task, t)) return false;
+            task = task + step < task ? ~0u : task + step;
             if (t.split < t.splits) return true;                    // (fewer chunks than the sequence's longest block of rows)
         }
     }
@@ -1034,7 +1054,7 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_
     __shared__ StageLds<D> l[2];
     Asked asked(a, 1);
     Task t;
-    while (asked.next(c, b, a, t)) {
+    while (asked.template next<kWideRows>(c, b, a, t)) {
         Rows<BF, Q8, D, NR> r;
         __syncthreads();                      // an earlier task's LDS is read out
         walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l, r);
@@ -1048,7 +1068,7 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_
     __shared__ MeetLds<D> l;
     Asked asked(a, 1);
     Task t;
-    while (asked.next(c, b, a, t)) {
+    while (asked.template next<kFewRows>(c, b, a, t)) {
         Rows<BF, Q8, D, 1> r;
         walk<BF, Q8, D>(c, sc, b, a, t, t.b0 + 2 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, r);
         meet<BF, Q8, D>(a, t, b.prefix, asked.end(c, b), r, l);
@@ -1060,7 +1080,7 @@ template <bool BF, bool Q8, int D>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window_waves(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
     Asked asked(a, 4);
     Task t;
-    while (asked.next(c, b, a, t)) {
+    while (asked.template next<kFewRows>(c, b, a, t)) {
         Rows<BF, Q8, D, 1> r;
         walk<BF, Q8, D>(c, sc, b, a, t, t.b0, 2, r);
         store<BF, Q8, D, 1, true>(a, t, asked.end(c, b), r, 0);
@@ -1080,8 +1100,8 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     const Seq q = seq_at(b, sq);
     if (t - q.start >= q.n) return;           // padding: its output stays as it is
     const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
-    const int64_t rb = ((int64_t)(t - q.start) * a.per + h % a.per) / a.RT;
-    const int lo = (int)(rb * a.RT / a.per), hi = (int)min((rb * a.RT + a.RT - 1) / a.per, (int64_t)q.n - 1);
+    const unsigned r0 = ((t - q.start) * a.per + h % a.per) & ~(a.RT - 1u);       // (RT is a power of two)
+    const int lo = (int)(r0 / a.per), hi = min((int)((r0 + a.RT - 1) / a.per), q.n - 1);
     int n = a.NP + chunks_of(seen(b, a, cap, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
     if (n == 1) return;                       // finished where it was computed
     if (place < 0) n = 0;                     // (the prefix was worked on for all rows)
@@ -1135,7 +1155,7 @@ enum { WIDE, SMALL, WAVES };                  // kernels
 
 struct Plan {
     bool wide_own;
-    int RT, NO, CT, NP, CP, rb, rows, ptasks, groups;
+    int RT, most, NO, CT, NP, CP, rb, rows, ptasks, groups;
     int own, before, slots;                   // kernels of the sequences' tasks and of the prefix's; partial results of a row
     bool fold;
 };
@@ -1179,6 +1199,7 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     // blocks of 16 positions that a block of rows may see
     int64_t most = (together ? 0 : (b.prefix + 15) / 16) + held;
     if (W < kAll) most = std::min(most, ((int64_t)W + p->RT / per + 2 + 15) / 16 + 3 + ((int64_t)S + 15) / 16);
+    p->most = (int)most;
     const int64_t tiles = std::max<int64_t>(1, (most + 1) / 2);
     const int64_t blocks = (seqs + std::max<int64_t>(rows - seqs * per, 0) / p->RT) * c.G;
     // About 1024 tasks where the tables are full (over 18 batches of ragged lengths 384 to 1536 are within 3 %), of at least
@@ -1204,6 +1225,9 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     p->slots = p->fold ? p->NP : p->NP + p->NO > 1 ? p->NP + p->NO : 0;
     return LOOPSPEC_OK;
 }
+
+// for unit_div of numbers below per + 128 by per
+unsigned unit_magic(int per) { return per > 1 ? (unsigned)(((1ull << 32) + per - 1) / per) : 0u; }
 
 uint64_t bytes_of(const PagedCache& c, const PagedBatch& b, int H, const Plan& p) {
     return (uint64_t)b.T * H * p.slots * (c.D + 2) * 4;
@@ -1279,7 +1303,7 @@ int loopspec_window_attention(const loopspec_paged_cache* cache, const loopspec_
     const uint64_t rows = (uint64_t)b.T * args->n_heads;
     WinArgs a{(const uint16_t*)args->q_dev, args->q_token, args->q_head, (uint16_t*)args->out_dev, args->out_token, args->out_head,
               args->lse_dev, (float*)workspace_dev, (float*)workspace_dev + rows * p.slots * c.D, cs, c.D, args->n_heads,
-              args->n_heads / c.G, window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.NO, p.CT,
+              args->n_heads / c.G, unit_magic(args->n_heads / c.G), window ? std::min(window, kAll) : kAll, std::min(sinks, kAll), p.RT, p.most, p.NO, p.CT,
               p.NP, p.CP, p.rb, p.rows, 0, p.slots, p.fold};
     hipStream_t st = (hipStream_t)stream;
     const bool bf = cache->dtype == LOOPSPEC_BF16, q8 = scales != nullptr;
