@@ -213,9 +213,9 @@ struct Seen {
     int head, from, n;
 };
 __device__ __forceinline__ int block_of(int j, int P, int PB) { return j < P ? j >> 4 : PB + ((j - P) >> 4); }
-__device__ __forceinline__ Seen seen(const PagedBatch& b, const WinArgs& a, int64_t cap, int lo, int hi) {
+__device__ __forceinline__ Seen seen(const PagedBatch& b, const WinArgs& a, int cap, int lo, int hi) {
     const int P = b.prefix, PB = (P + 15) >> 4;
-    hi = (int)min((int64_t)hi, P + cap - 1);
+    hi = min(hi, P + cap - 1);                // (a table spans 2^28 positions at most, a prefix as many)
     lo = max(lo, P);
     if (hi < P) return Seen{0, 0, 0};         // (behind the table's end lo may pass hi)
     const int to = block_of(hi, P, PB) + 1;
@@ -326,14 +326,14 @@ struct Tasks {
     template <int RT>
     __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, unsigned task, Task& t) {
         if (task >= last) return false;       // (without asking for the lengths again)
-        const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
+        const int cap = b.width * c.unit * kPageUnit;
         const int lane = threadIdx.x & 63, PB = (b.prefix + 15) >> 4;
         for (; base < b.B; base += 64) {
             Seq q{0, 0, 0};
             if (base + lane < b.B) q = seq_at(b, base + lane);
             const int nb = (q.n * a.per + RT - 1) / RT;             // (rows are below 2^26)
             // chunks of its blocks of rows at most
-            int most = (a.NP ? 0 : PB) + (int)((min(max((int64_t)q.first + q.n, (int64_t)0), cap) + 15) >> 4);
+            int most = (a.NP ? 0 : PB) + ((min(max(q.first + q.n, 0), cap) + 15) >> 4);
             most = min(most, a.most);
             const int nc = a.NO == 1 ? 1 : chunks_of(most, a.CT);
             const unsigned mine = (unsigned)nb * nc * c.G;          // (below 2^31: chunks go down as blocks go up)
@@ -535,7 +535,7 @@ struct Rows {
                 }
         }
     }
-    __device__ __forceinline__ void finish(int64_t end) {
+    __device__ __forceinline__ void finish(int end) {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
             sum[rt] += __shfl_xor(sum[rt], 16);
@@ -829,7 +829,9 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
             const StageLds<D>& st = l[turn & 1];
             __syncthreads();                  // the stage is there, and nobody reads the one before
             read_k(st, 0);
+            __builtin_amdgcn_s_setprio(1);    // (everybody waits for it: 80 -> 78 us for 1000 rows over 8007 positions)
             next();
+            __builtin_amdgcn_s_setprio(0);
             factors(st, 0);
             scores();
             read_v(st, 0);
@@ -923,7 +925,7 @@ __device__ __forceinline__ void take_in(const WinArgs& a, size_t row, float* ref
 
 // a wave's rows without the workgroup's other waves: partial results, or whole ones
 template <bool BF, bool Q8, int D, int NR, bool FOLD>
-__device__ __forceinline__ void store(const WinArgs& a, const Task& t, int64_t end, Rows<BF, Q8, D, NR>& r, int row0) {
+__device__ __forceinline__ void store(const WinArgs& a, const Task& t, int end, Rows<BF, Q8, D, NR>& r, int row0) {
     constexpr int E = D / 16;
     const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
     r.finish(end);
@@ -972,7 +974,7 @@ struct MeetLds {
 
 // the four waves' results of a workgroup's task, summed and stored
 template <bool BF, bool Q8, int D>
-__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix, int64_t end, Rows<BF, Q8, D, 1>& r, MeetLds<D>& l) {
+__device__ __forceinline__ void meet(const WinArgs& a, const Task& t, int prefix, int end, Rows<BF, Q8, D, 1>& r, MeetLds<D>& l) {
     constexpr int E = D / 16;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, n = lane & 15, gq = lane >> 4;
     r.finish(end);
@@ -1042,8 +1044,8 @@ struct Asked {
             if (t.split < t.splits) return true;                    // (fewer chunks than the sequence's longest block of rows)
         }
     }
-    __device__ __forceinline__ int64_t end(const PagedCache& c, const PagedBatch& b) const {
-        return prefix ? (int64_t)kAll : b.prefix + (int64_t)b.width * c.unit * kPageUnit;
+    __device__ __forceinline__ int end(const PagedCache& c, const PagedBatch& b) const {
+        return prefix ? kAll : b.prefix + b.width * c.unit * kPageUnit;
     }
 };
 
@@ -1099,7 +1101,7 @@ __global__ void __launch_bounds__(kT) k_window_join(PagedCache c, PagedBatch b, 
     if (sq < 0) return;
     const Seq q = seq_at(b, sq);
     if (t - q.start >= q.n) return;           // padding: its output stays as it is
-    const int64_t cap = (int64_t)b.width * c.unit * kPageUnit;
+    const int cap = b.width * c.unit * kPageUnit;
     const unsigned r0 = ((t - q.start) * a.per + h % a.per) & ~(a.RT - 1u);       // (RT is a power of two)
     const int lo = (int)(r0 / a.per), hi = min((int)((r0 + a.RT - 1) / a.per), q.n - 1);
     int n = a.NP + chunks_of(seen(b, a, cap, b.prefix + q.first + lo, b.prefix + q.first + hi).n, a.CT);
