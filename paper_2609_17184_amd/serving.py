@@ -9,6 +9,13 @@ For one layer and one step of a batch:
     ...
     tokens, probs, kept = sample(logits, u, temperature, top_k, top_p, min_p)
 
+For long contexts the cache may be a QuantizedCache (8-bit pages), attention window_attention (a window and a few first
+positions, or all, over either cache), and between steps
+
+    seq_len, table, refs, short = fork_pages(seq_len, table, parent, refs, caches, P, window, sinks, room=1)
+
+continues some rows, several times or not at all, and lets their pages go that nobody needs.
+
 Argument marshalling only: the work runs in the HIP library, on the current
 stream of the tensors' device, without waiting for it, and records no
 gradients.  Wrong shapes, types or

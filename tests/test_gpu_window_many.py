@@ -22,6 +22,9 @@ BATCHES = [
     (32, 8, 32, 16, "f16", [9] * 65, [i * 5 % 50 + 9 for i in range(65)], 20),       # 36 rows: blocks of many rows
     (55, 55, 96, 16, "f16", [1] * 12, [i * 31 % 200 + 1 for i in range(12)], 40),
     (8, 8, 128, 48, "bf16", [i % 4 for i in range(150)], [i * 11 % 300 + 3 for i in range(150)], 61),
+    (300, 1, 16, 16, "f16", [1, 2, 1], [1, 40, 30], 33),                             # more heads on one than a block has rows
+    (47, 1, 32, 16, "bf16", [1] * 6, [9, 40, 1, 16, 33, 70], 900),
+    (14, 2, 64, 16, "f16", [5, 0, 7, 1], [5, 3, 90, 200], 0),                        # heads that divide no block
 ]
 
 
