@@ -585,10 +585,11 @@ struct Loader {
         for (int i = 0; i < 4; ++i) to[i].load((const char*)c.v + x.v + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), v);
     }
 };
-// What a block's scale bytes say: the scores' factor and the values' exponent.
+// What a block's scale bytes say: the scores' factor (neither 0 nor infinite, which times the -infinity of a hidden position
+// or a score of 0 were NaN) and the values' exponent.
 template <bool Q8>
 __device__ __forceinline__ void scales_of(const WinArgs& a, int info, float* ck, float* ev) {
-    *ck = Q8 ? ldexpf(a.c, (info & 255) - 127) : a.c;
+    *ck = Q8 ? __builtin_amdgcn_fmed3f(ldexpf(a.c, (info & 255) - 127), 0x1p-126f, 0x1p127f) : a.c;
     *ev = Q8 ? (float)value_exp(info >> 8 & 255) : 0.f;
 }
 

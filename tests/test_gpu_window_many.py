@@ -146,3 +146,18 @@ def test_scores_too_large_for_their_differences(many, dtype, eight, size):
     torch.testing.assert_close(out.cpu().double(), want, rtol=2 * torch.finfo(c.dtype).eps, atol=0)
     score = size * size * D ** 0.5
     assert (lse.cpu().double() / score - 1).abs().max() < 2.0 ** -19
+
+
+@pytest.mark.parametrize("new", [[3, 1], [60, 1], [1] * 130])
+@pytest.mark.parametrize("byte,scale", [(63, 1e-30), (1, 1e-3), (250, 300.0)])
+def test_factors_of_scores_at_fp32s_ends(new, byte, scale):
+    """Key scales and a scale of the scores whose product leaves fp32, downwards or upwards (then with keys of 0): no score
+    and no hidden position becomes NaN by it."""
+    c = Quantized(16, 8, 32, 16, "bf16", new, [n + 40 for n in new], 21, seed=13)
+    c.kb.view(torch.uint8)[c.kb.view(torch.uint8) != 255] = byte
+    if byte == 250:
+        c.kd.view(torch.uint8).zero_()
+        c.kc.zero_()
+    c.k = c.kc.nan_to_num(0.0) * 2.0 ** (byte - 127) * scale * 32 ** 0.5
+    out, lse = attend(c, 30, 5, scale)
+    check_window(c, 30, 5, 32 ** -0.5, out, lse, torch.full(c.q.shape, 3.0, dtype=c.dtype))
