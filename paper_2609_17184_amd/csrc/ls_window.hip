@@ -112,7 +112,11 @@ __device__ __forceinline__ constexpr int column_of(int m, int e) {
 // 64-bit addresses of them outside the loops and add these to every block's base, 2 registers and an instruction a load.
 struct Offsets {
     uint32_t a, b;
-    __device__ __forceinline__ void same() { asm("" : "+v"(a), "+v"(b)); }
+    template <bool BOTH>
+    __device__ __forceinline__ void same() {
+        asm("" : "+v"(a));
+        if (BOTH) asm("" : "+v"(b));
+    }
 };
 
 // A lane's part of the keys of 16 positions.
@@ -346,6 +350,9 @@ struct Tasks {
 
     template <int RT>
     __device__ bool find(const PagedCache& c, const PagedBatch& b, const WinArgs& a, unsigned task, Task& t) {
+        // the same in all lanes, which the compiler does not see
+        task = __builtin_amdgcn_readfirstlane(task), last = __builtin_amdgcn_readfirstlane(last);
+        done = __builtin_amdgcn_readfirstlane(done), base = __builtin_amdgcn_readfirstlane(base);
         if (task >= last) return false;       // (without asking for the lengths again)
         const int cap = b.width * c.unit * kPageUnit;
         const int lane = threadIdx.x & 63, PB = (b.prefix + 15) >> 4;
@@ -576,11 +583,11 @@ struct Loader {
         v = Vals<BF, Q8, D / 16>::offsets(4 * (lane >> 4) * (uint32_t)c.vs, lane & 15);
     }
     __device__ __forceinline__ void keys(Keys<BF, Q8, D>& to, const PagedCache& c, const Where& x) {
-        k.same();
+        k.template same<Q8 && D % 64 != 0>();
         to.load((const char*)c.k + x.k, k, (threadIdx.x & 63) >> 4);
     }
     __device__ __forceinline__ void values(Vals<BF, Q8, D / 16> (&to)[4], const PagedCache& c, const Where& x) {
-        v.same();
+        v.template same<Q8 && D == 96>();
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i].load((const char*)c.v + x.v + (int64_t)i * (Q8 ? c.vs : 2 * c.vs), v);
     }
@@ -949,7 +956,12 @@ __device__ __forceinline__ void take_in(const WinArgs& a, size_t row, float* ref
 template <bool BF, bool Q8, int D, int NR, bool FOLD>
 __device__ __forceinline__ void store(const WinArgs& a, const Task& t, int end, Rows<BF, Q8, D, NR>& r, int row0) {
     constexpr int E = D / 16;
-    const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+    // Where all registers are in use, the lane is made here: the compiler would hold addresses that hang on it through all of
+    // the task, and for them put others into memory.  No kernel here does that; where it is done at the begin of a block
+    // that some lanes skip, the lanes' common numbers are lost for these (seen with three waves a SIMD, which need it).
+    int lane = threadIdx.x & 63;
+    if (!Q8 && D == 128) asm volatile("" : "+v"(lane));
+    const int n = lane & 15, gq = lane >> 4;
     r.finish(end);
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {

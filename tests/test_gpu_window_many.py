@@ -22,6 +22,8 @@ BATCHES = [
     (32, 8, 32, 16, "f16", [9] * 65, [i * 5 % 50 + 9 for i in range(65)], 20),       # 36 rows: blocks of many rows
     (55, 55, 96, 16, "f16", [1] * 12, [i * 31 % 200 + 1 for i in range(12)], 40),
     (8, 8, 128, 48, "bf16", [i % 4 for i in range(150)], [i * 11 % 300 + 3 for i in range(150)], 61),
+    (16, 16, 32, 32, "f16", [1] * 200, [i * 37 % 900 + 1 for i in range(200)], 0),   # workgroups that take six tasks each
+    (4, 4, 128, 32, "f16", [1] * 400, [i * 37 % 800 + 1 for i in range(400)], 0),
     (300, 1, 16, 16, "f16", [1, 2, 1], [1, 40, 30], 33),                             # more heads on one than a block has rows
     (47, 1, 32, 16, "bf16", [1] * 6, [9, 40, 1, 16, 33, 70], 900),
     (14, 2, 64, 16, "f16", [5, 0, 7, 1], [5, 3, 90, 200], 0),                        # heads that divide no block
@@ -161,3 +163,20 @@ def test_factors_of_scores_at_fp32s_ends(new, byte, scale):
     c.k = c.kc.nan_to_num(0.0) * 2.0 ** (byte - 127) * scale * 32 ** 0.5
     out, lse = attend(c, 30, 5, scale)
     check_window(c, 30, 5, 32 ** -0.5, out, lse, torch.full(c.q.shape, 3.0, dtype=c.dtype))
+
+
+@pytest.mark.parametrize("D,dtype,eight", [(16, "bf16", False), (16, "f16", True), (128, "f16", False)])
+def test_more_blocks_of_rows_than_workgroups(D, dtype, eight):
+    """Prompts whose blocks of rows are more than the workgroups of a launch, which go on from one to the next: the same
+    bits as from fewer of them at once."""
+    from paper_2609_17184_amd import serving
+    G, B, n = 64, 272, 50
+    c = (Quantized if eight else Case)(G, G, D, 16, dtype, [n] * B, [n + i % 12 for i in range(B)], 0, seed=14)
+    q = c.q.to(DEV)
+    out, lse = serving.window_attention(q, c.cache, c.batch, 40, 3, return_lse=True)
+    starts = torch.arange(69, dtype=torch.int32, device=DEV) * n
+    for b in range(0, B, 68):
+        part = serving.Batch(c.batch.seq_len[b:b + 68].contiguous(), c.batch.table[b:b + 68], starts)
+        o, l = serving.window_attention(q[b * n:(b + 68) * n], c.cache, part, 40, 3, return_lse=True)
+        assert torch.equal(o, out[b * n:(b + 68) * n]) and torch.equal(l, lse[b * n:(b + 68) * n])
+    assert out.isfinite().all() and lse.isfinite().all()
