@@ -18,7 +18,7 @@
 // Bound by memory and by the angles and codes beside it: 16001 tokens of 28 query
 // and 4 key and value heads of 128 (bf16, norms, half of a head rotated, 278 MB)
 // take 62 us, 4.5 TB/s, of which a large copy's rate is 59; 5 prompts of up to 900
-// tokens of 55 heads of 96 (fp16, 176 MB) 53 us, 3.3 TB/s, the run's angles anew in
+// tokens of 55 heads of 96 (fp16, 176 MB) 52 us, 3.4 TB/s, the run's angles anew in
 // each of its slices.  One token takes 4 us, a launch and the loads that wait for
 // each other.
 #include "ls_paged.h"
@@ -58,6 +58,22 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
     const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(c, 0), __builtin_amdgcn_cvt_f32_fp8(c, 1), __builtin_amdgcn_cvt_f32_fp8(c, 2),
                         __builtin_amdgcn_cvt_f32_fp8(c, 3)};
     return encode4(x, f);
+}
+
+// Sine and cosine of a fraction of a turn, |x| <= 1/2: Taylor's series on an eighth of a turn to either side, in 64 bits
+// (their next terms are below 2^-36 of the result), each rounded once.  fp32's functions are off by up to two roundings,
+// and a key's code shows on which side of a border a value lies (against 64 bits its error was twice that of exactly rounded
+// angles).  18 products; 5 prompts of 55 heads take 52 us, with fp32's functions 53.
+__device__ __forceinline__ void sine_cosine(double x, float* sine, float* cosine) {
+    const int quarter = (int)rint(4.0 * x);
+    const double a = (x - 0.25 * quarter) * 6.283185307179586477, z = a * a;
+    const double s = a * fma(z, fma(z, fma(z, fma(z, fma(z, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
+    const double c = fma(z, fma(z, fma(z, fma(z, fma(z, fma(z, 1.0 / 479001600, -1.0 / 3628800), 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
+    const float fs = (float)s, fc = (float)c;
+    const bool odd = quarter & 1;             // a quarter turn on: the sine is the cosine, the cosine the sine's negative
+    const float p = odd ? fc : fs, q = odd ? -fs : fc;
+    *sine = quarter & 2 ? -p : p;
+    *cosine = quarter & 2 ? -q : q;
 }
 
 // A run: token t0 + i begins it at `place` of sequence `seq`, n tokens long.
@@ -206,14 +222,8 @@ __global__ void __launch_bounds__(kT) k_append8(PagedCache c, PageScales sc, Pag
         for (int j = tid; j < r.n * half; j += kT) {
             const int t = j / half, f = j - t * half;
             const double turns = (double)(b.prefix + r.place + t) * a.freq[f] * 0.15915494309189533577;
-            // the fraction of a turn in two floats: one alone is off by 2^-26, which the codes' rounding shows (a key's error
-            // against 64 bits 8e-5 instead of 4e-5)
             const double part = turns - rint(turns);
-            const float a0 = (float)part, a1 = 6.2831853f * (float)(part - (double)a0);
-            float sn, cn;
-            sincospif(2.0f * a0, &sn, &cn);
-            cs[t][f] = fmaf(-a1, sn, cn);
-            cs[t][64 + f] = fmaf(a1, cn, sn);
+            sine_cosine(part, &cs[t][64 + f], &cs[t][f]);
         }
         __syncthreads();
         const int first = by * kW + w, step = slices * kW;
@@ -259,10 +269,10 @@ extern "C" int loopspec_rope_append_quantized(const loopspec_paged_cache* cache,
     int per = b.T > 1 << 22 || (b.q_start && b.T >= 8ll * b.B) ? 16 : 1;    // (a grid holds 2^32 threads)
     const int x = (b.T + per - 1) / per;
     // Slices of the heads, each of which takes the run's angles again: 1001 runs of 36 heads 60.6 us in one, 67.0 in two;
-    // 214 runs of 165 heads 54.9 in nine, 58.5 in four, 65.2 in two.  Workgroups of 256 threads, whose share of the angles
-    // is twice as long, take 61.8 and 54.0, of 1024 67.0 and 58.4.
+    // 214 runs of 165 heads 57.3 in nine, 52.4 in seven, 54.2 in six, 53.2 in five, 65.2 in two.  Workgroups of 256 threads,
+    // whose share of the angles is twice as long, took 61.8 and 54.0 where these took 60.6 and 53, of 1024 67.0 and 58.4.
     const int most = per > 1 ? (items + kW - 1) / kW : (items * L + 64 * kW - 1) / (64 * kW);
-    int slices = std::max(1, std::min(most, 1900 / x));
+    int slices = std::max(1, std::min(most, 1500 / x));
     void* kargs[] = {&c, &s, &b, &a, &per, &slices};
     const void* f = cache->dtype == LOOPSPEC_BF16 ? append8_kernel<true>(L) : append8_kernel<false>(L);
     return hipLaunchKernel(f, dim3(x * slices), dim3(kT), kargs, 0, (hipStream_t)stream) == hipSuccess ? LOOPSPEC_OK : LOOPSPEC_EHIP;
