@@ -27,7 +27,7 @@
 // queries' type for the second product.
 //
 // Three kernels, since one that held all three ways had the registers of the
-// largest (and 135 us where two launches take 76): blocks of 128 rows, whose four
+// largest (and 135 us where two launches take 73): blocks of 128 rows, whose four
 // waves share positions through LDS (k_window_wide); blocks of 16, whose waves
 // take every fourth tile and meet at the end (k_window); a wave alone for short
 // tasks (k_window_waves).
@@ -36,12 +36,12 @@
 // heads of 128 over 4100 of 12000 positions (bf16, 954 MB): 166, 5.7 TB/s; a large
 // copy moves 4.8.  32 rows of 16 heads of 128 over up to 8192 positions (fp16 over
 // 8-bit pages, 584 MB): 118, 4.9 TB/s, 5 of them the join.  8001 rows of 28 heads
-// on 4 of 128 under a window of 2048 (bf16, 206 GFLOP): 232, 890 TFLOP/s; the
+// on 4 of 128 under a window of 2048 (bf16, 206 GFLOP): 235, 880 TFLOP/s; the
 // matrix cores are busy 36 % of the cycles and vector instructions 41 %, which two
 // waves a SIMD overlap in part only.  250 tokens of 32 heads on 8 of 128 behind
-// 8007 positions (bf16 over 8-bit pages, 33 GFLOP): 76, of which the own positions'
+// 8007 positions (bf16 over 8-bit pages, 33 GFLOP): 73, of which the own positions'
 // launch and the taking in of partial results 22.  5 prompts of up to 900 tokens,
-// 55 heads of 96 (fp16 over 8-bit pages, 66 GFLOP): 147; a task's begin and end
+// 55 heads of 96 (fp16 over 8-bit pages, 66 GFLOP): 145; a task's begin and end
 // (lengths, pages, first loads, the two stages that the diagonal cuts) take 13 of
 // the 25 that a block of 128 rows over 640 positions does, while the CU's other
 // workgroup goes on.  One token: 8, of which 3 are an empty launch and the rest
