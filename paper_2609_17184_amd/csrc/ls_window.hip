@@ -530,11 +530,12 @@ struct Rows {
         take(s, w, ck, ev);
         settle(s, w, p, ck, ev);
     }
-    // What values that are not finite contribute to the rows that see them: the products' operand has zeros in their
-    // places, since a zero weight would not keep them out of the other rows.
+    // What values that are not finite contribute to the rows that see them, of N blocks: the products' operand has zeros in
+    // their places, since a zero weight would not keep them out of the other rows.
+    template <int N>
     __device__ __forceinline__ void add_odd(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a, const Task& t, int at) {
         const int gq = (threadIdx.x & 63) >> 4;
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16 * N; ++i) {
             const Blk y = look(b, t, at + (i >> 4));
             const Where w = where<Q8>(c, sc, b, t, Inner{}, at + (i >> 4));
             if ((i & 15) >= y.nv || (w.info & kBad)) continue;
@@ -705,7 +706,7 @@ __device__ __forceinline__ void walk(const PagedCache& c, const PageScales& sc, 
             for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], sel);
             r.o[0][e] = mfma16<BF>(f, w[0], r.o[0][e]);
         }
-        if (part && __any(!fine)) r.add_odd(c, sc, b, a, t, at);
+        if (part && __any(!fine)) r.template add_odd<2>(c, sc, b, a, t, at);
     }
     if (at >= t.b1) return;
     run = find(turn + 1);                     // 32 more, outside the loop: a branch in it costs copies of the accumulators
@@ -723,12 +724,19 @@ struct StageLds {
     u32x4 k[kBlocks][NS][64];
     u32x4 v[E][kBlocks / 2][64];              // a column of each lane's, 32 positions each
     float ck[kBlocks], ev[kBlocks];           // 8-bit pages: the scores' factors and the values' exponents
-    int odd[kBlocks];                         // values that are not finite have been left out
+};
+// Blocks of a task whose values that are not finite have been left out, as the wave that brought them wrote them down: the
+// first kOdd of them, and where more lie.  Only what some row of the task does not see whole is looked at, about 6 blocks a
+// wave and all of a prefix where a sequence is shorter than its tokens.
+constexpr int kOdd = 8;
+struct OddLds {
+    alignas(16) int n[kBlocks];
+    int at[kBlocks][kOdd], from[kBlocks], to[kBlocks];
 };
 
 template <bool BF, bool Q8, int D, int NR>
 __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales& sc, const PagedBatch& b, const WinArgs& a,
-                                          const Task& t, StageLds<D> (&l)[2], Rows<BF, Q8, D, NR>& r) {
+                                          const Task& t, StageLds<D> (&l)[2], OddLds& odd, Rows<BF, Q8, D, NR>& r) {
     constexpr int E = D / 16, NS = (D + 31) / 32, EW = (E + 1) / 2;
     const int lane = threadIdx.x & 63, gq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = w * NR * 16;             // the wave's rows of the block
@@ -781,19 +789,21 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
 #pragma unroll
                 for (int m = 0; m < EW; ++m) v[i][m] = some ? sane<BF>(v[i][m], &fine) : 0;
             }
-            fine = !__any(!fine);
-            if (lane == 0) s.odd[w] = !fine;
+            if (__any(!fine) && lane == 0) {
+                const int n = odd.n[w]++;
+                if (n < kOdd) odd.at[w][n] = at;
+                if (n == kOdd) odd.from[w] = at;
+                odd.to[w] = at;
+            }
             if (bad)                          // its scores are NaN
 #pragma unroll
                 for (int k = 0; k < NS; ++k) s.k[w][k][lane] = u32x4{~0u, ~0u, ~0u, ~0u};
-            write_v(s, v);
-        } else {
-            if (lane == 0) s.odd[w] = 0;
-            write_v(s, v);
         }
+        write_v(s, v);
         if (Q8 && lane == 0) s.ck[w] = bad ? 1.f : ck, s.ev[w] = bad ? 0.f : ev;
     };
     int at = t.b0;
+    if (lane == 0) odd.n[w] = 0;              // (the wave's own until the first stage's barrier)
     // (the queries first: loads come back in order, and one that is still out when the loop begins would be waited for in
     // every stage)
     u32x4 q[NR][NS];
@@ -893,10 +903,22 @@ __device__ __forceinline__ void walk_wide(const PagedCache& c, const PageScales&
             factors(st, h);
             r.weights(s, wt, ck, ev);
             add();
-            if (st.odd[2 * h] | st.odd[2 * h + 1]) r.add_odd(c, sc, b, a, t, at + 2 * h);
         }
         ++turn, at += kBlocks;
         if (at >= t.b1) break;
+    }
+    // What was left out of a stage is missing to every row that sees it, also in waves that see all of the stage: here, behind
+    // the last stage's barrier, for both loops.
+    const u32x4 any = *(const u32x4*)odd.n;
+    if (!__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3])) return;
+#pragma unroll 1
+    for (int i = 0; i < kBlocks; ++i) {
+        const int n = __builtin_amdgcn_readfirstlane(odd.n[i]);
+#pragma unroll 1
+        for (int k = 0; k < min(n, kOdd); ++k) r.template add_odd<1>(c, sc, b, a, t, __builtin_amdgcn_readfirstlane(odd.at[i][k]));
+        if (n > kOdd)
+#pragma unroll 1
+            for (int k = odd.from[i]; k <= odd.to[i]; k += kBlocks) r.template add_odd<1>(c, sc, b, a, t, k);
     }
 }
 
@@ -1088,12 +1110,13 @@ template <bool BF, bool Q8, int D>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(2))) k_window_wide(PagedCache c, PageScales sc, PagedBatch b, WinArgs a) {
     constexpr int NR = kWideRows / 64;
     __shared__ StageLds<D> l[2];
+    __shared__ OddLds odd;
     Asked asked(a, 1);
     Task t;
     while (asked.template next<kWideRows>(c, b, a, t)) {
         Rows<BF, Q8, D, NR> r;
         __syncthreads();                      // an earlier task's LDS is read out
-        walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l, r);
+        walk_wide<BF, Q8, D, NR>(c, sc, b, a, t, l, odd, r);
         store<BF, Q8, D, NR, false>(a, t, asked.end(c, b), r, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NR * 16);
     }
 }
