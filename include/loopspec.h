@@ -641,17 +641,23 @@ typedef struct {
  * parent's positions.  The first child of a row takes its pages over; every other
  * one shares the full pages and has a page of its own for what the last one holds
  * (n positions, n = length mod page_size), to which keys and values (and scales)
- * of these positions are copied in each of the n_caches caches.  Pages that hold
+ * of these positions are copied in each of the n_caches caches.  A partly filled
+ * page, or one behind the positions, that refs counts more often than the parent's
+ * entries name it (a row was shortened into pages that it shares) is not taken
+ * over: the first child has a copy, or a new page within `room`, as others have,
+ * and lets it go.  So no other row holds the pages that a child appends to; a row
+ * that is shortened below the end of a page it shares is forked at that length
+ * before it is appended to.  Pages that hold
  * no position that the sequence's next one sees (window, sinks) are let go, and so
  * are those of rows without a child.  Then a child gets pages until it holds
  * those of `room` positions more.  refs_out counts the new table's entries in the
  * old one's place; new pages are those whose count has become 0, the lowest
- * first, in the order of children and positions.  Where none is left, or the
+ * first, in the order of children and positions (a last page that the first child
+ * has a copy of is not given out in the same step).  Where none is left, or the
  * table has no place, short counts and the entry is -1, as are all entries
- * without a page.  Children without a parent have length -1.  The last
- * page of a row must not be held by another.  scales: [n_caches] or NULL (16-bit
- * pages); a NULL k_dev marks a 16-bit cache.  Errors: EINVAL (arguments, checked
- * before any launch), EHIP. */
+ * without a page.  Children without a parent have length -1.  scales: [n_caches]
+ * or NULL (16-bit pages); a NULL k_dev marks a 16-bit cache.  Errors: EINVAL
+ * (arguments, checked before any launch), EHIP. */
 int loopspec_fork_pages(const loopspec_fork_args* args, const loopspec_paged_cache* caches,
                         const loopspec_page_scales* scales, int32_t n_caches, void* workspace_dev,
                         uint64_t workspace_bytes, void* stream);

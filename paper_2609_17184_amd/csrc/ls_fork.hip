@@ -8,7 +8,10 @@
 // pages and copies.  For few rows and pages one workgroup does all but the copies.
 //
 // Which child takes its parent's pages over is found by looking through the
-// children before it, so nothing has to be exchanged for it.
+// children before it, so nothing has to be exchanged for it.  It does not take
+// over what it would append to and others hold too (a row that was shortened into
+// a page it shares): the counts from before the step tell.  Such a page is let go
+// only when the free ones have been numbered, since others may copy from it.
 //
 // Measured, in a queue of calls (us): 192 children of 192 rows of up to 16 pages of
 // 64, 6 caches of 8 heads of 128 in 8 bits (48 MB): 28, the four launches 2 + 3 + 4 +
@@ -32,8 +35,8 @@ struct Fork {
     int n, m, width, ps, pages, P, W, S, room;
     int32_t *len_out, *table_out, *refs_out, *lack;
     int32_t* need;                            // [m + 1] pages that a child wants, then the number of the first of them; pages given out
-    int32_t* source;                          // [m] page that a child has a copy of, or -1
-    int32_t* free;                            // [pages] those given out, in rising order
+    int32_t* source;                          // [m] page that a child has a copy of, or -1; -2 - page if it is to be let go
+    int32_t* free;                            // [pages] the counts as they were, then the pages given out, in rising order
 };
 
 struct Copied {
@@ -74,32 +77,52 @@ struct InMemory {
     __device__ __forceinline__ void set(int x, int v) const { r[x] = v; }
 };
 
+// Which lanes' pages x (those that `ask`) others hold beside the row `from`: they count more than the row names them
+// (`before`, the counts as they were).
+__device__ __forceinline__ bool held_by_others(const Fork& f, const int32_t* before, const int32_t* from, int x, bool ask) {
+    const int lane = threadIdx.x & 63, count = ask ? before[x] : 0;
+    bool others = false;
+    for (unsigned long long left = __ballot(count > 1); left; left &= left - 1) {
+        const int l = __ffsll(left) - 1, y = __shfl(x, l);
+        int named = 0;
+        for (int i0 = 0; i0 < f.width; i0 += 64) named += __popcll(__ballot(i0 + lane < f.width && from[min(i0 + lane, f.width - 1)] == y));
+        if (lane == l) others = count > named;
+    }
+    return others;
+}
+
 // A wave's row j of the new table: what it takes over of its parent's, -1 elsewhere, kWanted where it is to get a page.
 // Gives the number of these.
 template <class R>
-__device__ int child_row(const Fork& f, const R& refs, int32_t* lack, int j) {
+__device__ int child_row(const Fork& f, const R& refs, const int32_t* before, int32_t* lack, int j) {
     const int lane = threadIdx.x & 63, p = f.parent[j];
     const int len = (unsigned)p < (unsigned)f.n ? f.seq_len[p] : -1;
     int32_t* const to = f.table_out + j * f.out_stride;
     int wants = 0, source = -1;
+    bool heir = false;
     if (len < 0) {
         for (int i = lane; i < f.width; i += 64) to[i] = -1;
     } else {
-        const bool heir = !has_child(f, p, j);
+        heir = !has_child(f, p, j);
         const int32_t* const from = f.table + p * f.stride;
         const int full = (int)min((int64_t)(len / f.ps), (int64_t)f.width), held = pages_of(f, len);
         const int64_t more = (min((int64_t)len, (int64_t)f.width * f.ps) + f.room + f.ps - 1) / f.ps;
         const int want = f.room ? (int)min(more, (int64_t)f.width) : held;
         for (int i0 = 0; i0 < f.width; i0 += 64) {
-            const int i = i0 + lane;
+            const int i = i0 + lane, x = i < f.width ? from[i] : -1;
+            const bool ok = page_ok(f, x), off = gone(f, len, i);
+            const bool others = heir && held_by_others(f, before, from, x, ok && !off && i >= full);
             int y = -1;
             if (i < f.width) {
-                const int x = from[i];
-                const bool ok = page_ok(f, x), off = gone(f, len, i);
                 if (heir) {
-                    if (ok && off) refs.add(x, -1);
-                    if (ok && !off) y = x;
-                    if (!ok && i >= held && i < want) y = kWanted;
+                    if (others && i < held) {
+                        y = kWanted, source = x;                    // (let go later)
+                    } else if (ok && (off || others)) {
+                        refs.add(x, -1);
+                    } else if (ok) {
+                        y = x;
+                    }
+                    if (i >= held && i < want && y < 0) y = kWanted;
                 } else if (i < full) {
                     if (ok && !off) y = x, refs.add(x, 1);
                 } else if (i < held) {
@@ -115,8 +138,14 @@ __device__ int child_row(const Fork& f, const R& refs, int32_t* lack, int j) {
     }
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) source = max(source, __shfl_xor(source, o));
-    if (lane == 0) f.source[j] = source, f.len_out[j] = len < 0 ? -1 : len;
+    if (lane == 0) f.source[j] = heir && source >= 0 ? -2 - source : source, f.len_out[j] = len < 0 ? -1 : len;
     return wants;
+}
+
+// An heir that has a copy of its last page lets that page go.
+template <class R>
+__device__ __forceinline__ void let_go(const Fork& f, const R& refs, int j) {
+    if (f.source[j] < -1) refs.add(-2 - f.source[j], -1);
 }
 
 // A row without a child lets its pages go; a wave's work.
@@ -200,7 +229,11 @@ __device__ int hand_out(const Fork& f, const R& refs, int32_t* need, int32_t* fr
 
 __global__ void __launch_bounds__(kT) k_fork_start(Fork f) {
     const int i = blockIdx.x * kT + threadIdx.x;
-    if (i < f.pages && f.refs_out != f.refs) f.refs_out[i] = f.refs[i];
+    if (i < f.pages) {
+        const int32_t count = f.refs[i];
+        f.free[i] = count;
+        if (f.refs_out != f.refs) f.refs_out[i] = count;
+    }
     if (i == 0) *f.lack = 0;
 }
 // a wave per child, then one per parent
@@ -208,7 +241,7 @@ __global__ void __launch_bounds__(kT) k_fork_rows(Fork f) {
     const int i = blockIdx.x * (kT / 64) + (threadIdx.x >> 6);
     const InMemory refs{f.refs_out};
     if (i < f.m) {
-        const int wants = child_row(f, refs, f.lack, i);
+        const int wants = child_row(f, refs, f.free, f.lack, i);
         if ((threadIdx.x & 63) == 0) f.need[i] = wants;
     } else if (i < f.m + f.n) {
         end_row(f, refs, i - f.m);
@@ -231,12 +264,12 @@ struct InLds {
 __global__ void __launch_bounds__(kMost) k_fork_small(Fork f) {
     __shared__ int refs[kFewPages], free[kFewPages], need[kFewRows + 1], lack;
     const int tid = threadIdx.x, w = tid >> 6;
-    for (int i = tid; i < f.pages; i += kMost) refs[i] = f.refs[i];
+    for (int i = tid; i < f.pages; i += kMost) refs[i] = free[i] = f.refs[i];
     if (tid == 0) lack = 0;
     __syncthreads();
     for (int i = w; i < f.m + f.n; i += kMost / 64) {
         if (i < f.m) {
-            const int wants = child_row(f, InLds{refs}, &lack, i);
+            const int wants = child_row(f, InLds{refs}, free, &lack, i);
             if ((tid & 63) == 0) need[i] = wants;
         } else {
             end_row(f, InLds{refs}, i - f.m);
@@ -246,19 +279,26 @@ __global__ void __launch_bounds__(kMost) k_fork_small(Fork f) {
     const int short_of = hand_out<kMost>(f, InLds{refs}, need, free);
     __syncthreads();
     const int given = need[f.m];
-    for (int i = tid; i < f.pages; i += kMost) f.refs_out[i] = refs[i];
+    // (a row's wave is the one that wrote it)
+    for (int j = w; j < f.m; j += kMost / 64) {
+        if ((tid & 63) == 0) let_go(f, InLds{refs}, j);
+        fill_row(f, free, j, need[j], given);
+    }
     for (int i = tid; i < given; i += kMost) f.free[i] = free[i];
     for (int i = tid; i <= f.m; i += kMost) f.need[i] = need[i];
     if (tid == 0) *f.lack = lack + short_of;
-    // (a row's wave is the one that wrote it)
-    for (int j = w; j < f.m; j += kMost / 64) fill_row(f, free, j, need[j], given);
+    __syncthreads();
+    for (int i = tid; i < f.pages; i += kMost) f.refs_out[i] = refs[i];
 }
 
 // Workgroup (child, y, z): positions of the child's last page, half a cache (keys or values) and a share of the pieces
-// each; the first one fills in the child's wanted entries as well.
+// each; the first one fills in the child's wanted entries and lets go what is left to, as well.
 __global__ void __launch_bounds__(kT) k_fork_copy(Fork f, CopySet set, int fill) {
-    const int j = blockIdx.x, first = f.need[j], given = f.need[f.m], src = f.source[j];
-    if (fill && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 64) fill_row(f, f.free, j, first, given);
+    const int j = blockIdx.x, first = f.need[j], given = f.need[f.m], source = f.source[j], src = source < -1 ? -2 - source : source;
+    if (fill && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 64) {
+        fill_row(f, f.free, j, first, given);
+        if (threadIdx.x == 0) let_go(f, InMemory{f.refs_out}, j);
+    }
     if (src < 0 || first >= given || (int)blockIdx.y >= 2 * set.n) return;
     const int dst = f.free[first], n = f.len_out[j] % f.ps;         // (the copy's page is the first that the child wants)
     const Copied& c = set.c[blockIdx.y >> 1];

@@ -195,7 +195,7 @@ def rope_append(q, k, v, cache, batch: Batch, freq=None, q_norm=None, k_norm=Non
     (None: no rotation), the first rot_dim elements of a head being rotated in halves.  Returns the queries: `out`
     (which may be q) or a new tensor, whose padding rows are then undefined.  Into a QuantizedCache keys and values go
     as codes: a block of 16 positions has the power of two that holds its largest magnitude within 448, and keeps the
-    one of positions it holds already where that is larger."""
+    one of positions it holds already where that is larger.  No two sequences may append to one page."""
     import torch
     tokens, heads = _heads(q, cache)
     _rows(k, cache.n_kv_heads, cache, tokens, "k", q.dtype)
@@ -290,7 +290,9 @@ def fork_pages(seq_len, table, parent, refs, caches, prefix_len: int = 0, window
     page_size).  refs [n_pages]: how many entries name a page (a prefix's pages have theirs from the caller).  A row's
     first child takes its pages over, others share the full ones and get a copy of what the last one holds; pages without
     a child, or that the next position does not see (window, sinks), are let go; every child then holds pages for
-    `room` more positions.  table's entries without a page lie outside the cache (-1), also those behind a row's last
+    `room` more positions.  What a child appends to it shares with nobody, as far as refs tells: a row that was shortened
+    into a page it shares must be forked at that length before it is appended to (its first child, too, then gets a copy
+    of that page's rest, and other pages behind it).  table's entries without a page lie outside the cache (-1), also those behind a row's last
     page.  Returns (seq_len, table, refs, short), new int32 tensors: short [1] counts the pages that were not to be had,
     whose entries are -1."""
     caches = list(caches)
