@@ -69,6 +69,11 @@ PROMPTS = {
     "two": (4, 4, 16, 64, "f16", [130, 70], [200, 71], 21),
     "short": (2, 2, 64, 16, "f16", [129], [100], 0),
     "short-prefix": (2, 2, 64, 16, "bf16", [129], [90], 300),
+    # rows of several tokens in blocks of 16, over a prefix with the other sequences' and alone
+    "few": (8, 2, 64, 16, "bf16", [9], [100], 0),
+    "few-short": (4, 2, 96, 32, "f16", [7, 3], [3, 130], 70),
+    "together": (8, 2, 128, 16, "bf16", [3] * 20, [30] * 20, 700),
+    "together-few": (4, 4, 32, 16, "f16", [2] * 5, [20] * 5, 900),
 }
 
 
