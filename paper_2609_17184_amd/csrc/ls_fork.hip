@@ -16,7 +16,7 @@
 // Measured, in a queue of calls (us): 192 children of 192 rows of up to 16 pages of
 // 64, 6 caches of 8 heads of 128 in 8 bits (48 MB): 28, the four launches 2 + 3 + 4 +
 // 14 (3.4 TB/s in the copies, a large copy 4.8) and the host's 28.  8 children of 4
-// rows: 21, all of it the host's; 5 + 4 in the two kernels, chains of loads.
+// rows: 22, all of it the host's; 6 + 4 in the two kernels, chains of loads.
 #include "ls_paged.h"
 
 #include <algorithm>
@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(kMost) k_fork_free(Fork f) {
 }
 
 // All of it but the copies for few rows and pages, with counts and lists in LDS: 4 rows, 8 children and 190 pages 24 us in
-// all instead of 31 (two launches less).  Of more rows a workgroup's 16 waves would take several each, one after another.
+// all instead of 31 (two launches less).  Of more rows a workgroup's 16 waves would take several each, one after another,
+// and look for heirs through all children each time.
 constexpr int kFewRows = 128, kFewPages = 4096;
 struct InLds {
     int* r;

@@ -18,9 +18,9 @@
 // Bound by memory and by the angles and codes beside it: 16001 tokens of 28 query
 // and 4 key and value heads of 128 (bf16, norms, half of a head rotated, 278 MB)
 // take 62 us, 4.5 TB/s, of which a large copy's rate is 59; 5 prompts of up to 900
-// tokens of 55 heads of 96 (fp16, 176 MB) 52 us, 3.4 TB/s, the run's angles anew in
-// each of its slices.  One token takes 4 us, a launch and the loads that wait for
-// each other.
+// tokens of 55 heads of 96 (fp16, 176 MB) 51 us, 3.4 TB/s, a head's loads behind the
+// angles, the next head's behind its codes, and the angles anew in each slice.  One
+// token takes 5 us, a launch and the loads that wait for each other.
 #include "ls_paged.h"
 
 #include <algorithm>
@@ -269,7 +269,8 @@ extern "C" int loopspec_rope_append_quantized(const loopspec_paged_cache* cache,
     int per = b.T > 1 << 22 || (b.q_start && b.T >= 8ll * b.B) ? 16 : 1;    // (a grid holds 2^32 threads)
     const int x = (b.T + per - 1) / per;
     // Slices of the heads, each of which takes the run's angles again: 1001 runs of 36 heads 60.6 us in one, 67.0 in two;
-    // 214 runs of 165 heads 57.3 in nine, 52.4 in seven, 54.2 in six, 53.2 in five, 65.2 in two.  Workgroups of 256 threads,
+    // 214 runs of 165 heads 57.3 in nine, 52.4 in seven, 54.2 in six, 53.2 in five, 65.2 in two: from five to seven is
+    // noise, and no other shapes were measured.  Workgroups of 256 threads,
     // whose share of the angles is twice as long, took 61.8 and 54.0 where these took 60.6 and 53, of 1024 67.0 and 58.4.
     const int most = per > 1 ? (items + kW - 1) / kW : (items * L + 64 * kW - 1) / (64 * kW);
     int slices = std::max(1, std::min(most, 1500 / x));

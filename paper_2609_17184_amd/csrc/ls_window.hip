@@ -33,19 +33,19 @@
 // tasks (k_window_waves).
 //
 // Measured (us a call), and what bounds it.  64 rows x 4 heads of 8 key/value
-// heads of 128 over 4100 of 12000 positions (bf16, 954 MB): 166, 5.7 TB/s; a large
-// copy moves 4.8.  32 rows of 16 heads of 128 over up to 8192 positions (fp16 over
-// 8-bit pages, 584 MB): 118, 4.9 TB/s, 5 of them the join.  8001 rows of 28 heads
-// on 4 of 128 under a window of 2048 (bf16, 206 GFLOP): 235, 880 TFLOP/s; the
-// matrix cores are busy 36 % of the cycles and vector instructions 41 %, which two
+// heads of 128 over 4100 of 12000 positions (bf16, 954 MB): 165, 5.8 TB/s; a plain
+// stream of reads reaches 7.2.  32 rows of 16 heads of 128 over up to 8192 positions
+// (fp16 over 8-bit pages, 584 MB): 117, of which 113 at 5.2 TB/s and 5 the join.
+// 8001 rows of 28 heads on 4 of 128 under a window of 2048 (bf16, 206 GFLOP): 234,
+// 880 TFLOP/s; the matrix cores are busy 36 % of the cycles and vector instructions 41 %, which two
 // waves a SIMD overlap in part only.  250 tokens of 32 heads on 8 of 128 behind
-// 8007 positions (bf16 over 8-bit pages, 33 GFLOP): 73, of which the own positions'
+// 8007 positions (bf16 over 8-bit pages, 33 GFLOP): 72, of which the own positions'
 // launch and the taking in of partial results 22.  5 prompts of up to 900 tokens,
-// 55 heads of 96 (fp16 over 8-bit pages, 66 GFLOP): 145; a task's begin and end
+// 55 heads of 96 (fp16 over 8-bit pages, 66 GFLOP): 143; a task's begin and end
 // (lengths, pages, first loads, the two stages that the diagonal cuts) take 13 of
 // the 25 that a block of 128 rows over 640 positions does, while the CU's other
-// workgroup goes on.  One token: 8, of which 3 are an empty launch and the rest
-// loads that wait for each other (lengths, pages, scales, keys).
+// workgroup goes on.  Three tokens of 4 heads: 9.2, of which 3 are an empty launch and
+// the rest loads that wait for each other (lengths, pages, scales, keys).
 #include <algorithm>
 
 #include "ls_paged.h"
@@ -1264,6 +1264,7 @@ int plan_of(const PagedCache& c, const PagedBatch& b, int H, int W, int S, Plan*
     // About 1024 tasks where the tables are full (over 18 batches of ragged lengths 384 to 1536 are within 3 %), of at least
     // two tiles a wave.  What is short (700 positions 15 us, in chunks of 8 tiles 11 + 5) is not cut, nor are prompts and
     // windows, whose tasks are alike, that fill the card (64 rows over 4096 of 12000 positions 168 us, cut in two 172 + 6).
+    // The join's time is not weighed: one row over 100000 positions takes 103 us in 126 chunks a head, in 32 83.
     if ((!p->wide_own && tiles <= kUncut) || ((p->wide_own || W < kAll) && blocks >= slots))
         p->CT = (int)tiles;
     else
