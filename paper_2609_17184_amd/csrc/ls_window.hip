@@ -37,8 +37,8 @@
 // stream of reads reaches 7.2.  32 rows of 16 heads of 128 over up to 8192 positions
 // (fp16 over 8-bit pages, 584 MB): 117, of which 113 at 5.2 TB/s and 5 the join.
 // 8001 rows of 28 heads on 4 of 128 under a window of 2048 (bf16, 206 GFLOP): 234,
-// 880 TFLOP/s; the matrix cores are busy 36 % of the cycles and vector instructions 41 %, which two
-// waves a SIMD overlap in part only.  250 tokens of 32 heads on 8 of 128 behind
+// 880 TFLOP/s; the matrix cores are busy 36 % of the cycles and vector instructions
+// 41 %, which two waves a SIMD overlap in part only.  250 tokens of 32 heads on 8 of 128 behind
 // 8007 positions (bf16 over 8-bit pages, 33 GFLOP): 72, of which the own positions'
 // launch and the taking in of partial results 22.  5 prompts of up to 900 tokens,
 // 55 heads of 96 (fp16 over 8-bit pages, 66 GFLOP): 143; a task's begin and end

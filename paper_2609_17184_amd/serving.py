@@ -288,13 +288,13 @@ def fork_pages(seq_len, table, parent, refs, caches, prefix_len: int = 0, window
     """A batch whose row i continues row parent[i] (int32 [children]; outside the rows: none) of the batch seq_len
     [rows], table [rows, pages] over the caches of all layers (PagedCache or QuantizedCache, of equal n_pages and
     page_size).  refs [n_pages]: how many entries name a page (a prefix's pages have theirs from the caller).  A row's
-    first child takes its pages over, others share the full ones and get a copy of what the last one holds; pages without
-    a child, or that the next position does not see (window, sinks), are let go; every child then holds pages for
-    `room` more positions.  What a child appends to it shares with nobody, as far as refs tells: a row that was shortened
-    into a page it shares must be forked at that length before it is appended to (its first child, too, then gets a copy
-    of that page's rest, and other pages behind it).  table's entries without a page lie outside the cache (-1), also those behind a row's last
-    page.  Returns (seq_len, table, refs, short), new int32 tensors: short [1] counts the pages that were not to be had,
-    whose entries are -1."""
+    first child takes its pages over, others share the full ones and get a copy of what the last one holds; pages
+    without a child, or that the next position does not see (window, sinks), are let go; every child then holds pages
+    for `room` more positions.  What a child appends to it shares with nobody, as far as refs tells: a row that was
+    shortened into a page it shares must be forked at that length before it is appended to (its first child, too, then
+    gets a copy of that page's rest, and other pages behind it).  table's entries without a page lie outside the cache
+    (-1), also those behind a row's last page.  Returns (seq_len, table, refs, short), new int32 tensors: short [1]
+    counts the pages that were not to be had, whose entries are -1."""
     caches = list(caches)
     _need(bool(caches), "caches: one or more")
     dev, n_pages, page_size = caches[0].device, caches[0].n_pages, caches[0].page_size
